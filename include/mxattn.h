@@ -91,8 +91,10 @@ typedef enum {
     MXATTN_ERR_BOUNDARY = 9,    /* a scale boundary q outside [4, 8], a
                                    boundary count outside [1, 64], or a
                                    pre-scale gamma not in (0, 3e38)         */
-    MXATTN_ERR_SCRATCH = 10     /* the problem needs more than the static
+    MXATTN_ERR_SCRATCH = 10,    /* the problem needs more than the static
                                    scratch of mxattn_cross_attend_noalloc   */
+    MXATTN_ERR_VALUE = 11       /* rot, pairs, eps or page_tokens outside what
+                                   the call takes, or Hq no multiple of Hkv  */
 } mxattn_status;
 
 #define MXATTN_AXIS_TOKENS 2   /* blocks along N (V)      */
@@ -276,6 +278,96 @@ int mxattn_cross_attend_noalloc(const uint8_t* q_codes, const uint8_t* q_scales,
                                 const uint8_t* k_scales, const uint8_t* v_codes, const uint8_t* v_scales,
                                 void* out, int64_t B, int64_t H, int64_t Nq, int64_t Nkv, int64_t d,
                                 int mode, void* stream);
+
+/* ---- Queries and keys before attention, and K and V kept between calls.
+ *
+ * Norm and rotation of a head's 128 channels x at a position, in fp32:
+ *   y = x / sqrt(mean(x^2) + eps) * w         (w null: y = x)
+ *   (a, b) -> (a cos - b sin, b cos + a sin)  for each pair of the first `rot`
+ *                                             channels (rot 0: none)
+ *   pairs     MXATTN_PAIRS_INTERLEAVED (2i, 2i+1) or MXATTN_PAIRS_HALVES
+ *             (i, i + rot/2), i < rot/2
+ *   rot       0, or a multiple of 16 up to 128
+ *   cos, sin  device fp32 [table_rows, rot/2], 16-byte aligned: row p is the
+ *             angles of position p.  A position outside [0, table_rows) makes the
+ *             row's rotated channels NaN.
+ *   w         device fp32 [128], 16-byte aligned
+ *   eps       finite, >= 0 (used where w is given)
+ * All strides are in elements, non-negative and multiples of 8; pointers of bf16
+ * data are 16-byte aligned. */
+#define MXATTN_PAIRS_INTERLEAVED 0
+#define MXATTN_PAIRS_HALVES 1
+
+/* Norm and rotation of Q [B, Hq, N, d] and K [B, Hkv, N, d] in one launch, each
+ * rounded once to bf16: what a projection wrote, in any order of its axes, becomes
+ * the operands of mxattn_forward or mxattn_cache_attend.
+ *   q, k            device bf16; k (with k_out) may be NULL: Q alone
+ *   *_strides       HOST int64[3], of batch, head and token; NULL: contiguous
+ *                   [B, H, N, d].  Output rows must not overlap one another.
+ *   positions       device int32 [B, N], or NULL: a token's index in its batch
+ * MXATTN_ERR_SHAPE if the span of an output (first to last byte) shares a byte
+ * with the span of an input or of the other output. */
+int mxattn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, int64_t B, int64_t Hq,
+                        int64_t Hkv, int64_t N, int64_t d, const int64_t* q_strides,
+                        const int64_t* k_strides, const int64_t* q_out_strides,
+                        const int64_t* k_out_strides, const float* q_weight, const float* k_weight,
+                        float eps, const float* cos, const float* sin, const int32_t* positions,
+                        int64_t table_rows, int64_t rot, int pairs, void* stream);
+
+/* The paged cache.  K and V are held as 8-bit codes (E4M3: 4 exponent and 3
+ * fraction bits, largest 448) with one E8M0 scale per block of 32 consecutive
+ * tokens of a sequence and head.  Pages of `page_tokens` tokens (a power of two,
+ * 32 to 4096) are given to sequences by a page table.
+ *   k_codes   uint8 [pages, Hkv, page_tokens/32, 8, 32, 16]: channel 16 c + i of
+ *             token t of a block at [c][t][i]
+ *   v_codes   uint8 [pages, Hkv, page_tokens/32, 128, 32]: channel, token
+ *   k_scales, v_scales  uint8 [pages, Hkv, page_tokens/32]
+ * all on the device, codes 16-byte aligned.  A call's tokens belong to sequences:
+ *   page_table  device int32 [seqs, max_pages]: the pages of a sequence in order;
+ *               entries past its length are not read
+ *   q_start     device int32 [seqs + 1], ascending from 0: sequence s owns the call's
+ *               tokens q_start[s] .. q_start[s+1] - 1 (it may own none); tokens
+ *               behind the last sequence are left alone
+ *   kv_len      device int32 [seqs]: the sequence's length with these tokens, which
+ *               are its last ones.  Token i of n has position kv_len - n + i.
+ * These arrays are read by the kernels only (4-byte aligned).  Bad contents read
+ * and write nothing out of range: a kv_len below 0 or past max_pages * page_tokens,
+ * or a page outside [0, pages), appends nothing there and gives NaN to every query
+ * that would see it. */
+
+/* Append the call's tokens to the cache: K normed and rotated (w, eps, cos, sin,
+ * table_rows, rot, pairs as above; positions: device int32 [tokens], or NULL: a
+ * token's place in its sequence) and rounded once, V as it is.  A block's exponent
+ * is the smallest e >= -127 with max|x| <= 448 2^e over its new tokens, and at
+ * least that of the block if it holds older tokens; if it grew, those are rounded
+ * again, code * 2^(e_old - e).  Rounding is to nearest, ties to even.  Values that
+ * are not finite are stored as NaN and do not count towards the maximum.  Bytes of
+ * tokens past the sequence's end are left as they were.  Tokens whose position is
+ * negative (kv_len < n) are not stored.  Two sequences of one call must not append
+ * to the same page (which of them is stored is undefined).
+ *   k, v   device bf16 [tokens, Hkv, d], heads contiguous, token strides
+ * MXATTN_ERR_SHAPE if k or v shares a byte with the cache. */
+int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t v_stride, uint8_t* k_codes,
+                        uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int64_t pages,
+                        int64_t page_tokens, const int32_t* page_table, const int32_t* q_start,
+                        const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t tokens, int64_t Hkv,
+                        int64_t d, const float* k_weight, float eps, const float* cos, const float* sin,
+                        const int32_t* positions, int64_t table_rows, int64_t rot, int pairs, void* stream);
+
+/* Attention of the call's tokens over their sequences' cached keys (their own
+ * among them, appended before): O = softmax(Q K^T / sqrt(d)) V in fp32, P rounded
+ * to bf16 before the product with V.  Query head i reads KV head i / (Hq / Hkv).
+ * causal != 0: token i of n sees positions 0 .. kv_len - n + i, else all kv_len.
+ * A query that sees no key gets 0.
+ *   q     device bf16 [tokens, Hq, d], heads contiguous, token stride
+ *   out   device bf16 [tokens, Hq, d], likewise; tokens of no sequence are not
+ *         written.  MXATTN_ERR_SHAPE if it shares a byte with q or the cache. */
+int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                        const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
+                        const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len,
+                        int64_t seqs, int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d,
+                        int causal, int64_t max_q, int64_t max_kv, void* out, int64_t out_stride,
+                        void* stream);
 
 /* Sizes of the code and scale arrays of a [B, H, N, d] tensor blocked along
  * `block_axis`; 0 for invalid arguments. */

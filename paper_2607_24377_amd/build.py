@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmxattn.so")
-SOURCES = ["api.hip", "quantize.hip", "attention.hip", "qmax.hip", "rowsum.hip"]
+SOURCES = ["api.hip", "quantize.hip", "attention.hip", "qmax.hip", "rowsum.hip", "rope.hip", "cache_append.hip",
+           "cache_attend.hip"]
 ARCH = "gfx950"
 
 

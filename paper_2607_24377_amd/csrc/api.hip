@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "../../include/mxattn.h"
+#include "cache.h"
 #include "launch.h"
 #include "workspace.h"
 
@@ -51,7 +52,7 @@ int rule_of(int mode) { return mode == MXATTN_OCP_VANILLA ? mxattn::kRuleOcp : m
 
 extern "C" {
 
-int mxattn_version(void) { return 101; }
+int mxattn_version(void) { return 102; }
 
 int mxattn_release_workspace(void) { return mxattn::release_workspace(); }
 
@@ -72,6 +73,7 @@ const char* mxattn_status_string(int s) {
         case MXATTN_ERR_HIP: return "HIP runtime error";
         case MXATTN_ERR_SCRATCH: return "problem too large for the static scratch of the no-allocation entry point (needs B*H*ceil(Nkv/128) <= 32768)";
         case MXATTN_ERR_BOUNDARY: return "invalid scale boundary (need 4 <= q <= 8 and 1 <= nq <= 64) or pre-scale (need 0 < gamma < 3e38)";
+        case MXATTN_ERR_VALUE: return "invalid value (rot 0 or a multiple of 16 up to 128, pairs 0 or 1, eps finite and >= 0, page_tokens a power of two from 32 to 4096, Hq a multiple of Hkv)";
         default: return "unknown status";
     }
 }
@@ -515,6 +517,215 @@ int mxattn_cross_forward(const void* q, const void* k, const void* v, void* out,
 int mxattn_forward(const void* q, const void* k, const void* v, void* out, int64_t B, int64_t H,
                    int64_t N, int64_t d, int mode, void* stream) {
     return mxattn_cross_forward(q, k, v, out, B, H, N, N, d, mode, stream);
+}
+
+// ---- norm and rotation, and the paged cache
+
+// The last byte + 1 of rows [B, H, N, 128] of bf16 by strides, from their start.
+static size_t span_bytes(int64_t B, int64_t H, int64_t N, const int64_t* s) {
+    return (size_t)(((B - 1) * s[0] + (H - 1) * s[1] + (N - 1) * s[2] + 128) * 2);
+}
+
+static int check_strides(const int64_t* s) {
+    for (int i = 0; i < 3; i++) {
+        if (s[i] < 0 || s[i] > (int64_t)1 << 36) return MXATTN_ERR_SHAPE;
+        if (s[i] % 8 != 0) return MXATTN_ERR_ALIGN;
+    }
+    return MXATTN_OK;
+}
+
+// Whether rows of 128 elements by these strides lie apart from one another: each
+// axis steps over all that the axes of smaller stride span.
+static bool rows_apart(int64_t B, int64_t H, int64_t N, const int64_t* s) {
+    int64_t extent[3] = {B, H, N}, stride[3] = {s[0], s[1], s[2]};
+    int64_t span = 128;
+    for (int i = 0; i < 3; i++) {
+        int least = -1;
+        for (int j = 0; j < 3; j++)
+            if (extent[j] > 1 && (least < 0 || stride[j] < stride[least])) least = j;
+        if (least < 0) return true;
+        if (stride[least] < span) return false;
+        span += (extent[least] - 1) * stride[least];
+        extent[least] = 1;
+    }
+    return true;
+}
+
+static int check_transform(const float* w0, const float* w1, float eps, const float* cos, const float* sin,
+                           const int32_t* positions, int64_t table_rows, int64_t rot, int pairs) {
+    if (rot < 0 || rot > 128 || rot % 16 != 0) return MXATTN_ERR_VALUE;
+    if (pairs != MXATTN_PAIRS_INTERLEAVED && pairs != MXATTN_PAIRS_HALVES) return MXATTN_ERR_VALUE;
+    if ((w0 || w1) && !(eps >= 0.0f && eps <= 3.0e38f)) return MXATTN_ERR_VALUE;
+    if (rot > 0) {
+        if (!cos || !sin) return MXATTN_ERR_NULL;
+        if (table_rows < 1 || table_rows > (int64_t)1 << 31) return MXATTN_ERR_SHAPE;
+        if (!aligned(cos, 16) || !aligned(sin, 16)) return MXATTN_ERR_ALIGN;
+    }
+    if (!aligned(w0, 16) || !aligned(w1, 16) || !aligned(positions, 4)) return MXATTN_ERR_ALIGN;
+    return MXATTN_OK;
+}
+
+int mxattn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, int64_t B, int64_t Hq, int64_t Hkv,
+                        int64_t N, int64_t d, const int64_t* q_strides, const int64_t* k_strides,
+                        const int64_t* q_out_strides, const int64_t* k_out_strides, const float* q_weight,
+                        const float* k_weight, float eps, const float* cos, const float* sin,
+                        const int32_t* positions, int64_t table_rows, int64_t rot, int pairs, void* stream) {
+    if (!q || !q_out || (k == nullptr) != (k_out == nullptr)) return MXATTN_ERR_NULL;
+    if (int st = check_shape(B, Hq, N, d)) return st;
+    if (k)
+        if (int st = check_shape(B, Hkv, N, d)) return st;
+    if (int st = check_transform(q_weight, k ? k_weight : nullptr, eps, cos, sin, positions, table_rows, rot, pairs))
+        return st;
+    const int64_t heads[2] = {Hq, k ? Hkv : 0};
+    const void* in[2] = {q, k};
+    void* out[2] = {q_out, k_out};
+    const int64_t* given[4] = {q_strides, k_strides, q_out_strides, k_out_strides};
+    int64_t strides[4][3];
+    mxattn::RopeArgs a{};
+    for (int i = 0; i < 4; i++) {
+        const int64_t H = heads[i & 1];
+        if (!H) continue;
+        const int64_t whole[3] = {H * N * 128, N * 128, 128};
+        for (int j = 0; j < 3; j++) strides[i][j] = given[i] ? given[i][j] : whole[j];
+        if (int st = check_strides(strides[i])) return st;
+    }
+    for (int i = 0; i < 2 && heads[i]; i++) {
+        if (!aligned(in[i], 16) || !aligned(out[i], 16)) return MXATTN_ERR_ALIGN;
+        if (!rows_apart(B, heads[i], N, strides[2 + i])) return MXATTN_ERR_SHAPE;
+        const size_t bytes = span_bytes(B, heads[i], N, strides[2 + i]);
+        for (int j = 0; j < 2 && heads[j]; j++) {
+            if (overlaps(out[i], bytes, in[j], span_bytes(B, heads[j], N, strides[j]))) return MXATTN_ERR_SHAPE;
+            if (j > i && overlaps(out[i], bytes, out[j], span_bytes(B, heads[j], N, strides[2 + j])))
+                return MXATTN_ERR_SHAPE;
+        }
+        a.in[i] = {static_cast<uint16_t*>(const_cast<void*>(in[i])), strides[i][0], strides[i][1], strides[i][2]};
+        a.out[i] = {static_cast<uint16_t*>(out[i]), strides[2 + i][0], strides[2 + i][1], strides[2 + i][2]};
+    }
+    a.w[0] = q_weight;
+    a.w[1] = k_weight;
+    a.t = {cos, sin, table_rows, eps, (int)rot};
+    a.positions = positions;
+    a.tokens = B * N;
+    a.N = (int)N;
+    a.Hq = (int)Hq;
+    a.Hkv = (int)heads[1];
+    hipError_t e = mxattn::launch_qk_norm_rope(a, pairs == MXATTN_PAIRS_HALVES, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) {
+        set_error("norm and rotation launch", e);
+        return MXATTN_ERR_HIP;
+    }
+    return MXATTN_OK;
+}
+
+// The checks that the calls on the paged cache share; fills c.
+static int check_cache(mxattn::CacheArgs& c, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                       const uint8_t* v_scales, int64_t pages, int64_t page_tokens, const int32_t* page_table,
+                       const int32_t* q_start, const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t tokens,
+                       int64_t Hkv, int64_t d) {
+    if (!k_codes || !k_scales || !v_codes || !v_scales || !page_table || !q_start || !kv_len) return MXATTN_ERR_NULL;
+    if (int st = check_shape(1, Hkv, tokens, d)) return st;
+    if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0) return MXATTN_ERR_VALUE;
+    const int64_t bpp = page_tokens / 32;
+    if (pages < 1 || pages > (int64_t)1 << 30 || pages * bpp > ((int64_t)1 << 40) / Hkv) return MXATTN_ERR_SHAPE;
+    if (seqs < 1 || seqs > 1 << 20 || max_pages < 1 || max_pages > ((int64_t)1 << 30) / page_tokens)
+        return MXATTN_ERR_SHAPE;
+    if (!aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(page_table, 4) || !aligned(q_start, 4) ||
+        !aligned(kv_len, 4))
+        return MXATTN_ERR_ALIGN;
+    c.kc = const_cast<uint8_t*>(k_codes);
+    c.vc = const_cast<uint8_t*>(v_codes);
+    c.ks = const_cast<uint8_t*>(k_scales);
+    c.vs = const_cast<uint8_t*>(v_scales);
+    c.page_table = page_table;
+    c.q_start = q_start;
+    c.kv_len = kv_len;
+    c.seqs = (int)seqs;
+    c.tokens = (int)tokens;
+    c.heads = (int)Hkv;
+    c.pages = (int)pages;
+    c.max_pages = (int)max_pages;
+    c.bpp_log2 = __builtin_ctzll((unsigned long long)bpp);
+    return MXATTN_OK;
+}
+
+// Whether `bytes` at p share a byte with the cache.
+static bool in_cache(const void* p, size_t bytes, const mxattn::CacheArgs& c) {
+    const size_t blocks = ((size_t)c.pages * (size_t)c.heads) << c.bpp_log2;
+    return overlaps(p, bytes, c.kc, blocks * mxattn::kBlockBytes) || overlaps(p, bytes, c.vc, blocks * mxattn::kBlockBytes) ||
+           overlaps(p, bytes, c.ks, blocks) || overlaps(p, bytes, c.vs, blocks);
+}
+
+// The bytes of `tokens` rows of `heads` heads, and the checks of their stride.
+static int check_rows(const void* p, int64_t stride, int64_t tokens, int64_t heads, bool apart, size_t& bytes) {
+    if (stride < (apart && tokens > 1 ? heads * 128 : 0) || stride > (int64_t)1 << 32) return MXATTN_ERR_SHAPE;
+    if (!aligned(p, 16) || stride % 8 != 0) return MXATTN_ERR_ALIGN;
+    bytes = (size_t)(((tokens - 1) * stride + heads * 128) * 2);
+    return MXATTN_OK;
+}
+
+int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t v_stride, uint8_t* k_codes,
+                        uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int64_t pages, int64_t page_tokens,
+                        const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len, int64_t seqs,
+                        int64_t max_pages, int64_t tokens, int64_t Hkv, int64_t d, const float* k_weight, float eps,
+                        const float* cos, const float* sin, const int32_t* positions, int64_t table_rows, int64_t rot,
+                        int pairs, void* stream) {
+    if (!k || !v) return MXATTN_ERR_NULL;
+    mxattn::AppendArgs a{};
+    if (int st = check_cache(a.c, k_codes, k_scales, v_codes, v_scales, pages, page_tokens, page_table, q_start, kv_len,
+                             seqs, max_pages, tokens, Hkv, d))
+        return st;
+    if (int st = check_transform(k_weight, nullptr, eps, cos, sin, positions, table_rows, rot, pairs)) return st;
+    if (Hkv > 65535) return MXATTN_ERR_SHAPE;
+    size_t kb = 0, vb = 0;
+    if (int st = check_rows(k, k_stride, tokens, Hkv, false, kb)) return st;
+    if (int st = check_rows(v, v_stride, tokens, Hkv, false, vb)) return st;
+    if (in_cache(k, kb, a.c) || in_cache(v, vb, a.c)) return MXATTN_ERR_SHAPE;
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.w = k_weight;
+    a.t = {cos, sin, table_rows, eps, (int)rot};
+    a.positions = positions;
+    hipError_t e = mxattn::launch_cache_append(a, pairs == MXATTN_PAIRS_HALVES, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) {
+        set_error("cache append launch", e);
+        return MXATTN_ERR_HIP;
+    }
+    return MXATTN_OK;
+}
+
+int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                        const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
+                        const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len, int64_t seqs,
+                        int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d, int causal,
+                        int64_t max_q, int64_t max_kv, void* out, int64_t out_stride, void* stream) {
+    if (!q || !out) return MXATTN_ERR_NULL;
+    mxattn::CacheAttendArgs a{};
+    if (int st = check_cache(a.c, k_codes, k_scales, v_codes, v_scales, pages, page_tokens, page_table, q_start, kv_len,
+                             seqs, max_pages, tokens, Hkv, d))
+        return st;
+    if (int st = check_shape(1, Hq, tokens, d)) return st;
+    if (Hq % Hkv != 0) return MXATTN_ERR_VALUE;
+    if (Hkv > 65535 || max_q < 0 || max_kv < 0) return MXATTN_ERR_SHAPE;
+    size_t qb = 0, ob = 0;
+    if (int st = check_rows(q, q_stride, tokens, Hq, false, qb)) return st;
+    if (int st = check_rows(out, out_stride, tokens, Hq, true, ob)) return st;
+    if (overlaps(out, ob, q, qb) || in_cache(out, ob, a.c)) return MXATTN_ERR_SHAPE;
+    a.q = static_cast<const uint16_t*>(q);
+    a.out = static_cast<uint16_t*>(out);
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.Hq = (int)Hq;
+    a.group = (int)(Hq / Hkv);
+    a.causal = causal != 0;
+    a.scale = 0.12751743082459868f;  // fp32(log2(e) / sqrt(128))
+    hipError_t e = mxattn::launch_cache_attend(a, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) {
+        set_error("cache attention launch", e);
+        return MXATTN_ERR_HIP;
+    }
+    return MXATTN_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,85 @@
+// cache.h -- argument structures and launchers of the operators around the
+// 8-bit paged cache: per-head norm and rotation (rope.hip), appending
+// (cache_append.hip) and attention over it (cache_attend.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mxattn {
+
+constexpr int kHeadDim = 128;
+constexpr int kBlockTokens = 32;   // tokens of a head that share a scale
+constexpr int kBlockBytes = 4096;  // codes of a block of K or V
+
+// Norm and rotation of one tensor's heads; w null: no norm, rot 0: no rotation.
+struct HeadTransform {
+    const float* cos;  // [table_rows, rot / 2]
+    const float* sin;
+    int64_t table_rows;
+    float eps;
+    int rot;
+};
+
+// A tensor [B, H, N, 128] of bf16 by the strides of its first three axes (elements).
+struct Strided {
+    uint16_t* p;
+    int64_t b, h, n;
+};
+
+struct RopeArgs {
+    Strided in[2], out[2];    // Q and K
+    const float* w[2];
+    HeadTransform t;
+    const int32_t* positions; // [B, N] or null: a token's index in its batch
+    int64_t tokens;           // B * N
+    int N, Hq, Hkv;
+    int heads_per_chunk;      // set by the launcher, with
+    int64_t first;            // the first token of a launch
+};
+hipError_t launch_qk_norm_rope(const RopeArgs& a, bool halves, hipStream_t stream);
+
+// The paged cache and what a call does with it.
+struct CacheArgs {
+    uint8_t *kc, *vc;           // [pages, heads, blocks per page, 4096]
+    uint8_t *ks, *vs;           // [pages, heads, blocks per page]
+    const int32_t* page_table;  // [seqs, max_pages]
+    const int32_t* q_start;     // [seqs + 1]
+    const int32_t* kv_len;      // [seqs]
+    int seqs, tokens, heads, pages, max_pages;
+    int bpp_log2;               // blocks per page
+};
+
+struct AppendArgs {
+    CacheArgs c;
+    const uint16_t *k, *v;  // [tokens, heads, 128] by token strides
+    int64_t k_stride, v_stride;
+    const float* w;
+    HeadTransform t;
+    const int32_t* positions;  // [tokens] or null: a token's place in its sequence
+};
+hipError_t launch_cache_append(const AppendArgs& a, bool halves, hipStream_t stream);
+
+struct CacheAttendArgs {
+    CacheArgs c;
+    const uint16_t* q;  // [tokens, Hq, 128] by its token stride
+    uint16_t* out;
+    int64_t q_stride, out_stride;
+    int Hq, group;      // group = Hq / heads
+    int causal;
+    float scale;        // log2(e) / sqrt(128)
+};
+hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t stream);
+
+// New tokens of sequence s: [first, last) of the call's tokens, whatever
+// q_start holds.
+struct TokenRange {
+    int first, last;
+};
+__device__ __forceinline__ TokenRange token_range(const CacheArgs& c, int s) {
+    const int a = min(max(c.q_start[s], 0), c.tokens);
+    const int b = min(max(c.q_start[s + 1], a), c.tokens);
+    return {a, b};
+}
+
+}  // namespace mxattn

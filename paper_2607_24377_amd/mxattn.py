@@ -67,6 +67,15 @@ def lib() -> ctypes.CDLL:
             L.mxattn_cross_attend_noalloc.argtypes = [P, P, P, P, P, P, P, I64, I64, I64, I64, I64, I, P]
             L.mxattn_cross_attend_noalloc.restype = I
             L.mxattn_attend.restype = I
+            L.mxattn_qk_norm_rope.argtypes = [P, P, P, P, I64, I64, I64, I64, I64, P, P, P, P, P, P, F, P, P, P,
+                                              I64, I64, I, P]
+            L.mxattn_qk_norm_rope.restype = I
+            L.mxattn_cache_append.argtypes = [P, P, I64, I64, P, P, P, P, I64, I64, P, P, P, I64, I64, I64, I64, I64,
+                                              P, F, P, P, P, I64, I64, I, P]
+            L.mxattn_cache_append.restype = I
+            L.mxattn_cache_attend.argtypes = [P, I64, P, P, P, P, I64, I64, P, P, P, I64, I64, I64, I64, I64, I64, I,
+                                              I64, I64, P, I64, P]
+            L.mxattn_cache_attend.restype = I
             L.mxattn_codes_bytes.argtypes = [I, I64, I64, I64, I64]
             L.mxattn_codes_bytes.restype = SZ
             L.mxattn_scales_bytes.argtypes = [I, I64, I64, I64, I64]
@@ -269,6 +278,167 @@ def cross_attend(qc, qs, kc, ks, vc, vs, Nq: int, Nkv: int, mode, out=None, stre
                                    vc.data_ptr(), vs.data_ptr(), out.data_ptr(), B, H, Nq, Nkv, d,
                                    _mode(mode), _stream(stream))
     _check(st, "mxattn_cross_attend")
+    return out
+
+
+PAIRS = {"interleaved": 0, "halves": 1}
+BLOCK_TOKENS = 32
+
+
+class _OnDevice:
+    """The stream to run on, with the tensors' device current while the call is made."""
+
+    def __init__(self, device, stream):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self.given = stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return _stream(self.given)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _tensor(t, name, dtype, device, shape=None):
+    """t's address; None passes as NULL.  Whole (contiguous) where a shape is given."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} on {device}")
+    if shape is not None and (t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _heads(t, name, device):
+    """Address and strides of a bf16 [B, H, N, d] tensor with contiguous channels."""
+    if t.dim() != 4 or t.dtype != torch.bfloat16 or t.device != device or not t.is_cuda or t.stride(3) != 1:
+        raise ValueError(f"{name} must be a bf16 [B, H, N, d] CUDA tensor on {device}, d contiguous")
+    return t.data_ptr(), (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def _tables(cos, sin, device):
+    """Addresses, rows and rotated channels of cos, sin [rows, rot / 2]; no rotation without them."""
+    if cos is None and sin is None:
+        return None, None, 0, 0
+    if cos is None or sin is None or cos.dim() != 2:
+        raise ValueError("cos and sin must both be given, [rows, rot / 2]")
+    return (_tensor(cos, "cos", torch.float32, device, cos.shape), _tensor(sin, "sin", torch.float32, device, cos.shape),
+            cos.shape[0], 2 * cos.shape[1])
+
+
+def _pairs(pairs) -> int:
+    return PAIRS[pairs] if isinstance(pairs, str) else int(pairs)
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weight=None, eps: float = 1e-6, cos=None,
+                 sin=None, positions=None, pairs="interleaved", q_out=None, k_out=None, stream=None):
+    """RMS norm of every head of bf16 q [B, Hq, N, d] and k [B, Hkv, N, d] (any strides; fp32 weights [d], None: no
+    norm) and their rotation by position (fp32 cos, sin [rows, rot / 2]; int32 positions [B, N], None: 0 .. N - 1);
+    returns (q_out, k_out), contiguous unless given.  k None: q alone."""
+    dev = q.device
+    qp, qs = _heads(q, "q", dev)
+    B, Hq, N, d = q.shape
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    elif q_out.shape != q.shape:
+        raise ValueError("q_out must have q's shape")
+    qop, qos = _heads(q_out, "q_out", dev)
+    kp = ks = kop = kos = None
+    Hkv = 0
+    if k is not None:
+        kp, ks = _heads(k, "k", dev)
+        Hkv = k.shape[1]
+        if k.shape != (B, Hkv, N, d):
+            raise ValueError("k must be [B, Hkv, N, d] with q's B, N, d")
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=dev)
+        elif k_out.shape != k.shape:
+            raise ValueError("k_out must have k's shape")
+        kop, kos = _heads(k_out, "k_out", dev)
+    elif k_out is not None or k_weight is not None:
+        raise ValueError("k_out and k_weight go with k")
+    cp, sp, rows, rot = _tables(cos, sin, dev)
+    with _OnDevice(dev, stream) as s:
+        st = lib().mxattn_qk_norm_rope(
+            qp, kp, qop, kop, B, Hq, Hkv, N, d, qs, ks, qos, kos, _tensor(q_weight, "q_weight", torch.float32, dev, (d,)),
+            _tensor(k_weight, "k_weight", torch.float32, dev, (d,)), eps, cp, sp,
+            _tensor(positions, "positions", torch.int32, dev, (B, N)), rows, rot, _pairs(pairs), s)
+    _check(st, "mxattn_qk_norm_rope")
+    return q_out, k_out
+
+
+def cache_shapes(pages: int, heads: int, page_tokens: int, d: int = 128):
+    """Shapes of the uint8 arrays of a paged cache: K codes, K scales, V codes, V scales."""
+    n = page_tokens // BLOCK_TOKENS
+    scales = (pages, heads, n)
+    return scales + (d // 16, BLOCK_TOKENS, 16), scales, scales + (d, BLOCK_TOKENS), scales
+
+
+def _token_rows(t, name, heads, device):
+    """Address and token stride of a bf16 [tokens, heads, d] tensor with contiguous heads."""
+    if (t.dim() != 3 or t.dtype != torch.bfloat16 or t.device != device or not t.is_cuda or t.stride(2) != 1
+            or (heads != 1 and t.stride(1) != t.shape[2])):
+        raise ValueError(f"{name} must be a bf16 [tokens, heads, d] CUDA tensor on {device}, heads contiguous")
+    return t.data_ptr(), t.stride(0)
+
+
+def _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, device):
+    """Checked addresses and sizes of a cache and its batch."""
+    if k_codes.dim() != 6:
+        raise ValueError("k_codes must be [pages, heads, page_tokens / 32, 8, 32, 16]")
+    pages, heads, blocks = k_codes.shape[:3]
+    shapes = cache_shapes(pages, heads, blocks * BLOCK_TOKENS, k_codes.shape[3] * 16)
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [seqs, max_pages]")
+    seqs, max_pages = page_table.shape
+    u8, i32 = torch.uint8, torch.int32
+    codes = (_tensor(k_codes, "k_codes", u8, device, shapes[0]), _tensor(k_scales, "k_scales", u8, device, shapes[1]),
+             _tensor(v_codes, "v_codes", u8, device, shapes[2]), _tensor(v_scales, "v_scales", u8, device, shapes[3]))
+    batch = (_tensor(page_table, "page_table", i32, device, page_table.shape),
+             _tensor(q_start, "q_start", i32, device, (seqs + 1,)), _tensor(kv_len, "kv_len", i32, device, (seqs,)))
+    return codes, (pages, blocks * BLOCK_TOKENS), batch, (seqs, max_pages), heads
+
+
+def cache_append(k: torch.Tensor, v: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len,
+                 k_weight=None, eps: float = 1e-6, cos=None, sin=None, positions=None, pairs="interleaved", stream=None):
+    """Append bf16 k, v [tokens, Hkv, d] to a paged cache (arrays of cache_shapes): k normed and rotated as by
+    qk_norm_rope on the way (int32 positions [tokens], None: a token's place in its sequence).  The call's tokens
+    q_start[s] .. q_start[s + 1] - 1 are the last ones of the kv_len[s] of sequence s."""
+    dev = k.device
+    codes, sizes, batch, counts, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
+    if k.shape != v.shape or k.dim() != 3 or k.shape[1] != heads:
+        raise ValueError("k and v must be [tokens, Hkv, d] with the cache's heads")
+    (kp, kst), (vp, vst) = _token_rows(k, "k", heads, dev), _token_rows(v, "v", heads, dev)
+    tokens, _, d = k.shape
+    cp, sp, rows, rot = _tables(cos, sin, dev)
+    with _OnDevice(dev, stream) as s:
+        st = lib().mxattn_cache_append(kp, vp, kst, vst, *codes, *sizes, *batch, *counts, tokens, heads, d,
+                                       _tensor(k_weight, "k_weight", torch.float32, dev, (d,)), eps, cp, sp,
+                                       _tensor(positions, "positions", torch.int32, dev, (tokens,)), rows, rot,
+                                       _pairs(pairs), s)
+    _check(st, "mxattn_cache_append")
+
+
+def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, causal: bool = True,
+                 max_q: int = 0, max_kv: int = 0, out=None, stream=None):
+    """Attention of bf16 q [tokens, Hq, d] over the sequences' cached keys; returns bf16 out [tokens, Hq, d]."""
+    dev = q.device
+    codes, sizes, batch, counts, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
+    qp, qst = _token_rows(q, "q", q.shape[1] if q.dim() == 3 else 0, dev)
+    tokens, Hq, d = q.shape
+    if out is None:
+        out = torch.empty((tokens, Hq, d), dtype=torch.bfloat16, device=dev)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    op, ost = _token_rows(out, "out", Hq, dev)
+    with _OnDevice(dev, stream) as s:
+        st = lib().mxattn_cache_attend(qp, qst, *codes, *sizes, *batch, *counts, tokens, Hq, heads, d, causal, max_q,
+                                       max_kv, op, ost, s)
+    _check(st, "mxattn_cache_attend")
     return out
 
 

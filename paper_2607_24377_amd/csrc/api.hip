@@ -720,12 +720,22 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
     a.group = (int)(Hq / Hkv);
     a.causal = causal != 0;
     a.scale = 0.12751743082459868f;  // fp32(log2(e) / sqrt(128))
-    hipError_t e = mxattn::launch_cache_attend(a, reinterpret_cast<hipStream_t>(stream));
+    const int64_t reach = max_pages * page_tokens;
+    if (max_kv == 0 || max_kv > reach) max_kv = reach;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const size_t bytes = mxattn::cache_attend_workspace(max_kv);
+    Workspace ws;
+    if (bytes) {
+        if (int st = ws.take(bytes, s)) return st;
+        a.workspace = ws.get();
+    }
+    int st = MXATTN_OK;
+    hipError_t e = mxattn::launch_cache_attend(a, max_kv, s);
     if (e != hipSuccess) {
         set_error("cache attention launch", e);
-        return MXATTN_ERR_HIP;
+        st = MXATTN_ERR_HIP;
     }
-    return MXATTN_OK;
+    return bytes ? ws.give_back(st) : st;
 }
 
 }  // extern "C"

@@ -68,8 +68,11 @@ struct CacheAttendArgs {
     int Hq, group;      // group = Hq / heads
     int causal;
     float scale;        // log2(e) / sqrt(128)
+    uint8_t* workspace; // cache_attend_workspace bytes
 };
-hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t stream);
+// max_kv: the longest sequence, as far as the caller knows (a wrong one costs time only).
+size_t cache_attend_workspace(int64_t max_kv);
+hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_kv, hipStream_t stream);
 
 // New tokens of sequence s: [first, last) of the call's tokens, whatever
 // q_start holds.

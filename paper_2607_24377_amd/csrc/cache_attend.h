@@ -1,0 +1,477 @@
+// cache_attend.h -- the arithmetic of attention over the 8-bit paged cache, and
+// how its work is divided over workgroups (device code of cache_attend.hip).
+// A row is one query token and head.  A wave holds 32 rows of a sequence that
+// share a KV head and walks cached blocks of 32 keys:
+//
+//   S^T = K Q^T   on the FP8 matrix cores (32x32x64), K's codes as they are.  A
+//                 bf16 number has 8 significant bits, two E4M3 numbers' worth:
+//                 Q = 2^e (hi + lo), hi the nearest E4M3 number to q 2^-e and lo
+//                 that of the rest, which leaves at most 2^-22 of the row's
+//                 largest magnitude.  Two FP8 products take the time of one in
+//                 bf16, and K needs no conversion;
+//   softmax       online, in fp32: m' = max(m, s c), p = exp2(s c - m');
+//   O^T += V^T P^T on the bf16 matrix cores: an E4M3 number times a power of two
+//                 is exact in bf16, and p is rounded to bf16 (2^-9 of a value
+//                 that is at most 1; l sums the unrounded p).
+//
+// As S^T has keys as rows, a lane holds the scores of one query.  The keys of a
+// block are taken in the order in which accumulator i of lane (query, half h) is
+// key 16 h + i, which is the operand order of the second product: no exchange
+// between lanes.  The cache stores K and V in these operands' orders.
+#pragma once
+
+#include "cache.h"
+#include "device_common.h"
+
+namespace mxattn {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// the running maximum before the first key: below every finite score, so that
+// masked scores (-inf) give p = 0 and never inf - inf
+constexpr float kNoMax = -3.0e38f;
+
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_fmaxf(a, b); }
+
+__device__ __forceinline__ float other_half(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x),
+                                                    false, false);
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? (uint32_t)r[0] : (uint32_t)r[1]);
+}
+
+// Q of one row as two E4M3 numbers per channel: lane (query, h) holds channels
+// 64 j + 32 h .. + 31 of product j.
+struct QOperand {
+    v8i hi[2], lo[2];
+    float c;  // scores times c are in units of log2: scale * 2^e; NaN for a row that is not finite
+};
+
+__device__ __forceinline__ QOperand load_q(const uint16_t* row, int h, float scale, bool live) {
+    uint4 raw[2][4];
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            raw[j][k] = live ? *reinterpret_cast<const uint4*>(row + 64 * j + 32 * h + 8 * k) : make_uint4(0, 0, 0, 0);
+            m = max_halves(m, raw[j][k]);
+        }
+    m = max(m & 0xFFFFu, m >> 16);
+    m = max(m, __builtin_bit_cast(uint32_t, other_half(__builtin_bit_cast(float, m))));
+    // the smallest e >= -127 with 1.f 2^(E-127) <= 448 2^e
+    const int e = max((int)(m >> 7) - 135 + ((m & 0x7Fu) > 0x60u ? 1 : 0), -127);
+    QOperand q;
+    q.c = m < 0x7F80u ? __builtin_ldexpf(scale, e) : __builtin_nanf("");
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const uint32_t u[4] = {raw[j][k].x, raw[j][k].y, raw[j][k].z, raw[j][k].w};
+#pragma unroll
+            for (int g = 0; g < 2; g++) {
+                float x[4];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    x[2 * i] = __builtin_ldexpf(__builtin_bit_cast(float, u[2 * g + i] << 16), -e);
+                    x[2 * i + 1] = __builtin_ldexpf(__builtin_bit_cast(float, u[2 * g + i] & 0xFFFF0000u), -e);
+                }
+                int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+                p = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], p, true);
+                const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(p, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(p, true);
+                int r = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - a[0]) * 16.f, (x[1] - a[1]) * 16.f, 0, false);
+                r = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - b[0]) * 16.f, (x[3] - b[1]) * 16.f, r, true);
+                q.hi[j][2 * k + g] = p;
+                q.lo[j][2 * k + g] = r;
+            }
+        }
+    return q;
+}
+
+__device__ __forceinline__ v8i join(uint4 a, uint4 b) {
+    return v8i{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
+}
+
+// The 32 x 32 scores of a block; `e` is the block's scale byte.
+__device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QOperand& q) {
+    v16f s;
+#pragma unroll
+    for (int i = 0; i < 16; i++) s[i] = 0.f;
+    constexpr int kOne = 0x7F7F7F7F, kSixteenth = 0x7B7B7B7B;  // 2^0, 2^-4
+    const v8i k0 = join(k[0], k[1]), k1 = join(k[2], k[3]);
+    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k0, q.lo[0], s, 0, 0, 0, e, 0, kSixteenth);
+    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k1, q.lo[1], s, 0, 0, 0, e, 0, kSixteenth);
+    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k0, q.hi[0], s, 0, 0, 0, e, 0, kOne);
+    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k1, q.hi[1], s, 0, 0, 0, e, 0, kOne);
+    return s;
+}
+
+// Eight codes (8 keys of a channel) as bf16, times the scale.
+__device__ __forceinline__ bf16x8 to_bf16(uint32_t a, uint32_t b, float scale) {
+    const bf16x2 w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
+    const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    const bf16x2 y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
+    const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+    return bf16x8{w[0], w[1], x[0], x[1], y[0], y[1], z[0], z[1]};
+}
+
+__device__ __forceinline__ bf16x8 probabilities(const v16f& p, int s) {
+    bf16x8 r;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const f32x2 a = {p[8 * s + 2 * i], p[8 * s + 2 * i + 1]};
+        const bf16x2 b = __builtin_convertvector(a, bf16x2);
+        r[2 * i] = b[0];
+        r[2 * i + 1] = b[1];
+    }
+    return r;
+}
+
+// A block of K and V in a wave's registers, with its scales; `lost`: no such page.
+struct Block {
+    uint4 k[4], v[4];
+    int ke;
+    float vs;
+    bool lost;
+};
+
+// The cache block `b` of sequence s and a head.
+struct BlockAt {
+    int64_t at;
+    bool lost;
+};
+__device__ __forceinline__ BlockAt block_at(const CacheArgs& c, int s, int head, int b) {
+    int page = c.page_table[(int64_t)s * c.max_pages + (b >> c.bpp_log2)];
+    const bool lost = (unsigned)page >= (unsigned)c.pages;
+    if (lost) page = 0;
+    return {(((int64_t)page * c.heads + head) << c.bpp_log2) + (b & ((1 << c.bpp_log2) - 1)), lost};
+}
+
+// The key of a block that is this lane's row of the K operand.
+__device__ __forceinline__ int operand_key(int q) { return 16 * ((q >> 2) & 1) + 4 * (q >> 3) + (q & 3); }
+
+__device__ __forceinline__ void load_block(Block& x, const CacheArgs& c, BlockAt p, int q, int h) {
+    const uint8_t* kb = c.kc + p.at * kBlockBytes + 2 * h * 512 + operand_key(q) * 16;
+    const uint8_t* vb = c.vc + p.at * kBlockBytes + q * 32 + 16 * h;
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int i = 0; i < 2; i++) x.k[2 * j + i] = *reinterpret_cast<const uint4*>(kb + (4 * j + i) * 512);
+#pragma unroll
+    for (int i = 0; i < 4; i++) x.v[i] = *reinterpret_cast<const uint4*>(vb + i * 1024);
+    x.ke = c.ks[p.at];
+    x.vs = e8m0_as_f32(c.vs[p.at]);
+    x.lost = p.lost;
+}
+
+// The running state of a wave's rows: lane (query, h) holds its half of l and
+// channels 32 n + 8 a + 4 h + b of O~ in O[n][4 a + b].
+struct State {
+    float m, l;
+    v16f O[4];
+    __device__ __forceinline__ void clear() {
+        m = kNoMax;
+        l = 0.f;
+#pragma unroll
+        for (int n = 0; n < 4; n++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) O[n][i] = 0.f;
+    }
+};
+
+// Bytes of v that are NaN codes, as 0x80 in each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t v) { return ((v & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+
+// A block that only some rows see and that holds NaN codes of V: a masked key
+// has p = 0, and 0 * NaN would reach every row.  The codes are taken out, and
+// the rows that see one get NaN: its count, from a product of ones.
+__device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], int visible, int h) {
+    bf16x8 seen[2];
+#pragma unroll
+    for (int i = 0; i < 16; i++) seen[i >> 3][i & 7] = 16 * h + i < visible ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll
+    for (int n = 0; n < 4; n++) {
+        uint32_t* x = reinterpret_cast<uint32_t*>(&v[n]);
+        uint32_t one[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t bad = nan_bytes(x[i]);
+            one[i] = (bad >> 7) * 0x38u;             // the code of 1
+            x[i] &= ~((bad >> 7) * 0xFFu);
+        }
+        v16f z;
+#pragma unroll
+        for (int i = 0; i < 16; i++) z[i] = 0.f;
+        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(one[0], one[1], 1.f), seen[0], z, 0, 0, 0);
+        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(one[2], one[3], 1.f), seen[1], z, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; i++) st.O[n][i] = z[i] > 0.f ? __builtin_nanf("") : st.O[n][i];
+    }
+}
+
+__device__ __forceinline__ bool has_nan(const uint4 (&v)[4]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int n = 0; n < 4; n++) m |= nan_bytes(v[n].x) | nan_bytes(v[n].y) | nan_bytes(v[n].z) | nan_bytes(v[n].w);
+    return m != 0;
+}
+
+// Softmax of a block's scores and their product with V; `visible`: keys of the
+// block that the lane's row sees (its first ones), `any`: some row does not see all.
+__device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float vscale, float c, int visible, bool any,
+                                        int h) {
+    if (any) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) s[i] = 16 * h + i < visible ? s[i] : -__builtin_inff();
+    }
+    float mx = max2(s[0], s[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) mx = max2(mx, max2(s[i], s[i + 1]));
+    mx *= c;
+    const float m = max2(st.m, max2(mx, other_half(mx)));
+    if (__any(m > st.m)) {  // else every alpha is 1
+        const float alpha = __builtin_amdgcn_exp2f(st.m - m);
+        st.m = m;
+        st.l *= alpha;
+#pragma unroll
+        for (int n = 0; n < 4; n++) st.O[n] *= alpha;
+    }
+    v16f p;
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m));
+        st.l += p[i];
+    }
+    const bf16x8 p0 = probabilities(p, 0), p1 = probabilities(p, 1);
+#pragma unroll
+    for (int n = 0; n < 4; n++) {
+        st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].x, v[n].y, vscale), p0, st.O[n], 0, 0, 0);
+        st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].z, v[n].w, vscale), p1, st.O[n], 0, 0, 0);
+    }
+}
+
+// One block for the wave's rows: `end` keys are the lane's row's, `keys` the
+// sequence's, `base` the block's first; `any`: some row does not see all of it.
+__device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand& q, int base, int end, int keys, bool any,
+                                             int h) {
+    if (any) {
+        // what lies behind the last key may be anything: zero
+        const int held = keys - base - 16 * h;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&x.v[i]);
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int left = held - 4 * j;
+                w[j] &= left <= 0 ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1;
+            }
+        }
+    }
+    if (x.lost) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) x.v[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (any && __any(has_nan(x.v))) spread_nan(st, x.v, end - base, h);
+    v16f s = scores(x.k, x.ke, q);
+    if (x.lost) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) s[i] = __builtin_nanf("");
+    }
+    consume(st, s, x.v, x.vs, q.c, end - base, any, h);
+}
+
+// ---------------------------------------------------------------------------
+// Division of the work.  An item is a tile of kRows rows of one sequence and KV
+// head; its weight is what it costs, in keys: the same for every tile of a
+// sequence, or, causal and with long runs of new tokens, growing by a constant
+// from tile to tile.  All items' weights in a row, sequence by sequence, head by
+// head, tile by tile, are cut into equal shares, one per workgroup, whatever the
+// lengths are: only the kernel sees them.  A share is a run of items, of which the
+// first and the last may be parts; a part's result (m, l, O~) goes to the
+// workgroup's slot in the workspace and the parts are joined by
+// cache_attend_join_kernel in a fixed order.
+
+// The tiles of a sequence: tile t of a head weighs a + b (t + 1).
+struct SeqWork {
+    int64_t a;
+    int tiles, b;
+    __device__ __forceinline__ int64_t before(int64_t t) const { return t * a + b * (t * (t + 1) / 2); }
+    __device__ __forceinline__ int64_t weight(int t) const { return a + (int64_t)b * (t + 1); }
+};
+
+// Keys of sequence s as far as they can be used: -1 where its length is impossible.
+__device__ __forceinline__ int keys_of(const CacheArgs& c, int s) {
+    const int len = c.kv_len[s];
+    return (unsigned)len > (unsigned)((c.max_pages << c.bpp_log2) * kBlockTokens) ? -1 : len;
+}
+
+template <int kRows, bool kGrowing>
+__device__ __forceinline__ SeqWork seq_work(const CacheAttendArgs& a, int s) {
+    const TokenRange r = token_range(a.c, s);
+    const int64_t rows = (int64_t)(r.last - r.first) * a.group;
+    const int keys = keys_of(a.c, s);
+    SeqWork w;
+    w.tiles = (int)((rows + kRows - 1) / kRows);
+    if (kGrowing && a.causal) {  // in units of a key times the group: kRows / group keys more per tile
+        w.a = (int64_t)max(keys - (r.last - r.first), 0) * a.group;
+        w.b = kRows;
+    } else {
+        w.a = max(keys, 1);
+        w.b = 0;
+    }
+    return w;
+}
+
+// A workgroup's place in the row of all items, and how far its share goes.
+struct Share {
+    int64_t at, end;  // of the total weight
+    int64_t offset;   // of `at` within sequence s
+    int s;
+};
+
+// The share of workgroup i of n; all kThreads threads call it.
+template <int kRows, bool kGrowing, int kThreads>
+__device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int n) {
+    __shared__ int64_t s_sum[kThreads / 64];
+    __shared__ Share s_share;
+    const int tid = threadIdx.x, seqs = a.c.seqs;
+    const int per = (seqs + kThreads - 1) / kThreads;
+    const int s0 = min(tid * per, seqs), s1 = min(s0 + per, seqs);
+    int64_t mine = 0;
+    for (int s = s0; s < s1; s++) {
+        const SeqWork w = seq_work<kRows, kGrowing>(a, s);
+        mine += w.before(w.tiles) * a.c.heads;
+    }
+    int64_t incl = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t x = __shfl_up(incl, d);
+        if ((tid & 63) >= d) incl += x;
+    }
+    if ((tid & 63) == 63) s_sum[tid >> 6] = incl;
+    if (tid == 0) s_share = {0, 0, 0, -1};
+    __syncthreads();
+    int64_t total = 0, before = incl - mine;
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; k++) {
+        if (k < (tid >> 6)) before += s_sum[k];
+        total += s_sum[k];
+    }
+    const int64_t lo = total * i / n, hi = total * (i + 1) / n;
+    if (before <= lo && lo < before + mine) {
+        int64_t at = before;
+        for (int s = s0; s < s1; s++) {
+            const SeqWork w = seq_work<kRows, kGrowing>(a, s);
+            const int64_t all = w.before(w.tiles) * a.c.heads;
+            if (lo < at + all) {
+                s_share = {lo, hi, lo - at, s};
+                break;
+            }
+            at += all;
+        }
+    }
+    __syncthreads();
+    return s_share;
+}
+
+// One item and the part of it that a workgroup works on.
+struct Item {
+    int s, head, row0;
+    int64_t x0, x1, w;  // from x0 to x1 of its weight w
+    __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == w; }
+};
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    const int lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return ((int64_t)hi << 32) | (uint32_t)lo;
+}
+
+// The item at the share's place; the share moves on behind it.
+template <int kRows, bool kGrowing>
+__device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
+    const SeqWork w = seq_work<kRows, kGrowing>(a, sh.s);
+    const int64_t per_head = w.before(w.tiles);
+    Item it;
+    it.s = sh.s;
+    it.head = (int)(sh.offset / per_head);
+    const int64_t r = sh.offset - it.head * per_head;
+    int t = 0;
+    if (w.b == 0) {
+        t = (int)(r / w.a);
+    } else {
+        int hi = w.tiles - 1;  // the last tile that starts at or before r
+        while (t < hi) {
+            const int mid = (t + hi + 1) >> 1;
+            if (w.before(mid) <= r)
+                t = mid;
+            else
+                hi = mid - 1;
+        }
+    }
+    it.row0 = t * kRows;
+    it.w = w.weight(t);
+    it.x0 = r - w.before(t);
+    it.x1 = it.x0 + (sh.end - sh.at) < it.w ? it.x0 + (sh.end - sh.at) : it.w;
+    const int64_t step = it.x1 - it.x0;
+    sh.at += step;
+    sh.offset += step;
+    if (sh.at < sh.end && sh.offset >= per_head * a.c.heads) {
+        sh.offset = 0;
+        do sh.s++;
+        while (sh.s < a.c.seqs - 1 && seq_work<kRows, kGrowing>(a, sh.s).tiles == 0);
+    }
+    return it;
+}
+
+// Which rows a tile has and what they see.
+struct TileRows {
+    int n, keys;           // the sequence's new tokens and keys
+    int rows;              // rows of the tile
+    int min_end, max_end;  // keys that its first and its last row see
+    int64_t first;         // the sequence's first token in the call
+    bool bad;              // no such cache
+};
+template <int kRows>
+__device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, int row0) {
+    const TokenRange r = token_range(a.c, s);
+    TileRows t;
+    t.n = r.last - r.first;
+    t.first = r.first;
+    const int keys = keys_of(a.c, s);
+    t.bad = keys < 0;
+    t.keys = max(keys, 0);
+    t.rows = min(kRows, t.n * a.group - row0);
+    t.min_end = a.causal ? t.keys - t.n + row0 / a.group + 1 : t.keys;
+    t.max_end = max(0, a.causal ? t.keys - t.n + (row0 + t.rows - 1) / a.group + 1 : t.keys);
+    return t;
+}
+
+// What a workgroup leaves for the join: `head`: its first item began in a share
+// before it (its part is in slot 2 i), and `ends` there; `tail`: its last item
+// goes on behind it (slot 2 i + 1).  A workgroup without a share leaves zeros.
+struct PartInfo {
+    int head, ends, tail;
+    int s, kv_head, row0;  // of the tail's item
+};
+
+// The workspace of n workgroups: their PartInfo, m and l of their slots' rows, O~.
+template <int kRows>
+struct Parts {
+    PartInfo* info;
+    float2* ml;   // [2 n, kRows]
+    float* o;     // [2 n, kRows, 128]
+    __device__ __forceinline__ Parts(uint8_t* ws, int n) {
+        o = reinterpret_cast<float*>(ws);
+        ml = reinterpret_cast<float2*>(ws + (size_t)2 * n * kRows * 512);
+        info = reinterpret_cast<PartInfo*>(ws + (size_t)2 * n * kRows * 520);
+    }
+};
+
+// Where row `row` of a tile's sequence lies in q or out.
+__device__ __forceinline__ int64_t row_offset(const CacheAttendArgs& a, int64_t first, int row, int head, int64_t stride) {
+    const int token = row / a.group;
+    return (first + token) * stride + (int64_t)(head * a.group + row - token * a.group) * kHeadDim;
+}
+
+}  // namespace mxattn

@@ -285,49 +285,56 @@ PAIRS = {"interleaved": 0, "halves": 1}
 BLOCK_TOKENS = 32
 
 
-class _OnDevice:
-    """The stream to run on, with the tensors' device current while the call is made."""
-
-    def __init__(self, device, stream):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-        self.given = stream
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return _stream(self.given)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _raw_stream(index: int) -> int:
+    """The device's current stream (torch.cuda.current_stream, which takes 4 us to make an object of it)."""
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _tensor(t, name, dtype, device, shape=None):
-    """t's address; None passes as NULL.  Whole (contiguous) where a shape is given."""
+def _run(fn, where: str, index: int, stream, args):
+    """fn(*args, stream) with device `index` current, on its current stream unless one is given."""
+    if index == torch._C._cuda_getDevice():
+        st = fn(*args, _raw_stream(index) if stream is None else _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, _raw_stream(index) if stream is None else _stream(stream))
+    if st != OK:
+        raise MxattnError(st, where)
+
+
+def _address(t, name, dtype, index, shape):
+    """The address of t, whole (contiguous) and of this shape on device `index`; NULL for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be {dtype} on {device}")
-    if shape is not None and (t.shape != shape or not t.is_contiguous()):
-        raise ValueError(f"{name} must be contiguous of shape {tuple(shape)}")
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of shape {tuple(shape)} on device {index}")
     return t.data_ptr()
 
 
-def _heads(t, name, device):
-    """Address and strides of a bf16 [B, H, N, d] tensor with contiguous channels."""
-    if t.dim() != 4 or t.dtype != torch.bfloat16 or t.device != device or not t.is_cuda or t.stride(3) != 1:
-        raise ValueError(f"{name} must be a bf16 [B, H, N, d] CUDA tensor on {device}, d contiguous")
-    return t.data_ptr(), (ctypes.c_int64 * 3)(*t.stride()[:3])
+def _index(t, name) -> int:
+    if t.dtype is not torch.bfloat16 or not t.is_cuda:
+        raise ValueError(f"{name} must be a bf16 CUDA tensor")
+    return t.get_device()
 
 
-def _tables(cos, sin, device):
+_Strides = ctypes.c_int64 * 3
+
+
+def _heads(t, name, index):
+    """Address and strides of a bf16 [B, H, N, d] tensor with contiguous channels (None: contiguous)."""
+    if t.dim() != 4 or t.dtype is not torch.bfloat16 or t.get_device() != index or t.stride(3) != 1:
+        raise ValueError(f"{name} must be a bf16 [B, H, N, d] CUDA tensor on device {index}, d contiguous")
+    return t.data_ptr(), None if t.is_contiguous() else _Strides(*t.stride()[:3])
+
+
+def _tables(cos, sin, index):
     """Addresses, rows and rotated channels of cos, sin [rows, rot / 2]; no rotation without them."""
     if cos is None and sin is None:
         return None, None, 0, 0
     if cos is None or sin is None or cos.dim() != 2:
         raise ValueError("cos and sin must both be given, [rows, rot / 2]")
-    return (_tensor(cos, "cos", torch.float32, device, cos.shape), _tensor(sin, "sin", torch.float32, device, cos.shape),
-            cos.shape[0], 2 * cos.shape[1])
+    shape = cos.shape
+    return (_address(cos, "cos", torch.float32, index, shape), _address(sin, "sin", torch.float32, index, shape),
+            shape[0], 2 * shape[1])
 
 
 def _pairs(pairs) -> int:
@@ -339,14 +346,16 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
     """RMS norm of every head of bf16 q [B, Hq, N, d] and k [B, Hkv, N, d] (any strides; fp32 weights [d], None: no
     norm) and their rotation by position (fp32 cos, sin [rows, rot / 2]; int32 positions [B, N], None: 0 .. N - 1);
     returns (q_out, k_out), contiguous unless given.  k None: q alone."""
-    dev = q.device
+    dev = _index(q, "q")
     qp, qs = _heads(q, "q", dev)
     B, Hq, N, d = q.shape
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        q_out = torch.empty((B, Hq, N, d), dtype=torch.bfloat16, device=q.device)
+        qop, qos = q_out.data_ptr(), None
     elif q_out.shape != q.shape:
         raise ValueError("q_out must have q's shape")
-    qop, qos = _heads(q_out, "q_out", dev)
+    else:
+        qop, qos = _heads(q_out, "q_out", dev)
     kp = ks = kop = kos = None
     Hkv = 0
     if k is not None:
@@ -355,19 +364,20 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
         if k.shape != (B, Hkv, N, d):
             raise ValueError("k must be [B, Hkv, N, d] with q's B, N, d")
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=dev)
+            k_out = torch.empty((B, Hkv, N, d), dtype=torch.bfloat16, device=q.device)
+            kop = k_out.data_ptr()
         elif k_out.shape != k.shape:
             raise ValueError("k_out must have k's shape")
-        kop, kos = _heads(k_out, "k_out", dev)
+        else:
+            kop, kos = _heads(k_out, "k_out", dev)
     elif k_out is not None or k_weight is not None:
         raise ValueError("k_out and k_weight go with k")
     cp, sp, rows, rot = _tables(cos, sin, dev)
-    with _OnDevice(dev, stream) as s:
-        st = lib().mxattn_qk_norm_rope(
-            qp, kp, qop, kop, B, Hq, Hkv, N, d, qs, ks, qos, kos, _tensor(q_weight, "q_weight", torch.float32, dev, (d,)),
-            _tensor(k_weight, "k_weight", torch.float32, dev, (d,)), eps, cp, sp,
-            _tensor(positions, "positions", torch.int32, dev, (B, N)), rows, rot, _pairs(pairs), s)
-    _check(st, "mxattn_qk_norm_rope")
+    f32 = torch.float32
+    _run((_lib or lib()).mxattn_qk_norm_rope, "mxattn_qk_norm_rope", dev, stream,
+         (qp, kp, qop, kop, B, Hq, Hkv, N, d, qs, ks, qos, kos, _address(q_weight, "q_weight", f32, dev, (d,)),
+          _address(k_weight, "k_weight", f32, dev, (d,)), eps, cp, sp,
+          _address(positions, "positions", torch.int32, dev, (B, N)), rows, rot, _pairs(pairs)))
     return q_out, k_out
 
 
@@ -378,29 +388,30 @@ def cache_shapes(pages: int, heads: int, page_tokens: int, d: int = 128):
     return scales + (d // 16, BLOCK_TOKENS, 16), scales, scales + (d, BLOCK_TOKENS), scales
 
 
-def _token_rows(t, name, heads, device):
+def _token_rows(t, name, index):
     """Address and token stride of a bf16 [tokens, heads, d] tensor with contiguous heads."""
-    if (t.dim() != 3 or t.dtype != torch.bfloat16 or t.device != device or not t.is_cuda or t.stride(2) != 1
-            or (heads != 1 and t.stride(1) != t.shape[2])):
-        raise ValueError(f"{name} must be a bf16 [tokens, heads, d] CUDA tensor on {device}, heads contiguous")
-    return t.data_ptr(), t.stride(0)
+    if t.dim() != 3 or t.dtype is not torch.bfloat16 or t.get_device() != index:
+        raise ValueError(f"{name} must be a bf16 [tokens, heads, d] CUDA tensor on device {index}")
+    stride, head, channel = t.stride()
+    if channel != 1 or (head != t.shape[2] and t.shape[1] != 1):
+        raise ValueError(f"{name}'s heads and channels must be contiguous")
+    return t.data_ptr(), stride
 
 
-def _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, device):
-    """Checked addresses and sizes of a cache and its batch."""
-    if k_codes.dim() != 6:
-        raise ValueError("k_codes must be [pages, heads, page_tokens / 32, 8, 32, 16]")
-    pages, heads, blocks = k_codes.shape[:3]
-    shapes = cache_shapes(pages, heads, blocks * BLOCK_TOKENS, k_codes.shape[3] * 16)
-    if page_table.dim() != 2:
-        raise ValueError("page_table must be [seqs, max_pages]")
+def _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, index):
+    """Checked addresses and sizes of a cache and its batch, as the library takes them, and the cache's heads."""
+    if k_codes.dim() != 6 or page_table.dim() != 2:
+        raise ValueError("k_codes must be [pages, heads, page_tokens / 32, 8, 32, 16], page_table [seqs, max_pages]")
+    pages, heads, blocks, chunks = k_codes.shape[:4]
     seqs, max_pages = page_table.shape
-    u8, i32 = torch.uint8, torch.int32
-    codes = (_tensor(k_codes, "k_codes", u8, device, shapes[0]), _tensor(k_scales, "k_scales", u8, device, shapes[1]),
-             _tensor(v_codes, "v_codes", u8, device, shapes[2]), _tensor(v_scales, "v_scales", u8, device, shapes[3]))
-    batch = (_tensor(page_table, "page_table", i32, device, page_table.shape),
-             _tensor(q_start, "q_start", i32, device, (seqs + 1,)), _tensor(kv_len, "kv_len", i32, device, (seqs,)))
-    return codes, (pages, blocks * BLOCK_TOKENS), batch, (seqs, max_pages), heads
+    u8, i32, scales = torch.uint8, torch.int32, (pages, heads, blocks)
+    return (_address(k_codes, "k_codes", u8, index, scales + (chunks, BLOCK_TOKENS, 16)),
+            _address(k_scales, "k_scales", u8, index, scales),
+            _address(v_codes, "v_codes", u8, index, scales + (16 * chunks, BLOCK_TOKENS)),
+            _address(v_scales, "v_scales", u8, index, scales), pages, blocks * BLOCK_TOKENS,
+            _address(page_table, "page_table", i32, index, (seqs, max_pages)),
+            _address(q_start, "q_start", i32, index, (seqs + 1,)), _address(kv_len, "kv_len", i32, index, (seqs,)), seqs,
+            max_pages), heads
 
 
 def cache_append(k: torch.Tensor, v: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len,
@@ -408,37 +419,32 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_codes, k_scales, v_codes, v
     """Append bf16 k, v [tokens, Hkv, d] to a paged cache (arrays of cache_shapes): k normed and rotated as by
     qk_norm_rope on the way (int32 positions [tokens], None: a token's place in its sequence).  The call's tokens
     q_start[s] .. q_start[s + 1] - 1 are the last ones of the kv_len[s] of sequence s."""
-    dev = k.device
-    codes, sizes, batch, counts, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
-    if k.shape != v.shape or k.dim() != 3 or k.shape[1] != heads:
-        raise ValueError("k and v must be [tokens, Hkv, d] with the cache's heads")
-    (kp, kst), (vp, vst) = _token_rows(k, "k", heads, dev), _token_rows(v, "v", heads, dev)
+    dev = _index(k, "k")
+    cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
+    (kp, kst), (vp, vst) = _token_rows(k, "k", dev), _token_rows(v, "v", dev)
     tokens, _, d = k.shape
+    if v.shape != k.shape or k.shape[1] != heads:
+        raise ValueError("k and v must be [tokens, Hkv, d] with the cache's heads")
     cp, sp, rows, rot = _tables(cos, sin, dev)
-    with _OnDevice(dev, stream) as s:
-        st = lib().mxattn_cache_append(kp, vp, kst, vst, *codes, *sizes, *batch, *counts, tokens, heads, d,
-                                       _tensor(k_weight, "k_weight", torch.float32, dev, (d,)), eps, cp, sp,
-                                       _tensor(positions, "positions", torch.int32, dev, (tokens,)), rows, rot,
-                                       _pairs(pairs), s)
-    _check(st, "mxattn_cache_append")
+    _run((_lib or lib()).mxattn_cache_append, "mxattn_cache_append", dev, stream,
+         (kp, vp, kst, vst, *cache, tokens, heads, d, _address(k_weight, "k_weight", torch.float32, dev, (d,)), eps, cp, sp,
+          _address(positions, "positions", torch.int32, dev, (tokens,)), rows, rot, _pairs(pairs)))
 
 
 def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, causal: bool = True,
                  max_q: int = 0, max_kv: int = 0, out=None, stream=None):
     """Attention of bf16 q [tokens, Hq, d] over the sequences' cached keys; returns bf16 out [tokens, Hq, d]."""
-    dev = q.device
-    codes, sizes, batch, counts, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
-    qp, qst = _token_rows(q, "q", q.shape[1] if q.dim() == 3 else 0, dev)
+    dev = _index(q, "q")
+    cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
+    qp, qst = _token_rows(q, "q", dev)
     tokens, Hq, d = q.shape
     if out is None:
-        out = torch.empty((tokens, Hq, d), dtype=torch.bfloat16, device=dev)
+        out = torch.empty((tokens, Hq, d), dtype=torch.bfloat16, device=q.device)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
-    op, ost = _token_rows(out, "out", Hq, dev)
-    with _OnDevice(dev, stream) as s:
-        st = lib().mxattn_cache_attend(qp, qst, *codes, *sizes, *batch, *counts, tokens, Hq, heads, d, causal, max_q,
-                                       max_kv, op, ost, s)
-    _check(st, "mxattn_cache_attend")
+    op, ost = _token_rows(out, "out", dev)
+    _run((_lib or lib()).mxattn_cache_attend, "mxattn_cache_attend", dev, stream,
+         (qp, qst, *cache, tokens, Hq, heads, d, causal, max_q, max_kv, op, ost))
     return out
 
 

@@ -73,7 +73,7 @@ const char* mxattn_status_string(int s) {
         case MXATTN_ERR_HIP: return "HIP runtime error";
         case MXATTN_ERR_SCRATCH: return "problem too large for the static scratch of the no-allocation entry point (needs B*H*ceil(Nkv/128) <= 32768)";
         case MXATTN_ERR_BOUNDARY: return "invalid scale boundary (need 4 <= q <= 8 and 1 <= nq <= 64) or pre-scale (need 0 < gamma < 3e38)";
-        case MXATTN_ERR_VALUE: return "invalid value (rot 0 or a multiple of 16 up to 128, pairs 0 or 1, eps finite and >= 0, page_tokens a power of two from 32 to 4096, Hq a multiple of Hkv)";
+        case MXATTN_ERR_VALUE: return "invalid value (rot 0 or a multiple of 16 up to 128, pairs 0 or 1, eps finite and >= 0, page_tokens a power of two from 32 to 4096, Hq a multiple of Hkv, at most 256 of it)";
         default: return "unknown status";
     }
 }
@@ -627,7 +627,7 @@ static int check_cache(mxattn::CacheArgs& c, const uint8_t* k_codes, const uint8
     if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0) return MXATTN_ERR_VALUE;
     const int64_t bpp = page_tokens / 32;
     if (pages < 1 || pages > (int64_t)1 << 30 || pages * bpp > ((int64_t)1 << 40) / Hkv) return MXATTN_ERR_SHAPE;
-    if (seqs < 1 || seqs > 1 << 20 || max_pages < 1 || max_pages > ((int64_t)1 << 30) / page_tokens)
+    if (seqs < 1 || seqs > 1 << 20 || max_pages < 1 || max_pages > mxattn::kMaxKeys / page_tokens)
         return MXATTN_ERR_SHAPE;
     if (!aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(page_table, 4) || !aligned(q_start, 4) ||
         !aligned(kv_len, 4))
@@ -706,7 +706,7 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
                              seqs, max_pages, tokens, Hkv, d))
         return st;
     if (int st = check_shape(1, Hq, tokens, d)) return st;
-    if (Hq % Hkv != 0) return MXATTN_ERR_VALUE;
+    if (Hq % Hkv != 0 || Hq / Hkv > 256) return MXATTN_ERR_VALUE;
     if (Hkv > 65535 || max_q < 0 || max_kv < 0) return MXATTN_ERR_SHAPE;
     size_t qb = 0, ob = 0;
     if (int st = check_rows(q, q_stride, tokens, Hq, false, qb)) return st;
@@ -722,15 +722,16 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
     a.scale = 0.12751743082459868f;  // fp32(log2(e) / sqrt(128))
     const int64_t reach = max_pages * page_tokens;
     if (max_kv == 0 || max_kv > reach) max_kv = reach;
+    if (max_q == 0 || max_q > tokens) max_q = tokens;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const size_t bytes = mxattn::cache_attend_workspace(max_kv);
+    const size_t bytes = mxattn::cache_attend_workspace(a, max_q, max_kv);
     Workspace ws;
     if (bytes) {
         if (int st = ws.take(bytes, s)) return st;
         a.workspace = ws.get();
     }
     int st = MXATTN_OK;
-    hipError_t e = mxattn::launch_cache_attend(a, max_kv, s);
+    hipError_t e = mxattn::launch_cache_attend(a, max_q, max_kv, s);
     if (e != hipSuccess) {
         set_error("cache attention launch", e);
         st = MXATTN_ERR_HIP;

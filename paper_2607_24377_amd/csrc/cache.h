@@ -70,9 +70,14 @@ struct CacheAttendArgs {
     float scale;        // log2(e) / sqrt(128)
     uint8_t* workspace; // cache_attend_workspace bytes
 };
-// max_kv: the longest sequence, as far as the caller knows (a wrong one costs time only).
-size_t cache_attend_workspace(int64_t max_kv);
-hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_kv, hipStream_t stream);
+// max_q, max_kv: most new tokens and keys of a sequence, as far as the caller knows
+// (wrong ones cost time only).
+size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv);
+hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream);
+
+// Tiles of 128 query rows (cache_attend_tiles.hip).
+size_t cache_attend_tiles_workspace();
+hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, hipStream_t stream);
 
 // New tokens of sequence s: [first, last) of the call's tokens, whatever
 // q_start holds.

@@ -136,13 +136,13 @@ struct Block {
     bool lost;
 };
 
-// The cache block `b` of sequence s and a head.
+// The cache block `b` of sequence s and a head (the same for the whole wave).
 struct BlockAt {
     int64_t at;
     bool lost;
 };
 __device__ __forceinline__ BlockAt block_at(const CacheArgs& c, int s, int head, int b) {
-    int page = c.page_table[(int64_t)s * c.max_pages + (b >> c.bpp_log2)];
+    int page = __builtin_amdgcn_readfirstlane(c.page_table[(int64_t)s * c.max_pages + (b >> c.bpp_log2)]);
     const bool lost = (unsigned)page >= (unsigned)c.pages;
     if (lost) page = 0;
     return {(((int64_t)page * c.heads + head) << c.bpp_log2) + (b & ((1 << c.bpp_log2) - 1)), lost};
@@ -217,6 +217,23 @@ __device__ __forceinline__ bool has_nan(const uint4 (&v)[4]) {
     return m != 0;
 }
 
+// V's codes of a block whose keys not every row sees, or of no page: `base` is its
+// first key's place where the lane's row sees `visible` keys and the sequence
+// holds `held`.
+__device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int base, int visible, int held, bool lost, int h) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            // what lies behind the last key may be anything: zero
+            const int left = lost ? 0 : held - base - 16 * h - 4 * j;
+            w[j] &= left <= 0 ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1;
+        }
+    }
+    if (__any(has_nan(v))) spread_nan(st, v, visible - base, h);
+}
+
 // Softmax of a block's scores and their product with V; `visible`: keys of the
 // block that the lane's row sees (its first ones), `any`: some row does not see all.
 __device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float vscale, float c, int visible, bool any,
@@ -255,24 +272,7 @@ __device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float 
 // sequence's, `base` the block's first; `any`: some row does not see all of it.
 __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand& q, int base, int end, int keys, bool any,
                                              int h) {
-    if (any) {
-        // what lies behind the last key may be anything: zero
-        const int held = keys - base - 16 * h;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&x.v[i]);
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const int left = held - 4 * j;
-                w[j] &= left <= 0 ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1;
-            }
-        }
-    }
-    if (x.lost) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) x.v[i] = make_uint4(0, 0, 0, 0);
-    }
-    if (any && __any(has_nan(x.v))) spread_nan(st, x.v, end - base, h);
+    if (any || x.lost) clean_values(st, x.v, 0, end - base, keys - base, x.lost, h);
     v16f s = scores(x.k, x.ke, q);
     if (x.lost) {
 #pragma unroll
@@ -327,8 +327,14 @@ __device__ __forceinline__ SeqWork seq_work(const CacheAttendArgs& a, int s) {
 struct Share {
     int64_t at, end;  // of the total weight
     int64_t offset;   // of `at` within sequence s
-    int s;
+    int64_t total;
+    int s, n;         // n: shares (no more than there is weight, so none is empty)
 };
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    const int lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return ((int64_t)hi << 32) | (uint32_t)lo;
+}
 
 // The share of workgroup i of n; all kThreads threads call it.
 template <int kRows, bool kGrowing, int kThreads>
@@ -350,7 +356,7 @@ __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int
         if ((tid & 63) >= d) incl += x;
     }
     if ((tid & 63) == 63) s_sum[tid >> 6] = incl;
-    if (tid == 0) s_share = {0, 0, 0, -1};
+    if (tid == 0) s_share = {0, 0, 0, 0, -1, 0};
     __syncthreads();
     int64_t total = 0, before = incl - mine;
 #pragma unroll
@@ -358,34 +364,32 @@ __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int
         if (k < (tid >> 6)) before += s_sum[k];
         total += s_sum[k];
     }
-    const int64_t lo = total * i / n, hi = total * (i + 1) / n;
-    if (before <= lo && lo < before + mine) {
+    n = (int)(total < n ? total : n);
+    const int64_t lo = i < n ? total * i / n : total, hi = i < n ? total * (i + 1) / n : total;
+    if (i < n && before <= lo && lo < before + mine) {
         int64_t at = before;
         for (int s = s0; s < s1; s++) {
             const SeqWork w = seq_work<kRows, kGrowing>(a, s);
             const int64_t all = w.before(w.tiles) * a.c.heads;
             if (lo < at + all) {
-                s_share = {lo, hi, lo - at, s};
+                s_share = {lo, hi, lo - at, total, s, n};
                 break;
             }
             at += all;
         }
     }
     __syncthreads();
-    return s_share;
+    return {uniform64(s_share.at), uniform64(s_share.end), uniform64(s_share.offset), uniform64(s_share.total),
+            __builtin_amdgcn_readfirstlane(s_share.s), __builtin_amdgcn_readfirstlane(s_share.n)};
 }
 
 // One item and the part of it that a workgroup works on.
 struct Item {
     int s, head, row0;
     int64_t x0, x1, w;  // from x0 to x1 of its weight w
+    int last;           // the workgroup of its last part
     __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == w; }
 };
-
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-    const int lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-    return ((int64_t)hi << 32) | (uint32_t)lo;
-}
 
 // The item at the share's place; the share moves on behind it.
 template <int kRows, bool kGrowing>
@@ -394,11 +398,11 @@ __device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
     const int64_t per_head = w.before(w.tiles);
     Item it;
     it.s = sh.s;
-    it.head = (int)(sh.offset / per_head);
-    const int64_t r = sh.offset - it.head * per_head;
+    it.head = __builtin_amdgcn_readfirstlane((int)(sh.offset / per_head));
+    const int64_t r = uniform64(sh.offset - it.head * per_head);
     int t = 0;
     if (w.b == 0) {
-        t = (int)(r / w.a);
+        t = __builtin_amdgcn_readfirstlane((int)(r / w.a));
     } else {
         int hi = w.tiles - 1;  // the last tile that starts at or before r
         while (t < hi) {
@@ -414,6 +418,9 @@ __device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
     it.x0 = r - w.before(t);
     it.x1 = it.x0 + (sh.end - sh.at) < it.w ? it.x0 + (sh.end - sh.at) : it.w;
     const int64_t step = it.x1 - it.x0;
+    // the share that holds the item's last unit of weight, y: the largest k with total k / n <= y
+    const int64_t y = sh.at + (it.w - it.x0) - 1;
+    it.last = __builtin_amdgcn_readfirstlane((int)(((y + 1) * sh.n - 1) / sh.total));
     sh.at += step;
     sh.offset += step;
     if (sh.at < sh.end && sh.offset >= per_head * a.c.heads) {
@@ -434,11 +441,12 @@ struct TileRows {
 };
 template <int kRows>
 __device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, int row0) {
-    const TokenRange r = token_range(a.c, s);
+    TokenRange r = token_range(a.c, s);
+    r = {__builtin_amdgcn_readfirstlane(r.first), __builtin_amdgcn_readfirstlane(r.last)};
     TileRows t;
     t.n = r.last - r.first;
     t.first = r.first;
-    const int keys = keys_of(a.c, s);
+    const int keys = __builtin_amdgcn_readfirstlane(keys_of(a.c, s));
     t.bad = keys < 0;
     t.keys = max(keys, 0);
     t.rows = min(kRows, t.n * a.group - row0);
@@ -447,12 +455,12 @@ __device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, i
     return t;
 }
 
-// What a workgroup leaves for the join: `head`: its first item began in a share
-// before it (its part is in slot 2 i), and `ends` there; `tail`: its last item
-// goes on behind it (slot 2 i + 1).  A workgroup without a share leaves zeros.
+// What workgroup i leaves for the join: `last` > i: its last item goes on behind
+// its share up to workgroup `last`'s; the item's parts are then in slots 2 i + 1,
+// 2 (i + 1), 2 (i + 2), ..., 2 last.
 struct PartInfo {
-    int head, ends, tail;
-    int s, kv_head, row0;  // of the tail's item
+    int last;
+    int s, head, row0;  // of that item
 };
 
 // The workspace of n workgroups: their PartInfo, m and l of their slots' rows, O~.
@@ -472,6 +480,106 @@ struct Parts {
 __device__ __forceinline__ int64_t row_offset(const CacheAttendArgs& a, int64_t first, int row, int head, int64_t stride) {
     const int token = row / a.group;
     return (first + token) * stride + (int64_t)(head * a.group + row - token * a.group) * kHeadDim;
+}
+
+// 1 / l, 0 for a row without keys.
+__device__ __forceinline__ float inverse(float l, bool bad) {
+    return bad ? __builtin_nanf("") : l == 0.f ? 0.f : 1.0f / l;
+}
+
+__device__ __forceinline__ uint2 bf16x4(float a, float b, float c, float d) {
+    const f32x2 x = {a, b}, y = {c, d};
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2)),
+                      __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2)));
+}
+
+// Four channels of a row, finished: O~ / l as bf16.
+__device__ __forceinline__ uint2 finished(float4 o, float l, bool bad) {
+    const float inv = inverse(l, bad);
+    return bf16x4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+}
+
+__device__ __forceinline__ void add_scaled(float4& o, const float4& x, float f) {
+    o.x = __builtin_fmaf(x.x, f, o.x);
+    o.y = __builtin_fmaf(x.y, f, o.y);
+    o.z = __builtin_fmaf(x.z, f, o.z);
+    o.w = __builtin_fmaf(x.w, f, o.w);
+}
+
+// Joins the parts of the item that began in workgroup blockIdx.x and went on
+// behind it, in the order of its keys: a row per group of 32 lanes, or, of many
+// parts, a row per workgroup, whose group g takes every eighth part.
+template <int kRows>
+__global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs a) {
+    __shared__ float4 s_o[8][32];
+    __shared__ float s_m[8], s_l[8];
+    const Parts<kRows> parts(a.workspace, gridDim.x);
+    const int i = blockIdx.x, tid = threadIdx.x;
+    const PartInfo info = parts.info[i];
+    if (info.last <= i) return;
+    const int count = info.last - i + 1;
+    auto slot = [i](int p) { return p ? 2 * (i + p) : 2 * i + 1; };
+    const TileRows t = tile_rows<kRows>(a, info.s, info.row0);
+    const int g = tid >> 5, ch = 4 * (tid & 31);
+    if (count <= 8) {  // a row for each group
+        for (int r = 8 * blockIdx.y + g; r < t.rows; r += 8 * gridDim.y) {
+            float m = kNoMax, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int p = 0; p < count; p++) m = max2(m, parts.ml[slot(p) * kRows + r].x);
+            for (int p = 0; p < count; p++) {
+                const float2 ml = parts.ml[slot(p) * kRows + r];
+                const float f = __builtin_amdgcn_exp2f(ml.x - m);
+                l = __builtin_fmaf(ml.y, f, l);
+                add_scaled(o, *reinterpret_cast<const float4*>(parts.o + ((int64_t)slot(p) * kRows + r) * kHeadDim + ch), f);
+            }
+            *reinterpret_cast<uint2*>(a.out + row_offset(a, t.first, info.row0 + r, info.head, a.out_stride) + ch) =
+                finished(o, l, t.bad);
+        }
+        return;
+    }
+    for (int r = blockIdx.y; r < t.rows; r += gridDim.y) {
+        float m = kNoMax, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = g; p < count; p += 8) m = max2(m, parts.ml[slot(p) * kRows + r].x);
+        for (int p = g; p < count; p += 8) {
+            const float2 ml = parts.ml[slot(p) * kRows + r];
+            const float f = __builtin_amdgcn_exp2f(ml.x - m);
+            l = __builtin_fmaf(ml.y, f, l);
+            add_scaled(o, *reinterpret_cast<const float4*>(parts.o + ((int64_t)slot(p) * kRows + r) * kHeadDim + ch), f);
+        }
+        s_o[g][tid & 31] = o;
+        if (ch == 0) {
+            s_m[g] = m;
+            s_l[g] = l;
+        }
+        __syncthreads();
+        if (g == 0) {
+            m = s_m[0];
+            for (int k = 1; k < 8; k++) m = max2(m, s_m[k]);
+            l = 0.f;
+            o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < 8; k++) {
+                const float f = __builtin_amdgcn_exp2f(s_m[k] - m);
+                l = __builtin_fmaf(s_l[k], f, l);
+                add_scaled(o, s_o[k][tid & 31], f);
+            }
+            *reinterpret_cast<uint2*>(a.out + row_offset(a, t.first, info.row0 + r, info.head, a.out_stride) + ch) =
+                finished(o, l, t.bad);
+        }
+        __syncthreads();
+    }
+}
+
+template <int kRows>
+inline hipError_t launch_cache_attend_join(const CacheAttendArgs& a, int workgroups, int64_t rows, hipStream_t stream) {
+    // a tile's rows over several workgroups (most have no item to join and end at once)
+    cache_attend_join_kernel<kRows><<<dim3(workgroups, (unsigned)((rows + 7) / 8)), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+template <int kRows>
+inline size_t parts_bytes(int workgroups) {
+    return (size_t)workgroups * (2 * kRows * 520 + sizeof(PartInfo));
 }
 
 }  // namespace mxattn

@@ -16,21 +16,6 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 32;
 constexpr int kRowFloats = 132;  // a row of O~ in LDS: 128 channels, padded off the banks of its neighbours
 
-// Four channels of a row, finished: O~ / l as bf16; a row without keys is 0.
-__device__ __forceinline__ uint2 finished(float4 o, float l, bool bad) {
-    const float inv = bad ? __builtin_nanf("") : l == 0.f ? 0.f : 1.0f / l;
-    const f32x2 x = {o.x * inv, o.y * inv}, y = {o.z * inv, o.w * inv};
-    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2)),
-                      __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2)));
-}
-
-__device__ __forceinline__ void add_scaled(float4& o, const float4& x, float f) {
-    o.x = __builtin_fmaf(x.x, f, o.x);
-    o.y = __builtin_fmaf(x.y, f, o.y);
-    o.z = __builtin_fmaf(x.z, f, o.z);
-    o.w = __builtin_fmaf(x.w, f, o.w);
-}
-
 // kDivided: shares of the work by workgroup (cache_attend.h); else one workgroup per
 // item, numbered as the workgroups of the append: sequence s has tiles
 // q_start[s] * group / 32 + s onwards.
@@ -46,7 +31,6 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
     PartInfo info{};
     if constexpr (kDivided) {
         sh = find_share<kRows, false, kThreads>(a, blockIdx.x, gridDim.x);
-        sh = {uniform64(sh.at), uniform64(sh.end), uniform64(sh.offset), __builtin_amdgcn_readfirstlane(sh.s)};
     } else {
         __shared__ int s_seq;
         if (tid == 0) s_seq = -1;
@@ -60,7 +44,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
         const int s = __builtin_amdgcn_readfirstlane(s_seq);
         if (s < 0) return;
         const TokenRange r = token_range(c, s);
-        it = {s, (int)blockIdx.y, (int)(blockIdx.x - ((int64_t)r.first * a.group / kRows + s)) * kRows, 0, 1, 1};
+        it = {s, (int)blockIdx.y, (int)(blockIdx.x - ((int64_t)r.first * a.group / kRows + s)) * kRows, 0, 1, 1, 0};
         if (it.row0 >= (r.last - r.first) * a.group) return;
         sh.end = 1;
     }
@@ -130,80 +114,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
                 if (ch == 0) parts.ml[slot * kRows + r] = make_float2(m, sum);
             }
         }
-        if (it.x0 > 0) {
-            info.head = 1;
-            info.ends = it.x1 == it.w;
-        } else if (!whole) {
-            info.tail = 1;
-            info.s = it.s;
-            info.kv_head = it.head;
-            info.row0 = it.row0;
-        }
+        if (it.x0 == 0 && !whole) info = {it.last, it.s, it.head, it.row0};
         first = false;
     }
     if (kDivided && tid == 0) parts.info[blockIdx.x] = info;
-}
-
-// Joins the parts of the item that began in workgroup blockIdx.x and went on
-// behind it, in the order of its keys: lane group g of 8 takes every eighth part,
-// then the eight meet in LDS.
-template <int kRows>
-__global__ __launch_bounds__(kThreads) void cache_attend_join_kernel(CacheAttendArgs a) {
-    __shared__ float4 s_o[8][32];
-    __shared__ float s_m[8], s_l[8];
-    __shared__ int s_count;
-    __shared__ int s_slot[1024];
-    const Parts<kRows> parts(a.workspace, gridDim.x);
-    const int i = blockIdx.x, tid = threadIdx.x;
-    const PartInfo info = parts.info[i];
-    if (!info.tail) return;
-    // the parts: this workgroup's tail, then the heads of those behind it up to the one where it ends
-    if (tid == 0) {
-        int n = 1;
-        s_slot[0] = 2 * i + 1;
-        for (int k = i + 1; k < (int)gridDim.x; k++) {
-            const PartInfo p = parts.info[k];
-            if (!p.head) continue;  // no share of its own
-            s_slot[n++] = 2 * k;
-            if (p.ends) break;
-        }
-        s_count = n;
-    }
-    __syncthreads();
-    const int count = s_count;
-    const TileRows t = tile_rows<kRows>(a, info.s, info.row0);
-    const int g = tid >> 5, ch = 4 * (tid & 31);
-    for (int r = 0; r < t.rows; r++) {
-        float m = kNoMax, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int p = g; p < count; p += 8) m = max2(m, parts.ml[s_slot[p] * kRows + r].x);
-        for (int p = g; p < count; p += 8) {
-            const float2 ml = parts.ml[s_slot[p] * kRows + r];
-            const float f = __builtin_amdgcn_exp2f(ml.x - m);
-            l = __builtin_fmaf(ml.y, f, l);
-            add_scaled(o, *reinterpret_cast<const float4*>(parts.o + ((int64_t)s_slot[p] * kRows + r) * kHeadDim + ch), f);
-        }
-        s_o[g][tid & 31] = o;
-        if (ch == 0) {
-            s_m[g] = m;
-            s_l[g] = l;
-        }
-        __syncthreads();
-        if (g == 0) {
-            m = s_m[0];
-            for (int k = 1; k < 8; k++) m = max2(m, s_m[k]);
-            l = 0.f;
-            o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k = 0; k < 8; k++) {
-                const float f = __builtin_amdgcn_exp2f(s_m[k] - m);
-                l = __builtin_fmaf(s_l[k], f, l);
-                add_scaled(o, s_o[k][tid & 31], f);
-            }
-            *reinterpret_cast<uint2*>(a.out + row_offset(a, t.first, info.row0 + r, info.kv_head, a.out_stride) + ch) =
-                finished(o, l, t.bad);
-        }
-        __syncthreads();
-    }
 }
 
 // Two workgroups per CU are resident (registers).
@@ -213,17 +127,22 @@ constexpr int64_t kUndivided = 1024;
 
 bool divided(int64_t max_kv) { return max_kv > kUndivided; }
 
+// Query rows of a sequence and head from which tiles of 128 rows pay.
+constexpr int64_t kTileRows = 64;
+bool tiled(const CacheAttendArgs& a, int64_t max_q) { return max_q * a.group > kTileRows; }
+
 }  // namespace
 
-size_t cache_attend_workspace(int64_t max_kv) {
-    return divided(max_kv) ? (size_t)kWorkgroups * (2 * kRows * 520 + sizeof(PartInfo)) : 0;
+size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    return tiled(a, max_q) ? cache_attend_tiles_workspace() : divided(max_kv) ? parts_bytes<kRows>(kWorkgroups) : 0;
 }
 
-hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_kv, hipStream_t stream) {
+hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream) {
+    if (tiled(a, max_q)) return launch_cache_attend_tiles(a, stream);
     if (divided(max_kv)) {
         cache_attend_kernel<true><<<kWorkgroups, kThreads, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
-        cache_attend_join_kernel<kRows><<<kWorkgroups, kThreads, 0, stream>>>(a);
+        return launch_cache_attend_join<kRows>(a, kWorkgroups, max_q * a.group < kRows ? max_q * a.group : kRows, stream);
     } else {
         const dim3 grid((unsigned)((int64_t)a.c.tokens * a.group / kRows + a.c.seqs), (unsigned)a.c.heads);
         cache_attend_kernel<false><<<grid, kThreads, 0, stream>>>(a);

@@ -1,0 +1,216 @@
+// cache_attend_tiles.hip -- attention over the 8-bit paged cache where a sequence
+// has many query rows per KV head (prompts, a video's next frame): bound by the
+// matrix cores and the softmax's vector work.
+//
+// A workgroup takes a tile of 128 rows, 32 per wave, and walks its keys 64 at a
+// time.  K's and V's codes (16 KiB) are copied straight into LDS, in the lanes'
+// operand order, two tiles of keys ahead of their use, and each wave reads them as
+// they are: FP8 operands for the scores, and codes that become bf16 in registers for
+// the second product.  The score products of the next 64 keys run under the
+// softmax of these.
+#include "cache_attend.h"
+
+namespace mxattn {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kRows = 32 * kWaves;
+constexpr int kKeys = 64;               // keys of a step: two blocks
+constexpr int kStageBytes = 4 * kBlockBytes;  // K, K, V, V
+
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+
+// What a step's operands need beside their codes.
+struct Scales {
+    int k[2];
+    float v[2];
+    bool lost[2];
+};
+
+// Copies of a step's blocks into LDS: part p (1 KiB) of a block is the operand
+// register group p of all lanes, 16 bytes each.  Wave w copies part w of each.
+struct StepLoader {
+    int koff, voff;  // of this lane in a block
+    int wave;
+    __device__ __forceinline__ StepLoader(int wave_, int lane) : wave(wave_) {
+        const int q = lane & 31, h = lane >> 5;
+        koff = (4 * (wave >> 1) + 2 * h + (wave & 1)) * 512 + operand_key(q) * 16;
+        voff = wave * 1024 + q * 32 + 16 * h;
+    }
+    __device__ __forceinline__ void copy(const uint8_t* block, int off, uint8_t* dst) const {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)block, 0, kBlockBytes, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(dst + wave * 1024), 16, off, 0, 0, 0);
+    }
+    // Blocks b and b + 1 (the second only below `blocks`: else the first again, for keys that are masked).
+    __device__ __forceinline__ void load(Scales& s, uint8_t* stage, const CacheArgs& c, int seq, int head, int b,
+                                         int blocks) const {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const BlockAt p = block_at(c, seq, head, min(b + i, blocks - 1));
+            copy(c.kc + p.at * kBlockBytes, koff, stage + i * kBlockBytes);
+            copy(c.vc + p.at * kBlockBytes, voff, stage + (2 + i) * kBlockBytes);
+            s.k[i] = c.ks[p.at];
+            s.v[i] = e8m0_as_f32(c.vs[p.at]);
+            s.lost[i] = p.lost;
+        }
+    }
+};
+
+__device__ __forceinline__ uint4 part(const uint8_t* block, int p, int lane) {
+    return *reinterpret_cast<const uint4*>(block + p * 1024 + lane * 16);
+}
+
+__device__ __forceinline__ v16f block_scores(const uint8_t* block, int e, const QOperand& q, int lane) {
+    uint4 k[4];
+#pragma unroll
+    for (int p = 0; p < 4; p++) k[p] = part(block, p, lane);
+    return scores(k, e, q);
+}
+
+// The softmax of a step's scores and its products with V.  `visible`: keys of the
+// step that the lane's row sees; `held`: keys that the sequence has in it; `any`:
+// whether some row does not see all.
+__device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* stage, const Scales& x, float c, int visible,
+                                     int held, bool any, int h, int lane) {
+    const bool lost = x.lost[0] || x.lost[1];
+    if (any || lost) {
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float y = x.lost[b] ? __builtin_nanf("") : s[b][i];
+                s[b][i] = 32 * b + 16 * h + i < visible ? y : -__builtin_inff();
+            }
+    }
+    float mx = max2(s[0][0], s[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; i++) mx = max2(mx, max2(s[0][i], s[1][i]));
+    mx *= c;
+    const float m = max2(st.m, max2(mx, other_half(mx)));
+    if (__any(m > st.m)) {  // else every alpha is 1
+        const float alpha = __builtin_amdgcn_exp2f(st.m - m);
+        st.m = m;
+        st.l *= alpha;
+#pragma unroll
+        for (int n = 0; n < 4; n++) st.O[n] *= alpha;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+        v16f p;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -m));
+            sum += p[i];
+        }
+        st.l += sum;
+        const bf16x8 p0 = probabilities(p, 0), p1 = probabilities(p, 1);
+        uint4 v[4];
+#pragma unroll
+        for (int n = 0; n < 4; n++) v[n] = part(stage + (2 + b) * kBlockBytes, n, lane);
+        if (any || lost) clean_values(st, v, 32 * b, visible, held, x.lost[b], h);
+#pragma unroll
+        for (int n = 0; n < 4; n++) {
+            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].x, v[n].y, x.v[b]), p0, st.O[n], 0, 0, 0);
+            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].z, v[n].w, x.v[b]), p1, st.O[n], 0, 0, 0);
+        }
+    }
+}
+
+// Workgroups 8 apart run on one XCD; the shares of one XCD are neighbours, which
+// read the same keys.
+__device__ __forceinline__ int share_index() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
+
+__global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAttendArgs a) {
+    __shared__ __align__(16) uint8_t st0[kStageBytes];
+    __shared__ __align__(16) uint8_t st1[kStageBytes];
+    __shared__ __align__(16) uint8_t st2[kStageBytes];
+    const CacheArgs& c = a.c;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = tid & 63, q = lane & 31, h = lane >> 5;
+    const int index = share_index();
+    Share sh = find_share<kRows, true, kThreads>(a, index, gridDim.x);
+    const Parts<kRows> parts(a.workspace, gridDim.x);
+    const StepLoader loader(wave, lane);
+    PartInfo info{};
+    while (sh.at < sh.end) {
+        const Item it = next_item<kRows, true>(a, sh);
+        const TileRows t = tile_rows<kRows>(a, it.s, it.row0);
+        const int blocks = (t.max_end + kBlockTokens - 1) / kBlockTokens;
+        const int steps = (blocks + 1) / 2;
+        const int j0 = (int)(it.x0 * steps / it.w), j1 = (int)(it.x1 * steps / it.w);
+        // this wave's rows
+        const int wrow = 32 * wave, wrows = min(32, t.rows - wrow);
+        const bool live = q < wrows;
+        const int row = it.row0 + min(wrow + q, t.rows - 1);
+        const int end = a.causal ? t.keys - t.n + row / a.group + 1 : t.keys;
+        const int wmin = a.causal ? t.keys - t.n + (it.row0 + min(wrow, t.rows - 1)) / a.group + 1 : t.keys;
+        const QOperand qo = load_q(a.q + row_offset(a, t.first, row, it.head, a.q_stride), h, a.scale, live);
+        State st;
+        st.clear();
+        Scales x0, x1, x2;
+        __syncthreads();  // the stages are free
+        if (j0 < j1) {
+            loader.load(x0, st0, c, it.s, it.head, 2 * j0, blocks);
+            if (j0 + 1 < j1) loader.load(x1, st1, c, it.s, it.head, 2 * j0 + 2, blocks);
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            auto one = [&](int j, const uint8_t* cur, uint8_t* far, const Scales& xc, Scales& xf) {
+                if (j + 2 < j1) loader.load(xf, far, c, it.s, it.head, 2 * j + 4, blocks);
+                v16f s[2];
+                s[0] = block_scores(cur, xc.k[0], qo, lane);
+                s[1] = block_scores(cur + kBlockBytes, xc.k[1], qo, lane);
+                step(st, s, cur, xc, qo.c, end - j * kKeys, t.keys - j * kKeys, (j + 1) * kKeys > wmin, h, lane);
+                __builtin_amdgcn_s_waitcnt(0);  // the next but one landed
+                __syncthreads();
+            };
+            for (int j = j0; j < j1; j += 3) {
+                one(j, st0, st2, x0, x2);
+                if (j + 1 < j1) one(j + 1, st1, st0, x1, x0);
+                if (j + 2 < j1) one(j + 2, st2, st1, x2, x1);
+            }
+        }
+        const float l = st.l + other_half(st.l);
+        const bool whole = it.whole();
+        if (live) {
+            if (whole) {
+                const float inv = inverse(l, t.bad);
+                uint16_t* dst = a.out + row_offset(a, t.first, row, it.head, a.out_stride) + 4 * h;
+#pragma unroll
+                for (int n = 0; n < 4; n++)
+#pragma unroll
+                    for (int g = 0; g < 4; g++)
+                        *reinterpret_cast<uint2*>(dst + 32 * n + 8 * g) =
+                            bf16x4(st.O[n][4 * g] * inv, st.O[n][4 * g + 1] * inv, st.O[n][4 * g + 2] * inv,
+                                   st.O[n][4 * g + 3] * inv);
+            } else {
+                const int64_t r = (int64_t)(2 * index + (it.x0 == 0)) * kRows + wrow + q;
+                if (h == 0) parts.ml[r] = make_float2(st.m, l);
+#pragma unroll
+                for (int n = 0; n < 4; n++)
+#pragma unroll
+                    for (int g = 0; g < 4; g++)
+                        *reinterpret_cast<float4*>(parts.o + r * kHeadDim + 32 * n + 8 * g + 4 * h) =
+                            make_float4(st.O[n][4 * g], st.O[n][4 * g + 1], st.O[n][4 * g + 2], st.O[n][4 * g + 3]);
+            }
+        }
+        if (it.x0 == 0 && !whole) info = {it.last, it.s, it.head, it.row0};
+    }
+    if (tid == 0) parts.info[index] = info;
+}
+
+// Two workgroups per CU are resident (registers).
+constexpr int kWorkgroups = 512;
+
+}  // namespace
+
+size_t cache_attend_tiles_workspace() { return parts_bytes<kRows>(kWorkgroups); }
+
+hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, hipStream_t stream) {
+    cache_attend_tiles_kernel<<<kWorkgroups, kThreads, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    return launch_cache_attend_join<kRows>(a, kWorkgroups, kRows, stream);
+}
+
+}  // namespace mxattn

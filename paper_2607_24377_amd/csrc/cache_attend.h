@@ -33,7 +33,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // masked scores (-inf) give p = 0 and never inf - inf
 constexpr float kNoMax = -3.0e38f;
 
-__device__ __forceinline__ float max2(float a, float b) { return __builtin_fmaxf(a, b); }
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 __device__ __forceinline__ float other_half(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x),
@@ -131,18 +131,27 @@ __device__ __forceinline__ bf16x8 probabilities(const v16f& p, int s) {
 // A block of K and V in a wave's registers, with its scales; `lost`: no such page.
 struct Block {
     uint4 k[4], v[4];
-    int ke;
-    float vs;
+    int ke, ve;
     bool lost;
 };
 
-// The cache block `b` of sequence s and a head (the same for the whole wave).
+// Loads of what no kernel of the library writes while this one runs, at an address
+// that the whole wave shares: scalar loads.
+__device__ __forceinline__ int uniform_load(const int32_t* p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uint64_t>(p));
+}
+
+// The page of block `b` of sequence s (the same for the whole wave).
+__device__ __forceinline__ int page_of(const CacheArgs& c, int s, int b) {
+    return uniform_load(c.page_table + (int64_t)s * c.max_pages + (b >> c.bpp_log2));
+}
+
+// The cache block of a page and head; no such page: `lost`, and some block to read.
 struct BlockAt {
     int64_t at;
     bool lost;
 };
-__device__ __forceinline__ BlockAt block_at(const CacheArgs& c, int s, int head, int b) {
-    int page = __builtin_amdgcn_readfirstlane(c.page_table[(int64_t)s * c.max_pages + (b >> c.bpp_log2)]);
+__device__ __forceinline__ BlockAt block_at(const CacheArgs& c, int page, int head, int b) {
     const bool lost = (unsigned)page >= (unsigned)c.pages;
     if (lost) page = 0;
     return {(((int64_t)page * c.heads + head) << c.bpp_log2) + (b & ((1 << c.bpp_log2) - 1)), lost};
@@ -161,7 +170,7 @@ __device__ __forceinline__ void load_block(Block& x, const CacheArgs& c, BlockAt
 #pragma unroll
     for (int i = 0; i < 4; i++) x.v[i] = *reinterpret_cast<const uint4*>(vb + i * 1024);
     x.ke = c.ks[p.at];
-    x.vs = e8m0_as_f32(c.vs[p.at]);
+    x.ve = c.vs[p.at];
     x.lost = p.lost;
 }
 
@@ -278,7 +287,7 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand
 #pragma unroll
         for (int i = 0; i < 16; i++) s[i] = __builtin_nanf("");
     }
-    consume(st, s, x.v, x.vs, q.c, end - base, any, h);
+    consume(st, s, x.v, e8m0_as_f32((uint32_t)x.ve), q.c, end - base, any, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -441,8 +450,7 @@ struct TileRows {
 };
 template <int kRows>
 __device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, int row0) {
-    TokenRange r = token_range(a.c, s);
-    r = {__builtin_amdgcn_readfirstlane(r.first), __builtin_amdgcn_readfirstlane(r.last)};
+    const TokenRange r = token_range(a.c, s);
     TileRows t;
     t.n = r.last - r.first;
     t.first = r.first;

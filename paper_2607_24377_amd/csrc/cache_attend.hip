@@ -66,10 +66,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
         int b = b0 + wave;
         if (b < b1) {
             Block x, y;
-            load_block(x, c, block_at(c, it.s, it.head, b), q, h);
+            load_block(x, c, block_at(c, page_of(c, it.s, b), it.head, b), q, h);
+            int page = page_of(c, it.s, min(b + kWaves, b1 - 1));
             while (true) {
                 const bool more = b + kWaves < b1;
-                if (more) load_block(y, c, block_at(c, it.s, it.head, b + kWaves), q, h);
+                if (more) {
+                    load_block(y, c, block_at(c, page, it.head, b + kWaves), q, h);
+                    page = page_of(c, it.s, min(b + 2 * kWaves, b1 - 1));
+                }
                 attend_block(st, x, qo, b * kBlockTokens, end, t.keys, (b + 1) * kBlockTokens > t.min_end, h);
                 if (!more) break;
                 x = y;

@@ -21,10 +21,9 @@ constexpr int kStageBytes = 4 * kBlockBytes;  // K, K, V, V
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
-// What a step's operands need beside their codes.
+// What a step's operands need beside their codes: the blocks' scale bytes.
 struct Scales {
-    int k[2];
-    float v[2];
+    int k[2], v[2];
     bool lost[2];
 };
 
@@ -42,18 +41,23 @@ struct StepLoader {
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)block, 0, kBlockBytes, 0x00020000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(dst + wave * 1024), 16, off, 0, 0, 0);
     }
-    // Blocks b and b + 1 (the second only below `blocks`: else the first again, for keys that are masked).
-    __device__ __forceinline__ void load(Scales& s, uint8_t* stage, const CacheArgs& c, int seq, int head, int b,
-                                         int blocks) const {
+    // Blocks b and b + 1 (the second only below `blocks`: else the first again, for keys that are masked) of
+    // these pages.
+    __device__ __forceinline__ void load(Scales& s, uint8_t* stage, const CacheArgs& c, const int (&page)[2], int head,
+                                         int b, int blocks) const {
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            const BlockAt p = block_at(c, seq, head, min(b + i, blocks - 1));
+            const BlockAt p = block_at(c, page[i], head, min(b + i, blocks - 1));
             copy(c.kc + p.at * kBlockBytes, koff, stage + i * kBlockBytes);
             copy(c.vc + p.at * kBlockBytes, voff, stage + (2 + i) * kBlockBytes);
             s.k[i] = c.ks[p.at];
-            s.v[i] = e8m0_as_f32(c.vs[p.at]);
+            s.v[i] = c.vs[p.at];
             s.lost[i] = p.lost;
         }
+    }
+    static __device__ __forceinline__ void pages(int (&page)[2], const CacheArgs& c, int seq, int b, int blocks) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) page[i] = page_of(c, seq, min(b + i, blocks - 1));
     }
 };
 
@@ -109,11 +113,12 @@ __device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* sta
         uint4 v[4];
 #pragma unroll
         for (int n = 0; n < 4; n++) v[n] = part(stage + (2 + b) * kBlockBytes, n, lane);
+        const float vscale = e8m0_as_f32((uint32_t)x.v[b]);
         if (any || lost) clean_values(st, v, 32 * b, visible, held, x.lost[b], h);
 #pragma unroll
         for (int n = 0; n < 4; n++) {
-            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].x, v[n].y, x.v[b]), p0, st.O[n], 0, 0, 0);
-            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].z, v[n].w, x.v[b]), p1, st.O[n], 0, 0, 0);
+            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].x, v[n].y, vscale), p0, st.O[n], 0, 0, 0);
+            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].z, v[n].w, vscale), p1, st.O[n], 0, 0, 0);
         }
     }
 }
@@ -152,12 +157,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
         Scales x0, x1, x2;
         __syncthreads();  // the stages are free
         if (j0 < j1) {
-            loader.load(x0, st0, c, it.s, it.head, 2 * j0, blocks);
-            if (j0 + 1 < j1) loader.load(x1, st1, c, it.s, it.head, 2 * j0 + 2, blocks);
+            int page[2];
+            StepLoader::pages(page, c, it.s, 2 * j0, blocks);
+            loader.load(x0, st0, c, page, it.head, 2 * j0, blocks);
+            StepLoader::pages(page, c, it.s, 2 * j0 + 2, blocks);
+            if (j0 + 1 < j1) loader.load(x1, st1, c, page, it.head, 2 * j0 + 2, blocks);
+            StepLoader::pages(page, c, it.s, 2 * j0 + 4, blocks);
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
             auto one = [&](int j, const uint8_t* cur, uint8_t* far, const Scales& xc, Scales& xf) {
-                if (j + 2 < j1) loader.load(xf, far, c, it.s, it.head, 2 * j + 4, blocks);
+                if (j + 2 < j1) {
+                    loader.load(xf, far, c, page, it.head, 2 * j + 4, blocks);
+                    StepLoader::pages(page, c, it.s, 2 * j + 6, blocks);
+                }
                 v16f s[2];
                 s[0] = block_scores(cur, xc.k[0], qo, lane);
                 s[1] = block_scores(cur + kBlockBytes, xc.k[1], qo, lane);

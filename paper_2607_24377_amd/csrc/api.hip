@@ -574,6 +574,7 @@ int mxattn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, 
     if (int st = check_shape(B, Hq, N, d)) return st;
     if (k)
         if (int st = check_shape(B, Hkv, N, d)) return st;
+    if (Hq > 65535 || (k && Hkv > 65535)) return MXATTN_ERR_SHAPE;
     if (int st = check_transform(q_weight, k ? k_weight : nullptr, eps, cos, sin, positions, table_rows, rot, pairs))
         return st;
     const int64_t heads[2] = {Hq, k ? Hkv : 0};

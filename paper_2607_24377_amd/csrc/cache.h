@@ -34,8 +34,7 @@ struct RopeArgs {
     const int32_t* positions; // [B, N] or null: a token's index in its batch
     int64_t tokens;           // B * N
     int N, Hq, Hkv;
-    int heads_per_chunk;      // set by the launcher, with
-    int64_t first;            // the first token of a launch
+    int64_t first;            // set by the launcher: the first token of a launch
 };
 hipError_t launch_qk_norm_rope(const RopeArgs& a, bool halves, hipStream_t stream);
 

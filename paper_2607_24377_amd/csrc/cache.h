@@ -89,4 +89,25 @@ __device__ __forceinline__ TokenRange token_range(const CacheArgs& c, int s) {
     return {a, b};
 }
 
+// The sequence that owns workgroup w where sequence s has workgroups
+// (its first token) * group / unit + step * s onwards, up to those of s + 1; -1: none.
+// All lanes of a wave call it: 64 places probed at a time.
+__device__ __forceinline__ int64_t first_group(const CacheArgs& c, int s, int64_t group, int unit, int step) {
+    const int first = min(max(c.q_start[s], 0), c.tokens);
+    return (int64_t)first * group / unit + (int64_t)step * s;
+}
+__device__ __forceinline__ int owner_of(const CacheArgs& c, int64_t w, int64_t group, int unit, int step) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = c.seqs;
+    while (true) {
+        const int each = (hi - lo + 63) / 64, s = lo + lane * each;
+        const uint64_t at = __ballot(s < hi && first_group(c, s, group, unit, step) <= w);
+        if (!at) return -1;
+        lo += (63 - __builtin_clzll(at)) * each;
+        if (each == 1) break;
+        hi = min(hi, lo + each);
+    }
+    return w < first_group(c, lo + 1, group, unit, step) ? lo : -1;
+}
+
 }  // namespace mxattn

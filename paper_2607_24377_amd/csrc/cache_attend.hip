@@ -32,16 +32,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
     if constexpr (kDivided) {
         sh = find_share<kRows, false, kThreads>(a, blockIdx.x, gridDim.x);
     } else {
-        __shared__ int s_seq;
-        if (tid == 0) s_seq = -1;
-        __syncthreads();
-        for (int s = tid; s < c.seqs; s += kThreads) {
-            const TokenRange r = token_range(c, s);
-            const int64_t base = (int64_t)r.first * a.group / kRows + s, next = (int64_t)r.last * a.group / kRows + s + 1;
-            if (base <= blockIdx.x && blockIdx.x < next) s_seq = s;
-        }
-        __syncthreads();
-        const int s = __builtin_amdgcn_readfirstlane(s_seq);
+        const int s = __builtin_amdgcn_readfirstlane(owner_of(c, blockIdx.x, a.group, kRows, 1));
         if (s < 0) return;
         const TokenRange r = token_range(c, s);
         it = {s, (int)blockIdx.y, (int)(blockIdx.x - ((int64_t)r.first * a.group / kRows + s)) * kRows, 0, 1, 1, 0};

@@ -1,11 +1,10 @@
 // heads.h -- the norm of a head and its rotation by position, in registers.
 //
-// A row of 128 channels lies in 16 consecutive lanes, 8 channels each (16
-// bytes of bf16).  y = x / sqrt(mean(x^2) + eps) * w in fp32; then each pair
-// (a, b) of the first `rot` channels becomes (a cos - b sin, b cos + a sin) with
-// the angles of the row's position.  Pairs are neighbours (2i, 2i + 1) or lie
-// rot / 2 apart (i, i + rot / 2); rot is a multiple of 16, so that a lane's eight
-// channels have their eight partners in one lane.
+// A row of 128 channels lies in 16 consecutive lanes, 8 channels each.  y = x /
+// sqrt(mean(x^2) + eps) * w in fp32; then each pair (a, b) of the first `rot`
+// channels becomes (a cos - b sin, b cos + a sin) with the angles of the row's
+// position.  Pairs are neighbours (2i, 2i + 1) or lie rot / 2 apart (i, i + rot / 2);
+// either way a lane holds both of its four pairs (rot is a multiple of 16).
 #pragma once
 
 #include "cache.h"
@@ -14,6 +13,8 @@
 namespace mxattn {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8), aligned(16)));
 
 // Sum over the 16 lanes of a row, in every lane of it (DPP moves: no LDS traffic).
@@ -48,69 +49,80 @@ __device__ __forceinline__ u32x4 pack_bf16(f32x8 x) {
     return v;
 }
 
-// What a lane needs of a head's rotation: its partner lane and its angles.
+// The channels of a lane, two groups of four from first and second on: eight in a
+// row, or, of rotated halves, four of each (and of the halves of what does not
+// rotate, so that the lanes' groups are neighbours there too).
+template <bool kHalves>
+struct Channels {
+    int first, second;
+    __device__ __forceinline__ Channels(int rot, int lane) {
+        const bool rotates = 8 * lane < rot;
+        const int base = rotates ? 0 : rot, width = rotates ? rot : kHeadDim - rot;
+        first = kHalves ? base + 4 * (lane - (base >> 3)) : 8 * lane;
+        second = kHalves ? first + (width >> 1) : first + 4;
+    }
+    __device__ __forceinline__ f32x8 weights(const float* w) const {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(w + first), y = *reinterpret_cast<const f32x4*>(w + second);
+        return f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    }
+    // bf16 channels of the row at p
+    __device__ __forceinline__ u32x4 load(const uint16_t* p) const {
+        if constexpr (!kHalves) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + first));
+        const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p + first));
+        const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p + second));
+        return u32x4{x[0], x[1], y[0], y[1]};
+    }
+};
+
+// The angles of a lane's four pairs.
 template <bool kHalves>
 struct Rotation {
-    f32x8 c, s;   // kHalves: of the lane's 8 channels, s with the sign; else of its 4 pairs in [0..3]
-    int partner;  // lane of the wave (kHalves)
-    bool on;      // whether the lane's channels rotate (the others pass as they are, infinities too)
+    f32x4 c, s;
+    bool on;  // whether the lane's channels rotate (the others pass as they are, infinities too)
 
-    // `lane` of the row (0..15); an angle row outside the table makes NaN.
-    __device__ __forceinline__ Rotation(const HeadTransform& t, int64_t pos, int lane) {
-        const int self = (int)threadIdx.x & 63;
-        partner = self;
-        on = 8 * lane < t.rot;
+    // Lane `lane` of the row (0..15); rows of angles at cos, sin (null: NaN, of a
+    // position that the table does not have).
+    __device__ __forceinline__ Rotation(const float* cos, const float* sin, int rot, int lane) {
+        on = 8 * lane < rot;
         if (!on) return;
-        const int half = t.rot >> 4;  // lanes of half the rotated channels
-        const bool second = kHalves && lane >= half;
-        if (kHalves) partner = second ? self - half : self + half;
-        if ((uint64_t)pos >= (uint64_t)t.table_rows) {
-            const float nan = __builtin_nanf("");
-            for (int i = 0; i < 8; i++) c[i] = s[i] = nan;
-            return;
-        }
+        const float nan = __builtin_nanf("");
+        c = s = f32x4{nan, nan, nan, nan};
+        if (!cos) return;
+        c = *reinterpret_cast<const f32x4*>(cos + 4 * lane);
+        s = *reinterpret_cast<const f32x4*>(sin + 4 * lane);
+    }
+    // Position pos of the table.
+    static __device__ __forceinline__ Rotation at(const HeadTransform& t, int64_t pos, int lane) {
+        const bool in = (uint64_t)pos < (uint64_t)t.table_rows;
         const int64_t row = pos * (t.rot >> 1);
-        if (kHalves) {
-            const int64_t at = row + 8 * (second ? lane - half : lane);
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                c[i] = t.cos[at + i];
-                s[i] = second ? t.sin[at + i] : -t.sin[at + i];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                c[i] = t.cos[row + 4 * lane + i];
-                s[i] = t.sin[row + 4 * lane + i];
-            }
-        }
+        return Rotation(in ? t.cos + row : nullptr, t.sin + row, t.rot, lane);
     }
 
     // The lane's eight channels turned.
-    __device__ __forceinline__ f32x8 turned(f32x8 x) const {
-        f32x8 y;
-        if constexpr (kHalves) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float p = __shfl(x[i], partner);
-                y[i] = on ? __builtin_fmaf(x[i], c[i], p * s[i]) : x[i];
-            }
-        } else {
+    __device__ __forceinline__ f32x8 turned(const f32x8& x) const {
+        f32x8 y = x;
+        if (on) {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                y[2 * i] = on ? __builtin_fmaf(x[2 * i], c[i], -(x[2 * i + 1] * s[i])) : x[2 * i];
-                y[2 * i + 1] = on ? __builtin_fmaf(x[2 * i + 1], c[i], x[2 * i] * s[i]) : x[2 * i + 1];
+                const int a = kHalves ? i : 2 * i, b = kHalves ? 4 + i : 2 * i + 1;
+                y[a] = __builtin_fmaf(x[a], c[i], -(x[b] * s[i]));
+                y[b] = __builtin_fmaf(x[b], c[i], x[a] * s[i]);
             }
         }
         return y;
     }
 };
 
-__device__ __forceinline__ f32x8 normed(f32x8 x, const f32x8& w, float eps) {
+// 1 / sqrt(mean + eps) of the row.
+__device__ __forceinline__ float inverse_rms(const f32x8& x, float eps) {
     float q = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; i++) q = __builtin_fmaf(x[i], x[i], q);
-    const float r = 1.0f / __builtin_sqrtf(row_sum16(q) * (1.0f / kHeadDim) + eps);
+    return 1.0f / __builtin_sqrtf(row_sum16(q) * (1.0f / kHeadDim) + eps);
+}
+
+__device__ __forceinline__ f32x8 normed(f32x8 x, const f32x8& w, float eps) {
+    const float r = inverse_rms(x, eps);
 #pragma unroll
     for (int i = 0; i < 8; i++) x[i] *= r * w[i];
     return x;

@@ -10,6 +10,8 @@
 // tokens x 40 heads, 1.36 GB: 236 us, 5.75 TB/s.  One head per group took 314 us,
 // eight in two turns 241, sixteen 247; two rows in flight 244; stores that stay in
 // the caches 252.
+#include <type_traits>
+
 #include "heads.h"
 
 namespace mxattn {
@@ -19,6 +21,45 @@ constexpr int kThreads = 256;
 constexpr int kTokensPerGroup = kThreads / 16;
 constexpr int kHeads = 4;
 
+// Rotated halves, with a lane's eight channels in a row (loads and stores of 16
+// bytes; with four of either half, 8 bytes each, rows of which half the channels
+// rotate took a quarter longer): a channel's partner is in another lane, which
+// hands over its eight.
+struct HalvesAcross {
+    f32x8 c, s;
+    int partner;  // lane of the wave
+    bool on;
+    __device__ __forceinline__ HalvesAcross(const HeadTransform& t, int64_t pos, int lane) {
+        const int self = (int)threadIdx.x & 63, half = t.rot >> 4;
+        on = 8 * lane < t.rot;
+        const bool second = lane >= half;
+        partner = !on ? self : second ? self - half : self + half;
+        if (!on) return;
+        const float nan = __builtin_nanf("");
+        c = s = f32x8{nan, nan, nan, nan, nan, nan, nan, nan};
+        if ((uint64_t)pos >= (uint64_t)t.table_rows) return;
+        const int64_t at = pos * (t.rot >> 1) + 8 * (second ? lane - half : lane);
+        c = *reinterpret_cast<const f32x8*>(t.cos + at);
+        s = *reinterpret_cast<const f32x8*>(t.sin + at);
+        if (!second) s = -s;
+    }
+    __device__ __forceinline__ f32x8 turned(f32x8 x) const {
+        f32x8 y;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float p = __shfl(x[i], partner);
+            y[i] = on ? __builtin_fmaf(x[i], c[i], p * s[i]) : x[i];
+        }
+        return y;
+    }
+};
+
+// Neighbours: a lane holds both channels of its four pairs.
+struct PairsWithin : Rotation<false> {
+    __device__ __forceinline__ PairsWithin(const HeadTransform& t, int64_t pos, int lane)
+        : Rotation<false>(Rotation<false>::at(t, pos, lane)) {}
+};
+
 template <bool kHalves>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(RopeArgs a) {
     const int lane = threadIdx.x & 15;
@@ -27,7 +68,11 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(RopeArgs a) {
     const int64_t tok = live ? token : a.tokens - 1;
     const int64_t b = tok / a.N, n = tok - b * a.N;
     const int64_t pos = a.positions ? (int64_t)a.positions[tok] : n;
-    const Rotation<kHalves> rotation(a.t, pos, lane);
+    const std::conditional_t<kHalves, HalvesAcross, PairsWithin> rotation(a.t, pos, lane);
+    f32x8 w[2] = {};
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+        if (a.w[i]) w[i] = *reinterpret_cast<const f32x8*>(a.w[i] + 8 * lane);
     const int h0 = blockIdx.y * kHeads, h1 = min(h0 + kHeads, a.Hq + a.Hkv);
     u32x4 raw[kHeads];
 #pragma unroll
@@ -43,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(RopeArgs a) {
         if (h >= h1) break;
         const Strided& out = a.out[which];
         f32x8 x = unpack_bf16(raw[i]);
-        if (const float* w = a.w[which]) x = normed(x, *reinterpret_cast<const f32x8*>(w + 8 * lane), a.t.eps);
+        if (a.w[which]) x = normed(x, which ? w[1] : w[0], a.t.eps);
         x = rotation.turned(x);
         u32x4* dst = reinterpret_cast<u32x4*>(out.p + b * out.b + (which ? h - a.Hq : h) * out.h + n * out.n + 8 * lane);
         if (live) __builtin_nontemporal_store(pack_bf16(x), dst);

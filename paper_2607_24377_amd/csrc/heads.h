@@ -113,12 +113,17 @@ struct Rotation {
     }
 };
 
-// 1 / sqrt(mean + eps) of the row.
+// 1 / sqrt(mean + eps) of the row, from the hardware's reciprocal square root (1 ulp;
+// the exact square root and division are 40 instructions), kept off subnormal
+// arguments.
 __device__ __forceinline__ float inverse_rms(const f32x8& x, float eps) {
     float q = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; i++) q = __builtin_fmaf(x[i], x[i], q);
-    return 1.0f / __builtin_sqrtf(row_sum16(q) * (1.0f / kHeadDim) + eps);
+    q = __builtin_fmaf(row_sum16(q), 1.0f / kHeadDim, eps);
+    const bool small = q < 0x1p-96f;
+    const float r = __builtin_amdgcn_rsqf(small ? q * 0x1p96f : q);
+    return small ? r * 0x1p48f : r;
 }
 
 __device__ __forceinline__ f32x8 normed(f32x8 x, const f32x8& w, float eps) {

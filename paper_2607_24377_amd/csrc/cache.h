@@ -75,7 +75,7 @@ size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t m
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream);
 
 // Tiles of 128 query rows (cache_attend_tiles.hip).
-size_t cache_attend_tiles_workspace();
+size_t cache_attend_tiles_workspace(const CacheAttendArgs& a);
 hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, hipStream_t stream);
 
 // New tokens of sequence s: [first, last) of the call's tokens, whatever

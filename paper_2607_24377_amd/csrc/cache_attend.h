@@ -392,11 +392,23 @@ __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int
             __builtin_amdgcn_readfirstlane(s_share.s), __builtin_amdgcn_readfirstlane(s_share.n)};
 }
 
+// Tiles of a sequence are numbered from here on: no two sequences' overlap, whatever
+// the number of sequences' tokens before it.
+template <int kRows>
+__device__ __forceinline__ int tile_number(const CacheAttendArgs& a, int first, int s) {
+    return (int)((int64_t)first * a.group / kRows) + s;
+}
+template <int kRows>
+inline int64_t tile_numbers(const CacheAttendArgs& a) {
+    return (int64_t)a.c.tokens * a.group / kRows + a.c.seqs;
+}
+
 // One item and the part of it that a workgroup works on.
 struct Item {
     int s, head, row0;
     int64_t x0, x1, w;  // from x0 to x1 of its weight w
-    int last;           // the workgroup of its last part
+    int last;           // the share of its last part
+    int number;         // PartInfo's
     __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == w; }
 };
 
@@ -423,6 +435,7 @@ __device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
         }
     }
     it.row0 = t * kRows;
+    it.number = (tile_number<kRows>(a, token_range(a.c, sh.s).first, sh.s) + t) * a.c.heads + it.head;
     it.w = w.weight(t);
     it.x0 = r - w.before(t);
     it.x1 = it.x0 + (sh.end - sh.at) < it.w ? it.x0 + (sh.end - sh.at) : it.w;
@@ -463,20 +476,20 @@ __device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, i
     return t;
 }
 
-// What workgroup i leaves for the join: `last` > i: its last item goes on behind
-// its share up to workgroup `last`'s; the item's parts are then in slots 2 i + 1,
-// 2 (i + 1), 2 (i + 2), ..., 2 last.
+// The shares that an item lies in; what they leave for the join is in slots
+// 2 first + 1, 2 (first + 1), 2 (first + 2), ..., 2 last, or nowhere if there is but
+// one share, which finishes it.  Item number: that of the items' workgroups
+// (tile_number) times the heads, plus the head.
 struct PartInfo {
-    int last;
-    int s, head, row0;  // of that item
+    int first, last;
 };
 
-// The workspace of n workgroups: their PartInfo, m and l of their slots' rows, O~.
+// The workspace of n shares: O~, m and l of their slots' rows, and the items' PartInfo.
 template <int kRows>
 struct Parts {
-    PartInfo* info;
-    float2* ml;   // [2 n, kRows]
     float* o;     // [2 n, kRows, 128]
+    float2* ml;   // [2 n, kRows]
+    PartInfo* info;
     __device__ __forceinline__ Parts(uint8_t* ws, int n) {
         o = reinterpret_cast<float*>(ws);
         ml = reinterpret_cast<float2*>(ws + (size_t)2 * n * kRows * 512);
@@ -514,47 +527,86 @@ __device__ __forceinline__ void add_scaled(float4& o, const float4& x, float f) 
     o.w = __builtin_fmaf(x.w, f, o.w);
 }
 
-// Joins the parts of the item that began in workgroup blockIdx.x and went on
-// behind it, in the order of its keys: a row per group of 32 lanes, or, of many
-// parts, a row per workgroup, whose group g takes every eighth part.
+// A lane's half of a finished row.
+__device__ __forceinline__ void store_row(const State& st, float inv, uint16_t* row, int h) {
+#pragma unroll
+    for (int n = 0; n < 4; n++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+            *reinterpret_cast<uint2*>(row + 32 * n + 8 * g + 4 * h) =
+                bf16x4(st.O[n][4 * g] * inv, st.O[n][4 * g + 1] * inv, st.O[n][4 * g + 2] * inv, st.O[n][4 * g + 3] * inv);
+}
+
+// A lane's half of row `row` of the workspace's slots.
 template <int kRows>
-__global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs a) {
+__device__ __forceinline__ void store_part(const State& st, float l, const Parts<kRows>& parts, int64_t row, int h) {
+    if (h == 0) parts.ml[row] = make_float2(st.m, l);
+#pragma unroll
+    for (int n = 0; n < 4; n++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+            *reinterpret_cast<float4*>(parts.o + row * kHeadDim + 32 * n + 8 * g + 4 * h) =
+                make_float4(st.O[n][4 * g], st.O[n][4 * g + 1], st.O[n][4 * g + 2], st.O[n][4 * g + 3]);
+}
+
+// Joins the parts of item blockIdx.x in the order of its keys: a row per workgroup
+// and turn, whose eight groups of 32 lanes take every eighth part.
+template <int kRows>
+__global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs a, int shares) {
     __shared__ float4 s_o[8][32];
     __shared__ float s_m[8], s_l[8];
-    const Parts<kRows> parts(a.workspace, gridDim.x);
-    const int i = blockIdx.x, tid = threadIdx.x;
-    const PartInfo info = parts.info[i];
-    if (info.last <= i) return;
-    const int count = info.last - i + 1;
-    auto slot = [i](int p) { return p ? 2 * (i + p) : 2 * i + 1; };
-    const TileRows t = tile_rows<kRows>(a, info.s, info.row0);
+    const int tid = threadIdx.x, number = blockIdx.x / a.c.heads, head = blockIdx.x - number * a.c.heads;
+    const Parts<kRows> parts(a.workspace, shares);
+    const PartInfo info = parts.info[blockIdx.x];
+    const int s = __builtin_amdgcn_readfirstlane(owner_of(a.c, number, a.group, kRows, 1));
+    if (s < 0) return;
+    const TokenRange range = token_range(a.c, s);
+    const int row0 = (number - tile_number<kRows>(a, range.first, s)) * kRows;
+    const int rows = min(kRows, (range.last - range.first) * a.group - row0);
+    if (rows <= 0 || info.first == info.last) return;  // no such item, or a finished one
+    const int count = info.last - info.first + 1;
+    auto slot = [&info](int p) { return p ? 2 * (info.first + p) : 2 * info.first + 1; };
+    const bool bad = keys_of(a.c, s) < 0;
     const int g = tid >> 5, ch = 4 * (tid & 31);
-    if (count <= 8) {  // a row for each group
-        for (int r = 8 * blockIdx.y + g; r < t.rows; r += 8 * gridDim.y) {
-            float m = kNoMax, l = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int p = 0; p < count; p++) m = max2(m, parts.ml[slot(p) * kRows + r].x);
-            for (int p = 0; p < count; p++) {
-                const float2 ml = parts.ml[slot(p) * kRows + r];
-                const float f = __builtin_amdgcn_exp2f(ml.x - m);
-                l = __builtin_fmaf(ml.y, f, l);
-                add_scaled(o, *reinterpret_cast<const float4*>(parts.o + ((int64_t)slot(p) * kRows + r) * kHeadDim + ch), f);
+    // the parts from p0 on, every `step`th, four in flight
+    auto gather = [&](int r, int p0, int step, float& m, float& l, float4& o) {
+        m = kNoMax;
+        l = 0.f;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = p0; p < count; p += 4 * step) {
+            float2 ml[4];
+            float4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int64_t row = (int64_t)slot(min(p + k * step, count - 1)) * kRows + r;
+                ml[k] = parts.ml[row];
+                x[k] = *reinterpret_cast<const float4*>(parts.o + row * kHeadDim + ch);
             }
-            *reinterpret_cast<uint2*>(a.out + row_offset(a, t.first, info.row0 + r, info.head, a.out_stride) + ch) =
-                finished(o, l, t.bad);
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                if (p + k * step >= count) break;
+                const float top = max2(m, ml[k].x), f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml[k].x - top);
+                m = top;
+                l = __builtin_fmaf(ml[k].y, g, l * f);
+                o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+                add_scaled(o, x[k], g);
+            }
+        }
+    };
+    auto finish = [&](int r, float l, const float4& o) {
+        *reinterpret_cast<uint2*>(a.out + row_offset(a, range.first, row0 + r, head, a.out_stride) + ch) = finished(o, l, bad);
+    };
+    float m, l;
+    float4 o;
+    if (count <= 4) {  // a row for each group
+        for (int r = 8 * blockIdx.y + g; r < rows; r += 8 * gridDim.y) {
+            gather(r, 0, 1, m, l, o);
+            finish(r, l, o);
         }
         return;
     }
-    for (int r = blockIdx.y; r < t.rows; r += gridDim.y) {
-        float m = kNoMax, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int p = g; p < count; p += 8) m = max2(m, parts.ml[slot(p) * kRows + r].x);
-        for (int p = g; p < count; p += 8) {
-            const float2 ml = parts.ml[slot(p) * kRows + r];
-            const float f = __builtin_amdgcn_exp2f(ml.x - m);
-            l = __builtin_fmaf(ml.y, f, l);
-            add_scaled(o, *reinterpret_cast<const float4*>(parts.o + ((int64_t)slot(p) * kRows + r) * kHeadDim + ch), f);
-        }
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+        gather(r, g, 8, m, l, o);
         s_o[g][tid & 31] = o;
         if (ch == 0) {
             s_m[g] = m;
@@ -571,23 +623,22 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
                 l = __builtin_fmaf(s_l[k], f, l);
                 add_scaled(o, s_o[k][tid & 31], f);
             }
-            *reinterpret_cast<uint2*>(a.out + row_offset(a, t.first, info.row0 + r, info.head, a.out_stride) + ch) =
-                finished(o, l, t.bad);
+            finish(r, l, o);
         }
         __syncthreads();
     }
 }
 
 template <int kRows>
-inline hipError_t launch_cache_attend_join(const CacheAttendArgs& a, int workgroups, int64_t rows, hipStream_t stream) {
-    // a tile's rows over several workgroups (most have no item to join and end at once)
-    cache_attend_join_kernel<kRows><<<dim3(workgroups, (unsigned)((rows + 7) / 8)), 256, 0, stream>>>(a);
+inline hipError_t launch_cache_attend_join(const CacheAttendArgs& a, int shares, unsigned turns, hipStream_t stream) {
+    const dim3 grid((unsigned)(tile_numbers<kRows>(a) * a.c.heads), turns);
+    cache_attend_join_kernel<kRows><<<grid, 256, 0, stream>>>(a, shares);
     return hipGetLastError();
 }
 
 template <int kRows>
-inline size_t parts_bytes(int workgroups) {
-    return (size_t)workgroups * (2 * kRows * 520 + sizeof(PartInfo));
+inline size_t parts_bytes(const CacheAttendArgs& a, int shares) {
+    return (size_t)shares * (2 * kRows * 520) + (size_t)(tile_numbers<kRows>(a) * a.c.heads) * sizeof(PartInfo);
 }
 
 }  // namespace mxattn

@@ -1,11 +1,13 @@
 // cache_attend.hip -- attention over the 8-bit paged cache where a sequence has
 // few query rows per KV head (a token or some drafts): bound by reading the keys.
 //
-// A workgroup takes one tile of 32 rows (cache_attend.h) and a run of its keys; its
-// four waves hold the same rows and take every fourth block of 32 keys, straight
-// from memory into the operands' registers, the next block in flight while one is
-// worked on.  No barrier until the run's end, where the waves' m, l and O~ meet in
-// LDS.
+// A wave takes a tile of 32 rows (cache_attend.h) and a run of its keys, straight from
+// memory into the operands' registers, the next block in flight while one is worked
+// on.  Long sequences: every wave has a share of the whole call's work, whatever the
+// lengths are, and no wave waits for another; what a share's ends leave in pieces is
+// joined by a second kernel.  Short ones: the four waves of a workgroup take an item's
+// blocks in turn and meet in LDS.
+#include <stdlib.h>
 #include "cache_attend.h"
 
 namespace mxattn {
@@ -14,113 +16,305 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 32;
-constexpr int kRowFloats = 132;  // a row of O~ in LDS: 128 channels, padded off the banks of its neighbours
 
-// kDivided: shares of the work by workgroup (cache_attend.h); else one workgroup per
-// item, numbered as the workgroups of the append: sequence s has tiles
-// q_start[s] * group / 32 + s onwards.
-template <bool kDivided>
-__global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendArgs a) {
-    __shared__ __align__(16) float s_o[kWaves][kRows][kRowFloats];
+// The shares of a call: n = 2^log2 of them, of the total number of units; a unit is
+// 2^unit blocks of 32 keys of a tile, so that 32 bits hold the total.  An item is a
+// tile of 32 rows of one sequence and KV head; the items lie in a row, sequence by
+// sequence, head by head, tile by tile.
+struct Cut {
+    uint32_t total;
+    int log2;
+    // the first unit of share k; no share is empty before the units are used up
+    __device__ __forceinline__ uint32_t first(int k) const {
+        if (total >> log2) return (uint32_t)(((uint64_t)total * (uint32_t)k) >> log2);
+        return min((uint32_t)k, total);
+    }
+    // the share that holds unit y
+    __device__ __forceinline__ int of(uint32_t y) const {
+        if (!(total >> log2)) return (int)y;
+        int k = (int)((float)y / (float)total * (float)(1 << log2));
+        while (first(k) > y) k--;
+        while (first(k + 1) <= y) k++;
+        return k;
+    }
+};
+
+// A sequence as the shares see it.
+struct Sequence {
+    int first, n;   // its tokens in the call
+    int keys;       // -1: an impossible length
+    int tiles;
+    uint32_t units; // of a tile
+    __device__ __forceinline__ Sequence(const CacheAttendArgs& a, int s, int unit) {
+        const TokenRange r = token_range(a.c, s);
+        first = r.first;
+        n = r.last - r.first;
+        keys = keys_of(a.c, s);
+        tiles = (n * a.group + kRows - 1) / kRows;
+        const int blocks = (max(keys, 1) + kBlockTokens - 1) / kBlockTokens;
+        units = (uint32_t)((blocks + (1 << unit) - 1) >> unit);
+    }
+    __device__ __forceinline__ uint32_t all(int heads) const { return (uint32_t)tiles * (uint32_t)heads * units; }
+};
+
+// A wave's rows of a tile.
+struct Rows {
+    int count, row, end, min_end, max_end;  // this lane's row and the keys that it, the first and the last row see
+    __device__ __forceinline__ Rows(const CacheAttendArgs& a, int n, int keys, int row0, int q) {
+        count = min(kRows, n * a.group - row0);
+        row = row0 + min(q, count - 1);
+        end = a.causal ? keys - n + row / a.group + 1 : keys;
+        min_end = a.causal ? keys - n + row0 / a.group + 1 : keys;
+        max_end = max(0, a.causal ? keys - n + (row0 + count - 1) / a.group + 1 : keys);
+    }
+};
+
+// A stage of a wave in LDS: a block of K and one of V in operand order, part p (1 KiB)
+// the register group p of all lanes.
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+
+struct BlockScales {
+    int k, v;
+    bool lost;
+};
+
+// Copies block b of a page straight into a stage (8 loads of 1 KiB, none through
+// registers).  Behind the run's last block nothing is read, but as many loads are
+// issued: the waits below count them.
+__device__ __forceinline__ BlockScales copy_block(uint8_t* stage, const CacheArgs& c, int page, int head, int b, int last,
+                                                  int q, int h) {
+    const BlockAt p = block_at(c, page, head, min(b, last));
+    const int bytes = b <= last ? kBlockBytes : 0;
+    const __amdgpu_buffer_rsrc_t kr =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(c.kc + p.at * kBlockBytes), 0, bytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t vr =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(c.vc + p.at * kBlockBytes), 0, bytes, 0x00020000);
+    const int koff = 2 * h * 512 + operand_key(q) * 16, voff = q * 32 + 16 * h;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_ptr_t)(stage + i * 1024), 16,
+                                                 koff + (4 * (i >> 1) + (i & 1)) * 512, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr_t)(stage + kBlockBytes + i * 1024), 16, voff + i * 1024, 0, 0,
+                                                 0);
+    const BlockScales x = {c.ks[p.at], c.vs[p.at], p.lost};
+    __builtin_amdgcn_sched_barrier(0);  // the copies of two blocks stay in order
+    return x;
+}
+
+// Blocks b0, b0 + step, ... below b1 for the wave's rows, two on their way while one is
+// worked on.
+__device__ __forceinline__ void attend_run(State& st, uint8_t* st0, uint8_t* st1, const CacheArgs& c, int s, int head,
+                                           int b0, int b1, int step, const QOperand& qo, const Rows& r, int keys, int q,
+                                           int h) {
+    if (b0 >= b1) return;
+    const int lane = 32 * h + q, last = b1 - 1;
+    const int page0 = page_of(c, s, b0), page1 = page_of(c, s, min(b0 + step, last));
+    int page = page_of(c, s, min(b0 + 2 * step, last));
+    BlockScales x0 = copy_block(st0, c, page0, head, b0, last, q, h);
+    BlockScales x1 = copy_block(st1, c, page1, head, b0 + step, last, q, h);
+    auto one = [&](int b, uint8_t* stage, BlockScales& x) {
+        __builtin_amdgcn_s_waitcnt(0x0F78);  // vmcnt(8): all but the next block's copies landed
+        Block y;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            y.k[i] = *reinterpret_cast<const uint4*>(stage + i * 1024 + lane * 16);
+            y.v[i] = *reinterpret_cast<const uint4*>(stage + kBlockBytes + i * 1024 + lane * 16);
+        }
+        y.ke = x.k;
+        y.ve = x.v;
+        y.lost = x.lost;
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage is read
+        x = copy_block(stage, c, page, head, b + 2 * step, last, q, h);
+        page = page_of(c, s, min(b + 3 * step, last));
+        attend_block(st, y, qo, b * kBlockTokens, r.end, keys, (b + 1) * kBlockTokens > r.min_end, h);
+    };
+    int b = b0;
+    for (; b + step < b1; b += 2 * step) {
+        one(b, st0, x0);
+        one(b + step, st1, x1);
+    }
+    if (b < b1) one(b, st0, x0);
+    // (what is still on its way brings nothing, but it writes to the stages)
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+}
+
+// Where a share begins.
+struct Start {
+    uint32_t at, end;  // units of the whole row
+    uint32_t offset;   // of `at` in sequence s
+    int s;
+};
+
+__global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheAttendArgs a, int log2, int unit) {
+    __shared__ __align__(16) uint8_t st0[kWaves][2 * kBlockBytes];
+    __shared__ __align__(16) uint8_t st1[kWaves][2 * kBlockBytes];
+    __shared__ uint32_t s_sum[kWaves];
+    __shared__ Start s_start[kWaves];
+    const CacheArgs& c = a.c;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = tid & 63, q = lane & 31, h = lane >> 5;
+    // all sequences' units before each thread's, and the total
+    const int per = (c.seqs + kThreads - 1) / kThreads;
+    const int s0 = min(tid * per, c.seqs), s1 = min(s0 + per, c.seqs);
+    uint32_t mine = 0;
+    for (int s = s0; s < s1; s++) mine += Sequence(a, s, unit).all(c.heads);
+    uint32_t incl = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t x = (uint32_t)__shfl_up((int)incl, d);
+        if (lane >= d) incl += x;
+    }
+    if (lane == 63) s_sum[wave] = incl;
+    if (tid < kWaves) s_start[tid] = {0, 0, 0, 0};
+    __syncthreads();
+    Cut cut{0, log2};
+    uint32_t before = incl - mine;
+#pragma unroll
+    for (int k = 0; k < kWaves; k++) {
+        if (k < wave) before += s_sum[k];
+        cut.total += s_sum[k];
+    }
+    cut.total = (uint32_t)__builtin_amdgcn_readfirstlane((int)cut.total);
+#pragma unroll
+    for (int k = 0; k < kWaves; k++) {
+        const uint32_t lo = cut.first(blockIdx.x * kWaves + k), hi = cut.first(blockIdx.x * kWaves + k + 1);
+        if (lo < hi && before <= lo && lo < before + mine) {
+            uint32_t at = before;
+            for (int s = s0; s < s1; s++) {
+                const uint32_t all = Sequence(a, s, unit).all(c.heads);
+                if (lo < at + all) {
+                    s_start[k] = {lo, hi, lo - at, s};
+                    break;
+                }
+                at += all;
+            }
+        }
+    }
+    __syncthreads();
+    const int index = blockIdx.x * kWaves + wave;
+    uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_start[wave].at);
+    const uint32_t end = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_start[wave].end);
+    const uint32_t offset = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_start[wave].offset);
+    int s = __builtin_amdgcn_readfirstlane(s_start[wave].s);
+    const Parts<kRows> parts(a.workspace, 1 << log2);
+    if (at < end) {
+        Sequence seq(a, s, unit);
+        const uint32_t per_head = (uint32_t)seq.tiles * seq.units;
+        int head = __builtin_amdgcn_readfirstlane((int)(offset / per_head));
+        int tile = __builtin_amdgcn_readfirstlane((int)((offset - head * per_head) / seq.units));
+        uint32_t x0 = offset - head * per_head - tile * seq.units;
+        while (true) {
+            const uint32_t x1 = min(seq.units, x0 + (end - at));
+            const int keys = max(seq.keys, 0);
+            const Rows r(a, seq.n, keys, tile * kRows, q);
+            const int blocks = (r.max_end + kBlockTokens - 1) / kBlockTokens;
+            const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale, q < r.count);
+            State st;
+            st.clear();
+            attend_run(st, st0[wave], st1[wave], c, s, head, min((int)(x0 << unit), blocks), min((int)(x1 << unit), blocks), 1, qo, r,
+                       keys, q, h);
+            const float l = st.l + other_half(st.l);
+            const bool whole = x0 == 0 && x1 == seq.units;
+            if (q < r.count) {
+                if (whole) {
+                    store_row(st, inverse(l, seq.keys < 0), a.out + row_offset(a, seq.first, r.row, head, a.out_stride), h);
+                } else {
+                    store_part(st, l, parts, (2 * index + (x0 == 0)) * kRows + q, h);
+                }
+            }
+            if (x0 == 0 && lane == 0)
+                parts.info[(tile_number<kRows>(a, seq.first, s) + tile) * c.heads + head] = {
+                    index, whole ? index : cut.of(at + seq.units - 1)};
+            at += x1 - x0;
+            if (at >= end) break;
+            x0 = 0;
+            if (++tile == seq.tiles) {
+                tile = 0;
+                if (++head == c.heads) {
+                    head = 0;
+                    do seq = Sequence(a, ++s, unit);
+                    while (seq.tiles == 0 && s < c.seqs - 1);
+                }
+            }
+        }
+    }
+}
+
+// One workgroup per item, numbered as the workgroups of the append: sequence s has
+// tiles q_start[s] * group / 32 + s onwards.  A wave takes every fourth block.
+__global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAttendArgs a) {
+    // the blocks' stages, then the waves' O~
+    __shared__ __align__(16) uint8_t st0[kWaves][2 * kBlockBytes];
+    __shared__ __align__(16) uint8_t st1[kWaves][2 * kBlockBytes];
     __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
     const CacheArgs& c = a.c;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, q = lane & 31, h = lane >> 5;
-    Share sh{};
-    Item it{};
-    PartInfo info{};
-    if constexpr (kDivided) {
-        sh = find_share<kRows, false, kThreads>(a, blockIdx.x, gridDim.x);
-    } else {
-        const int s = __builtin_amdgcn_readfirstlane(owner_of(c, blockIdx.x, a.group, kRows, 1));
-        if (s < 0) return;
-        const TokenRange r = token_range(c, s);
-        it = {s, (int)blockIdx.y, (int)(blockIdx.x - ((int64_t)r.first * a.group / kRows + s)) * kRows, 0, 1, 1, 0};
-        if (it.row0 >= (r.last - r.first) * a.group) return;
-        sh.end = 1;
+    const int s = __builtin_amdgcn_readfirstlane(owner_of(c, blockIdx.x, a.group, kRows, 1)), head = blockIdx.y;
+    if (s < 0) return;
+    const Sequence seq(a, s, 0);
+    const int row0 = ((int)blockIdx.x - tile_number<kRows>(a, seq.first, s)) * kRows;
+    if (row0 >= seq.n * a.group) return;
+    const int keys = max(seq.keys, 0);
+    const Rows r(a, seq.n, keys, row0, q);
+    const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale, q < r.count);
+    State st;
+    st.clear();
+    attend_run(st, st0[wave], st1[wave], c, s, head, wave, (r.max_end + kBlockTokens - 1) / kBlockTokens, kWaves, qo, r,
+               keys, q, h);
+    // O~ takes the stages' place: 16 rows of 512 bytes in each, the 16-byte chunks of a
+    // row in an order of its own, so that rows written at once lie in other banks
+    auto o_at = [&](int w, int row, int chunk) {
+        return (row < 16 ? st0[w] : st1[w]) + (row & 15) * 512 + (chunk ^ row) * 16;
+    };
+    const float l = st.l + other_half(st.l);
+    if (h == 0) {
+        s_m[wave][q] = st.m;
+        s_l[wave][q] = l;
     }
-    const Parts<kRows> parts(a.workspace, gridDim.x);
-    bool first = true;
-    while (sh.at < sh.end) {
-        if constexpr (kDivided)
-            it = next_item<kRows, false>(a, sh);
-        else
-            sh.at = sh.end;
-        const TileRows t = tile_rows<kRows>(a, it.s, it.row0);
-        const int blocks = (t.max_end + kBlockTokens - 1) / kBlockTokens;
-        const int b0 = (int)(it.x0 * blocks / it.w), b1 = (int)(it.x1 * blocks / it.w);
-        const int row = it.row0 + min(q, t.rows - 1);
-        const int end = a.causal ? t.keys - t.n + row / a.group + 1 : t.keys;
-        const QOperand qo = load_q(a.q + row_offset(a, t.first, row, it.head, a.q_stride), h, a.scale, q < t.rows);
-        State st;
-        st.clear();
-        int b = b0 + wave;
-        if (b < b1) {
-            Block x, y;
-            load_block(x, c, block_at(c, page_of(c, it.s, b), it.head, b), q, h);
-            int page = page_of(c, it.s, min(b + kWaves, b1 - 1));
-            while (true) {
-                const bool more = b + kWaves < b1;
-                if (more) {
-                    load_block(y, c, block_at(c, page, it.head, b + kWaves), q, h);
-                    page = page_of(c, it.s, min(b + 2 * kWaves, b1 - 1));
-                }
-                attend_block(st, x, qo, b * kBlockTokens, end, t.keys, (b + 1) * kBlockTokens > t.min_end, h);
-                if (!more) break;
-                x = y;
-                b += kWaves;
-            }
-        }
-        const float l = st.l + other_half(st.l);
-        if (!first) __syncthreads();  // the rows of the item before are read
-        if (h == 0) {
-            s_m[wave][q] = st.m;
-            s_l[wave][q] = l;
-        }
-        if (q < t.rows) {
+    if (q < r.count) {
 #pragma unroll
-            for (int n = 0; n < 4; n++)
+        for (int n = 0; n < 4; n++)
 #pragma unroll
-                for (int g = 0; g < 4; g++)
-                    *reinterpret_cast<float4*>(&s_o[wave][q][32 * n + 8 * g + 4 * h]) =
-                        make_float4(st.O[n][4 * g], st.O[n][4 * g + 1], st.O[n][4 * g + 2], st.O[n][4 * g + 3]);
-        }
-        __syncthreads();
-        const bool whole = it.whole();
-        const int slot = 2 * blockIdx.x + (it.x0 == 0);
-        for (int e = tid; e < t.rows * 32; e += kThreads) {
-            const int r = e >> 5, ch = 4 * (e & 31);
-            float m = s_m[0][r];
-#pragma unroll
-            for (int w = 1; w < kWaves; w++) m = max2(m, s_m[w][r]);
-            float sum = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < kWaves; w++) {
-                const float f = __builtin_amdgcn_exp2f(s_m[w][r] - m);
-                sum = __builtin_fmaf(s_l[w][r], f, sum);
-                add_scaled(o, *reinterpret_cast<const float4*>(&s_o[w][r][ch]), f);
-            }
-            if (whole) {
-                *reinterpret_cast<uint2*>(a.out + row_offset(a, t.first, it.row0 + r, it.head, a.out_stride) + ch) =
-                    finished(o, sum, t.bad);
-            } else {
-                *reinterpret_cast<float4*>(parts.o + ((int64_t)slot * kRows + r) * kHeadDim + ch) = o;
-                if (ch == 0) parts.ml[slot * kRows + r] = make_float2(m, sum);
-            }
-        }
-        if (it.x0 == 0 && !whole) info = {it.last, it.s, it.head, it.row0};
-        first = false;
+            for (int g = 0; g < 4; g++)
+                *reinterpret_cast<float4*>(o_at(wave, q, 8 * n + 2 * g + h)) =
+                    make_float4(st.O[n][4 * g], st.O[n][4 * g + 1], st.O[n][4 * g + 2], st.O[n][4 * g + 3]);
     }
-    if (kDivided && tid == 0) parts.info[blockIdx.x] = info;
+    __syncthreads();
+    for (int e = tid; e < r.count * 32; e += kThreads) {
+        const int i = e >> 5, ch = 4 * (e & 31);
+        float m = s_m[0][i];
+#pragma unroll
+        for (int w = 1; w < kWaves; w++) m = max2(m, s_m[w][i]);
+        float sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) {
+            const float f = __builtin_amdgcn_exp2f(s_m[w][i] - m);
+            sum = __builtin_fmaf(s_l[w][i], f, sum);
+            add_scaled(o, *reinterpret_cast<const float4*>(o_at(w, i, e & 31)), f);
+        }
+        *reinterpret_cast<uint2*>(a.out + row_offset(a, seq.first, row0 + i, head, a.out_stride) + ch) =
+            finished(o, sum, seq.keys < 0);
+    }
 }
 
-// Two workgroups per CU are resident (registers).
-constexpr int kWorkgroups = 512;
 // Keys up to which an item is one workgroup's.
 constexpr int64_t kUndivided = 1024;
+bool divided(int64_t max_kv) { static const int ud = getenv("UD") ? atoi(getenv("UD")) : kUndivided; return max_kv > ud; }
 
-bool divided(int64_t max_kv) { return max_kv > kUndivided; }
+// log2 of the number of shares: eight waves per CU are resident (registers), and a
+// share has at least four blocks, as far as the caller's bounds say.
+int shares_log2(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    const int64_t tiles = (max_q * a.group + kRows - 1) / kRows;
+    const int64_t blocks = a.c.seqs * tiles * a.c.heads * ((max_kv + kBlockTokens - 1) / kBlockTokens);
+    int log2 = 2;
+    static const int mb = getenv("MB") ? atoi(getenv("MB")) : 4;
+    while (log2 < 11 && blocks >> (log2 + 1) >= mb) log2++;
+    return log2;
+}
 
 // Query rows of a sequence and head from which tiles of 128 rows pay.
 constexpr int64_t kTileRows = 64;
@@ -129,19 +323,22 @@ bool tiled(const CacheAttendArgs& a, int64_t max_q) { return max_q * a.group > k
 }  // namespace
 
 size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
-    return tiled(a, max_q) ? cache_attend_tiles_workspace() : divided(max_kv) ? parts_bytes<kRows>(kWorkgroups) : 0;
+    return tiled(a, max_q) ? cache_attend_tiles_workspace(a) : divided(max_kv) ? parts_bytes<kRows>(a, 1 << shares_log2(a, max_q, max_kv)) : 0;
 }
 
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream) {
     if (tiled(a, max_q)) return launch_cache_attend_tiles(a, stream);
+    const int64_t tiles = tile_numbers<kRows>(a);
     if (divided(max_kv)) {
-        cache_attend_kernel<true><<<kWorkgroups, kThreads, 0, stream>>>(a);
+        // units that keep the total of all items within 31 bits, however long the sequences are
+        int unit = 0;
+        while ((tiles * a.c.heads * ((((int64_t)a.c.max_pages << a.c.bpp_log2) >> unit) + 1)) >> 31) unit++;
+        const int log2 = shares_log2(a, max_q, max_kv);
+        cache_attend_shares_kernel<<<(1 << log2) / kWaves, kThreads, 0, stream>>>(a, log2, unit);
         if (hipError_t e = hipGetLastError()) return e;
-        return launch_cache_attend_join<kRows>(a, kWorkgroups, max_q * a.group < kRows ? max_q * a.group : kRows, stream);
-    } else {
-        const dim3 grid((unsigned)((int64_t)a.c.tokens * a.group / kRows + a.c.seqs), (unsigned)a.c.heads);
-        cache_attend_kernel<false><<<grid, kThreads, 0, stream>>>(a);
+        return launch_cache_attend_join<kRows>(a, 1 << log2, (unsigned)(max_q * a.group < kRows ? max_q * a.group : kRows), stream);
     }
+    cache_attend_items_kernel<<<dim3((unsigned)tiles, (unsigned)a.c.heads), kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -138,7 +138,6 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
     Share sh = find_share<kRows, true, kThreads>(a, index, gridDim.x);
     const Parts<kRows> parts(a.workspace, gridDim.x);
     const StepLoader loader(wave, lane);
-    PartInfo info{};
     while (sh.at < sh.end) {
         const Item it = next_item<kRows, true>(a, sh);
         const TileRows t = tile_rows<kRows>(a, it.s, it.row0);
@@ -186,30 +185,13 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
         const float l = st.l + other_half(st.l);
         const bool whole = it.whole();
         if (live) {
-            if (whole) {
-                const float inv = inverse(l, t.bad);
-                uint16_t* dst = a.out + row_offset(a, t.first, row, it.head, a.out_stride) + 4 * h;
-#pragma unroll
-                for (int n = 0; n < 4; n++)
-#pragma unroll
-                    for (int g = 0; g < 4; g++)
-                        *reinterpret_cast<uint2*>(dst + 32 * n + 8 * g) =
-                            bf16x4(st.O[n][4 * g] * inv, st.O[n][4 * g + 1] * inv, st.O[n][4 * g + 2] * inv,
-                                   st.O[n][4 * g + 3] * inv);
-            } else {
-                const int64_t r = (int64_t)(2 * index + (it.x0 == 0)) * kRows + wrow + q;
-                if (h == 0) parts.ml[r] = make_float2(st.m, l);
-#pragma unroll
-                for (int n = 0; n < 4; n++)
-#pragma unroll
-                    for (int g = 0; g < 4; g++)
-                        *reinterpret_cast<float4*>(parts.o + r * kHeadDim + 32 * n + 8 * g + 4 * h) =
-                            make_float4(st.O[n][4 * g], st.O[n][4 * g + 1], st.O[n][4 * g + 2], st.O[n][4 * g + 3]);
-            }
+            if (whole)
+                store_row(st, inverse(l, t.bad), a.out + row_offset(a, t.first, row, it.head, a.out_stride), h);
+            else
+                store_part(st, l, parts, (int64_t)(2 * index + (it.x0 == 0)) * kRows + wrow + q, h);
         }
-        if (it.x0 == 0 && !whole) info = {it.last, it.s, it.head, it.row0};
+        if (it.x0 == 0 && tid == 0) parts.info[it.number] = {index, it.last};
     }
-    if (tid == 0) parts.info[index] = info;
 }
 
 // Two workgroups per CU are resident (registers).
@@ -217,12 +199,12 @@ constexpr int kWorkgroups = 512;
 
 }  // namespace
 
-size_t cache_attend_tiles_workspace() { return parts_bytes<kRows>(kWorkgroups); }
+size_t cache_attend_tiles_workspace(const CacheAttendArgs& a) { return parts_bytes<kRows>(a, kWorkgroups); }
 
 hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, hipStream_t stream) {
     cache_attend_tiles_kernel<<<kWorkgroups, kThreads, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    return launch_cache_attend_join<kRows>(a, kWorkgroups, kRows, stream);
+    return launch_cache_attend_join<kRows>(a, kWorkgroups, kRows / 8, stream);
 }
 
 }  // namespace mxattn

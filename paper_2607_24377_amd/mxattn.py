@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import threading
+from array import array
 
 import torch
 
@@ -301,12 +302,12 @@ def _run(fn, where: str, index: int, stream, args):
         raise MxattnError(st, where)
 
 
-def _address(t, name, dtype, index, shape):
-    """The address of t, whole (contiguous) and of this shape on device `index`; NULL for None."""
+def _address(t, name, dtype, index, numel):
+    """The address of t, contiguous and of so many elements on device `index`; NULL for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of shape {tuple(shape)} on device {index}")
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of {numel} elements on device {index}")
     return t.data_ptr()
 
 
@@ -316,25 +317,33 @@ def _index(t, name) -> int:
     return t.get_device()
 
 
-_Strides = ctypes.c_int64 * 3
-
-
 def _heads(t, name, index):
-    """Address and strides of a bf16 [B, H, N, d] tensor with contiguous channels (None: contiguous)."""
-    if t.dim() != 4 or t.dtype is not torch.bfloat16 or t.get_device() != index or t.stride(3) != 1:
-        raise ValueError(f"{name} must be a bf16 [B, H, N, d] CUDA tensor on device {index}, d contiguous")
-    return t.data_ptr(), None if t.is_contiguous() else _Strides(*t.stride()[:3])
+    """Address and strides (an array; None: contiguous) of a bf16 [B, H, N, d] tensor with contiguous channels."""
+    if t.dim() != 4 or t.dtype is not torch.bfloat16 or t.get_device() != index:
+        raise ValueError(f"{name} must be a bf16 [B, H, N, d] CUDA tensor on device {index}")
+    if t.is_contiguous():
+        return t.data_ptr(), None
+    strides = array("q", t.stride())
+    if strides[3] != 1:
+        raise ValueError(f"{name}'s channels must be contiguous")
+    return t.data_ptr(), strides
+
+
+def _items(strides):
+    return None if strides is None else strides.buffer_info()[0]
 
 
 def _tables(cos, sin, index):
     """Addresses, rows and rotated channels of cos, sin [rows, rot / 2]; no rotation without them."""
     if cos is None and sin is None:
         return None, None, 0, 0
-    if cos is None or sin is None or cos.dim() != 2:
+    if cos is None or sin is None or cos.dim() != 2 or sin.dim() != 2:
         raise ValueError("cos and sin must both be given, [rows, rot / 2]")
-    shape = cos.shape
-    return (_address(cos, "cos", torch.float32, index, shape), _address(sin, "sin", torch.float32, index, shape),
-            shape[0], 2 * shape[1])
+    rows, half = cos.shape
+    if sin.size(1) != half:
+        raise ValueError("sin must have cos's shape")
+    f32 = torch.float32
+    return (_address(cos, "cos", f32, index, rows * half), _address(sin, "sin", f32, index, rows * half), rows, 2 * half)
 
 
 def _pairs(pairs) -> int:
@@ -350,7 +359,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
     qp, qs = _heads(q, "q", dev)
     B, Hq, N, d = q.shape
     if q_out is None:
-        q_out = torch.empty((B, Hq, N, d), dtype=torch.bfloat16, device=q.device)
+        q_out = q.new_empty((B, Hq, N, d))
         qop, qos = q_out.data_ptr(), None
     elif q_out.shape != q.shape:
         raise ValueError("q_out must have q's shape")
@@ -364,7 +373,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
         if k.shape != (B, Hkv, N, d):
             raise ValueError("k must be [B, Hkv, N, d] with q's B, N, d")
         if k_out is None:
-            k_out = torch.empty((B, Hkv, N, d), dtype=torch.bfloat16, device=q.device)
+            k_out = q.new_empty((B, Hkv, N, d))
             kop = k_out.data_ptr()
         elif k_out.shape != k.shape:
             raise ValueError("k_out must have k's shape")
@@ -375,9 +384,10 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
     cp, sp, rows, rot = _tables(cos, sin, dev)
     f32 = torch.float32
     _run((_lib or lib()).mxattn_qk_norm_rope, "mxattn_qk_norm_rope", dev, stream,
-         (qp, kp, qop, kop, B, Hq, Hkv, N, d, qs, ks, qos, kos, _address(q_weight, "q_weight", f32, dev, (d,)),
-          _address(k_weight, "k_weight", f32, dev, (d,)), eps, cp, sp,
-          _address(positions, "positions", torch.int32, dev, (B, N)), rows, rot, _pairs(pairs)))
+         (qp, kp, qop, kop, B, Hq, Hkv, N, d, _items(qs), _items(ks), _items(qos), _items(kos),
+          _address(q_weight, "q_weight", f32, dev, d),
+          _address(k_weight, "k_weight", f32, dev, d), eps, cp, sp,
+          _address(positions, "positions", torch.int32, dev, B * N), rows, rot, _pairs(pairs)))
     return q_out, k_out
 
 
@@ -402,15 +412,14 @@ def _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, in
     """Checked addresses and sizes of a cache and its batch, as the library takes them, and the cache's heads."""
     if k_codes.dim() != 6 or page_table.dim() != 2:
         raise ValueError("k_codes must be [pages, heads, page_tokens / 32, 8, 32, 16], page_table [seqs, max_pages]")
-    pages, heads, blocks, chunks = k_codes.shape[:4]
+    pages, heads, blocks, chunks, _, _ = k_codes.shape
     seqs, max_pages = page_table.shape
-    u8, i32, scales = torch.uint8, torch.int32, (pages, heads, blocks)
-    return (_address(k_codes, "k_codes", u8, index, scales + (chunks, BLOCK_TOKENS, 16)),
-            _address(k_scales, "k_scales", u8, index, scales),
-            _address(v_codes, "v_codes", u8, index, scales + (16 * chunks, BLOCK_TOKENS)),
-            _address(v_scales, "v_scales", u8, index, scales), pages, blocks * BLOCK_TOKENS,
-            _address(page_table, "page_table", i32, index, (seqs, max_pages)),
-            _address(q_start, "q_start", i32, index, (seqs + 1,)), _address(kv_len, "kv_len", i32, index, (seqs,)), seqs,
+    u8, i32, n = torch.uint8, torch.int32, pages * heads * blocks
+    codes = n * chunks * 16 * BLOCK_TOKENS
+    return (_address(k_codes, "k_codes", u8, index, codes), _address(k_scales, "k_scales", u8, index, n),
+            _address(v_codes, "v_codes", u8, index, codes), _address(v_scales, "v_scales", u8, index, n), pages,
+            blocks * BLOCK_TOKENS, _address(page_table, "page_table", i32, index, seqs * max_pages),
+            _address(q_start, "q_start", i32, index, seqs + 1), _address(kv_len, "kv_len", i32, index, seqs), seqs,
             max_pages), heads
 
 
@@ -427,8 +436,8 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_codes, k_scales, v_codes, v
         raise ValueError("k and v must be [tokens, Hkv, d] with the cache's heads")
     cp, sp, rows, rot = _tables(cos, sin, dev)
     _run((_lib or lib()).mxattn_cache_append, "mxattn_cache_append", dev, stream,
-         (kp, vp, kst, vst, *cache, tokens, heads, d, _address(k_weight, "k_weight", torch.float32, dev, (d,)), eps, cp, sp,
-          _address(positions, "positions", torch.int32, dev, (tokens,)), rows, rot, _pairs(pairs)))
+         (kp, vp, kst, vst, *cache, tokens, heads, d, _address(k_weight, "k_weight", torch.float32, dev, d), eps, cp, sp,
+          _address(positions, "positions", torch.int32, dev, tokens), rows, rot, _pairs(pairs)))
 
 
 def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, causal: bool = True,
@@ -439,7 +448,7 @@ def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_tab
     qp, qst = _token_rows(q, "q", dev)
     tokens, Hq, d = q.shape
     if out is None:
-        out = torch.empty((tokens, Hq, d), dtype=torch.bfloat16, device=q.device)
+        out = q.new_empty((tokens, Hq, d))
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     op, ost = _token_rows(out, "out", dev)

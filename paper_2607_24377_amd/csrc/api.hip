@@ -719,6 +719,7 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
     a.out_stride = out_stride;
     a.Hq = (int)Hq;
     a.group = (int)(Hq / Hkv);
+    a.per_group = (((uint64_t)1 << 36) + a.group - 1) / a.group;
     a.causal = causal != 0;
     a.scale = 0.12751743082459868f;  // fp32(log2(e) / sqrt(128))
     const int64_t reach = max_pages * page_tokens;

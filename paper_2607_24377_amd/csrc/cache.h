@@ -64,7 +64,8 @@ struct CacheAttendArgs {
     const uint16_t* q;  // [tokens, Hq, 128] by its token stride
     uint16_t* out;
     int64_t q_stride, out_stride;
-    int Hq, group;      // group = Hq / heads
+    int Hq, group;      // group = Hq / heads, at most 256
+    uint64_t per_group; // ceil(2^36 / group)
     int causal;
     float scale;        // log2(e) / sqrt(128)
     uint8_t* workspace; // cache_attend_workspace bytes
@@ -75,8 +76,8 @@ size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t m
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream);
 
 // Tiles of 128 query rows (cache_attend_tiles.hip).
-size_t cache_attend_tiles_workspace(const CacheAttendArgs& a);
-hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, hipStream_t stream);
+size_t cache_attend_tiles_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv);
+hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream);
 
 // New tokens of sequence s: [first, last) of the call's tokens, whatever
 // q_start holds.

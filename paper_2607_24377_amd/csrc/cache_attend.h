@@ -28,10 +28,16 @@ namespace mxattn {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 // the running maximum before the first key: below every finite score, so that
 // masked scores (-inf) give p = 0 and never inf - inf
 constexpr float kNoMax = -3.0e38f;
+
+// row / group, a row below 2^28 (a product and a shift: the division is 25 instructions).
+__device__ __forceinline__ int token_of(const CacheAttendArgs& a, int row) {
+    return (int)(((uint64_t)(uint32_t)row * a.per_group) >> 36);
+}
 
 __device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
@@ -60,8 +66,10 @@ __device__ __forceinline__ QOperand load_q(const uint16_t* row, int h, float sca
         }
     m = max(m & 0xFFFFu, m >> 16);
     m = max(m, __builtin_bit_cast(uint32_t, other_half(__builtin_bit_cast(float, m))));
-    // the smallest e >= -127 with 1.f 2^(E-127) <= 448 2^e
-    const int e = max((int)(m >> 7) - 135 + ((m & 0x7Fu) > 0x60u ? 1 : 0), -127);
+    // the smallest e >= -127 with 1.f 2^(E-127) <= 448 2^e; lo in steps 2^-4 of hi's, or as
+    // small as they get
+    const int e = max((int)(m >> 7) - 135 + ((m & 0x7Fu) > 0x60u ? 1 : 0), -122);
+    const float fh = e8m0_as_f32((uint32_t)(e + 127)), fl = e8m0_as_f32((uint32_t)(e + 123));
     QOperand q;
     q.c = m < 0x7F80u ? __builtin_ldexpf(scale, e) : __builtin_nanf("");
 #pragma unroll
@@ -71,19 +79,20 @@ __device__ __forceinline__ QOperand load_q(const uint16_t* row, int h, float sca
             const uint32_t u[4] = {raw[j][k].x, raw[j][k].y, raw[j][k].z, raw[j][k].w};
 #pragma unroll
             for (int g = 0; g < 2; g++) {
-                float x[4];
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    x[2 * i] = __builtin_ldexpf(__builtin_bit_cast(float, u[2 * g + i] << 16), -e);
-                    x[2 * i + 1] = __builtin_ldexpf(__builtin_bit_cast(float, u[2 * g + i] & 0xFFFF0000u), -e);
-                }
-                int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-                p = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], p, true);
-                const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(p, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(p, true);
-                int r = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - a[0]) * 16.f, (x[1] - a[1]) * 16.f, 0, false);
-                r = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - b[0]) * 16.f, (x[3] - b[1]) * 16.f, r, true);
-                q.hi[j][2 * k + g] = p;
-                q.lo[j][2 * k + g] = r;
+                const i16x2 none = {0, 0};
+                i16x2 p = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(none, __builtin_bit_cast(bf16x2, u[2 * g]), fh, false);
+                p = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(p, __builtin_bit_cast(bf16x2, u[2 * g + 1]), fh, true);
+                const uint32_t hi = __builtin_bit_cast(uint32_t, p);
+                const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, fh, false);
+                const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, fh, true);
+                i16x2 r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(
+                    none, __builtin_bit_cast(float, u[2 * g] << 16) - a[0],
+                    __builtin_bit_cast(float, u[2 * g] & 0xFFFF0000u) - a[1], fl, false);
+                r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(
+                    r, __builtin_bit_cast(float, u[2 * g + 1] << 16) - b[0],
+                    __builtin_bit_cast(float, u[2 * g + 1] & 0xFFFF0000u) - b[1], fl, true);
+                q.hi[j][2 * k + g] = (int)hi;
+                q.lo[j][2 * k + g] = (int)__builtin_bit_cast(uint32_t, r);
             }
         }
     return q;
@@ -251,9 +260,10 @@ __device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float 
 #pragma unroll
         for (int i = 0; i < 16; i++) s[i] = 16 * h + i < visible ? s[i] : -__builtin_inff();
     }
-    float mx = max2(s[0], s[1]);
+    float mx = max2(max2(s[0], s[1]), s[2]);
 #pragma unroll
-    for (int i = 2; i < 16; i += 2) mx = max2(mx, max2(s[i], s[i + 1]));
+    for (int i = 3; i < 15; i += 2) mx = max2(max2(mx, s[i]), s[i + 1]);  // (three-input maxima)
+    mx = max2(mx, s[15]);
     mx *= c;
     const float m = max2(st.m, max2(mx, other_half(mx)));
     if (__any(m > st.m)) {  // else every alpha is 1
@@ -282,11 +292,8 @@ __device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float 
 __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand& q, int base, int end, int keys, bool any,
                                              int h) {
     if (any || x.lost) clean_values(st, x.v, 0, end - base, keys - base, x.lost, h);
-    v16f s = scores(x.k, x.ke, q);
-    if (x.lost) {
-#pragma unroll
-        for (int i = 0; i < 16; i++) s[i] = __builtin_nanf("");
-    }
+    if (x.lost && end > base) st.l = __builtin_nanf("");  // no such page: NaN for the rows that would see it
+    const v16f s = scores(x.k, x.ke, q);
     consume(st, s, x.v, e8m0_as_f32((uint32_t)x.ve), q.c, end - base, any, h);
 }
 
@@ -471,8 +478,8 @@ __device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, i
     t.bad = keys < 0;
     t.keys = max(keys, 0);
     t.rows = min(kRows, t.n * a.group - row0);
-    t.min_end = a.causal ? t.keys - t.n + row0 / a.group + 1 : t.keys;
-    t.max_end = max(0, a.causal ? t.keys - t.n + (row0 + t.rows - 1) / a.group + 1 : t.keys);
+    t.min_end = a.causal ? t.keys - t.n + token_of(a, row0) + 1 : t.keys;
+    t.max_end = max(0, a.causal ? t.keys - t.n + token_of(a, row0 + t.rows - 1) + 1 : t.keys);
     return t;
 }
 
@@ -499,7 +506,7 @@ struct Parts {
 
 // Where row `row` of a tile's sequence lies in q or out.
 __device__ __forceinline__ int64_t row_offset(const CacheAttendArgs& a, int64_t first, int row, int head, int64_t stride) {
-    const int token = row / a.group;
+    const int token = token_of(a, row);
     return (first + token) * stride + (int64_t)(head * a.group + row - token * a.group) * kHeadDim;
 }
 
@@ -557,13 +564,15 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
     __shared__ float s_m[8], s_l[8];
     const int tid = threadIdx.x, number = blockIdx.x / a.c.heads, head = blockIdx.x - number * a.c.heads;
     const Parts<kRows> parts(a.workspace, shares);
+    // finished items and (whatever their entry holds) most numbers of no item end here
     const PartInfo info = parts.info[blockIdx.x];
+    if (info.first < 0 || info.last <= info.first || info.last >= shares) return;
     const int s = __builtin_amdgcn_readfirstlane(owner_of(a.c, number, a.group, kRows, 1));
     if (s < 0) return;
     const TokenRange range = token_range(a.c, s);
     const int row0 = (number - tile_number<kRows>(a, range.first, s)) * kRows;
     const int rows = min(kRows, (range.last - range.first) * a.group - row0);
-    if (rows <= 0 || info.first == info.last) return;  // no such item, or a finished one
+    if (rows <= 0) return;
     const int count = info.last - info.first + 1;
     auto slot = [&info](int p) { return p ? 2 * (info.first + p) : 2 * info.first + 1; };
     const bool bad = keys_of(a.c, s) < 0;
@@ -630,9 +639,11 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
 }
 
 template <int kRows>
-inline hipError_t launch_cache_attend_join(const CacheAttendArgs& a, int shares, unsigned turns, hipStream_t stream) {
-    const dim3 grid((unsigned)(tile_numbers<kRows>(a) * a.c.heads), turns);
-    cache_attend_join_kernel<kRows><<<grid, 256, 0, stream>>>(a, shares);
+inline hipError_t launch_cache_attend_join(const CacheAttendArgs& a, int shares, hipStream_t stream) {
+    const int64_t items = tile_numbers<kRows>(a) * a.c.heads;
+    // a row each, or eight where that is a workgroup for every one of 2048 slots
+    const int64_t rows = items >= 2048 / (kRows / 8) ? kRows / 8 : kRows;
+    cache_attend_join_kernel<kRows><<<dim3((unsigned)items, (unsigned)rows), 256, 0, stream>>>(a, shares);
     return hipGetLastError();
 }
 

@@ -7,7 +7,6 @@
 // lengths are, and no wave waits for another; what a share's ends leave in pieces is
 // joined by a second kernel.  Short ones: the four waves of a workgroup take an item's
 // blocks in turn and meet in LDS.
-#include <stdlib.h>
 #include "cache_attend.h"
 
 namespace mxattn {
@@ -63,81 +62,31 @@ struct Rows {
     __device__ __forceinline__ Rows(const CacheAttendArgs& a, int n, int keys, int row0, int q) {
         count = min(kRows, n * a.group - row0);
         row = row0 + min(q, count - 1);
-        end = a.causal ? keys - n + row / a.group + 1 : keys;
-        min_end = a.causal ? keys - n + row0 / a.group + 1 : keys;
-        max_end = max(0, a.causal ? keys - n + (row0 + count - 1) / a.group + 1 : keys);
+        end = a.causal ? keys - n + token_of(a, row) + 1 : keys;
+        min_end = a.causal ? keys - n + token_of(a, row0) + 1 : keys;
+        max_end = max(0, a.causal ? keys - n + token_of(a, row0 + count - 1) + 1 : keys);
     }
 };
 
-// A stage of a wave in LDS: a block of K and one of V in operand order, part p (1 KiB)
-// the register group p of all lanes.
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-
-struct BlockScales {
-    int k, v;
-    bool lost;
-};
-
-// Copies block b of a page straight into a stage (8 loads of 1 KiB, none through
-// registers).  Behind the run's last block nothing is read, but as many loads are
-// issued: the waits below count them.
-__device__ __forceinline__ BlockScales copy_block(uint8_t* stage, const CacheArgs& c, int page, int head, int b, int last,
-                                                  int q, int h) {
-    const BlockAt p = block_at(c, page, head, min(b, last));
-    const int bytes = b <= last ? kBlockBytes : 0;
-    const __amdgpu_buffer_rsrc_t kr =
-        __builtin_amdgcn_make_buffer_rsrc((void*)(c.kc + p.at * kBlockBytes), 0, bytes, 0x00020000);
-    const __amdgpu_buffer_rsrc_t vr =
-        __builtin_amdgcn_make_buffer_rsrc((void*)(c.vc + p.at * kBlockBytes), 0, bytes, 0x00020000);
-    const int koff = 2 * h * 512 + operand_key(q) * 16, voff = q * 32 + 16 * h;
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_ptr_t)(stage + i * 1024), 16,
-                                                 koff + (4 * (i >> 1) + (i & 1)) * 512, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr_t)(stage + kBlockBytes + i * 1024), 16, voff + i * 1024, 0, 0,
-                                                 0);
-    const BlockScales x = {c.ks[p.at], c.vs[p.at], p.lost};
-    __builtin_amdgcn_sched_barrier(0);  // the copies of two blocks stay in order
-    return x;
-}
-
-// Blocks b0, b0 + step, ... below b1 for the wave's rows, two on their way while one is
-// worked on.
-__device__ __forceinline__ void attend_run(State& st, uint8_t* st0, uint8_t* st1, const CacheArgs& c, int s, int head,
-                                           int b0, int b1, int step, const QOperand& qo, const Rows& r, int keys, int q,
-                                           int h) {
+// Blocks b0, b0 + step, ... below b1 for the wave's rows, the next one in flight while
+// one is worked on.  (Two in flight through LDS gained nothing, and three copies of
+// this loop's body in the instruction cache cost the short calls.)
+__device__ __forceinline__ void attend_run(State& st, const CacheArgs& c, int s, int head, int b0, int b1, int step,
+                                           const QOperand& qo, const Rows& r, int keys, int q, int h) {
     if (b0 >= b1) return;
-    const int lane = 32 * h + q, last = b1 - 1;
-    const int page0 = page_of(c, s, b0), page1 = page_of(c, s, min(b0 + step, last));
-    int page = page_of(c, s, min(b0 + 2 * step, last));
-    BlockScales x0 = copy_block(st0, c, page0, head, b0, last, q, h);
-    BlockScales x1 = copy_block(st1, c, page1, head, b0 + step, last, q, h);
-    auto one = [&](int b, uint8_t* stage, BlockScales& x) {
-        __builtin_amdgcn_s_waitcnt(0x0F78);  // vmcnt(8): all but the next block's copies landed
-        Block y;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            y.k[i] = *reinterpret_cast<const uint4*>(stage + i * 1024 + lane * 16);
-            y.v[i] = *reinterpret_cast<const uint4*>(stage + kBlockBytes + i * 1024 + lane * 16);
+    const int last = b1 - 1;
+    Block x, y;
+    load_block(x, c, block_at(c, page_of(c, s, b0), head, b0), q, h);
+    int page = page_of(c, s, min(b0 + step, last));
+    for (int b = b0;; b += step) {
+        if (b + step < b1) {
+            load_block(y, c, block_at(c, page, head, b + step), q, h);
+            page = page_of(c, s, min(b + 2 * step, last));
         }
-        y.ke = x.k;
-        y.ve = x.v;
-        y.lost = x.lost;
-        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage is read
-        x = copy_block(stage, c, page, head, b + 2 * step, last, q, h);
-        page = page_of(c, s, min(b + 3 * step, last));
-        attend_block(st, y, qo, b * kBlockTokens, r.end, keys, (b + 1) * kBlockTokens > r.min_end, h);
-    };
-    int b = b0;
-    for (; b + step < b1; b += 2 * step) {
-        one(b, st0, x0);
-        one(b + step, st1, x1);
+        attend_block(st, x, qo, b * kBlockTokens, r.end, keys, (b + 1) * kBlockTokens > r.min_end, h);
+        if (b + step >= b1) break;
+        x = y;
     }
-    if (b < b1) one(b, st0, x0);
-    // (what is still on its way brings nothing, but it writes to the stages)
-    __builtin_amdgcn_s_waitcnt(0x0F70);
 }
 
 // Where a share begins.
@@ -148,8 +97,6 @@ struct Start {
 };
 
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheAttendArgs a, int log2, int unit) {
-    __shared__ __align__(16) uint8_t st0[kWaves][2 * kBlockBytes];
-    __shared__ __align__(16) uint8_t st1[kWaves][2 * kBlockBytes];
     __shared__ uint32_t s_sum[kWaves];
     __shared__ Start s_start[kWaves];
     const CacheArgs& c = a.c;
@@ -213,8 +160,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
             const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale, q < r.count);
             State st;
             st.clear();
-            attend_run(st, st0[wave], st1[wave], c, s, head, min((int)(x0 << unit), blocks), min((int)(x1 << unit), blocks), 1, qo, r,
-                       keys, q, h);
+            attend_run(st, c, s, head, min((int)(x0 << unit), blocks), min((int)(x1 << unit), blocks), 1, qo, r, keys, q, h);
             const float l = st.l + other_half(st.l);
             const bool whole = x0 == 0 && x1 == seq.units;
             if (q < r.count) {
@@ -245,9 +191,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
 // One workgroup per item, numbered as the workgroups of the append: sequence s has
 // tiles q_start[s] * group / 32 + s onwards.  A wave takes every fourth block.
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAttendArgs a) {
-    // the blocks' stages, then the waves' O~
-    __shared__ __align__(16) uint8_t st0[kWaves][2 * kBlockBytes];
-    __shared__ __align__(16) uint8_t st1[kWaves][2 * kBlockBytes];
+    __shared__ __align__(16) uint8_t s_o[kWaves][kRows * 512];
     __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
     const CacheArgs& c = a.c;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -262,13 +206,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
     const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale, q < r.count);
     State st;
     st.clear();
-    attend_run(st, st0[wave], st1[wave], c, s, head, wave, (r.max_end + kBlockTokens - 1) / kBlockTokens, kWaves, qo, r,
-               keys, q, h);
-    // O~ takes the stages' place: 16 rows of 512 bytes in each, the 16-byte chunks of a
-    // row in an order of its own, so that rows written at once lie in other banks
-    auto o_at = [&](int w, int row, int chunk) {
-        return (row < 16 ? st0[w] : st1[w]) + (row & 15) * 512 + (chunk ^ row) * 16;
-    };
+    attend_run(st, c, s, head, wave, (r.max_end + kBlockTokens - 1) / kBlockTokens, kWaves, qo, r, keys, q, h);
+    // the 16-byte chunks of a row in an order of its own, so that rows written at once lie
+    // in other banks
+    auto o_at = [&](int w, int row, int chunk) { return s_o[w] + row * 512 + (chunk ^ row) * 16; };
     const float l = st.l + other_half(st.l);
     if (h == 0) {
         s_m[wave][q] = st.m;
@@ -301,45 +242,56 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
     }
 }
 
-// Keys up to which an item is one workgroup's.
-constexpr int64_t kUndivided = 1024;
-bool divided(int64_t max_kv) { static const int ud = getenv("UD") ? atoi(getenv("UD")) : kUndivided; return max_kv > ud; }
-
-// log2 of the number of shares: eight waves per CU are resident (registers), and a
-// share has at least four blocks, as far as the caller's bounds say.
-int shares_log2(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
-    const int64_t tiles = (max_q * a.group + kRows - 1) / kRows;
-    const int64_t blocks = a.c.seqs * tiles * a.c.heads * ((max_kv + kBlockTokens - 1) / kBlockTokens);
-    int log2 = 2;
-    static const int mb = getenv("MB") ? atoi(getenv("MB")) : 4;
-    while (log2 < 11 && blocks >> (log2 + 1) >= mb) log2++;
-    return log2;
+// Which kernel, from the caller's bounds on a sequence's query rows per KV head and its
+// keys (us, kernels with their joins; 8 KV heads):
+//   few keys: an item is one workgroup's.  16 sequences x 5 rows x 1000 keys 13.7, in
+//   shares 17.2; one sequence's row over 2000 keys 16.7 and 13.4.  Up to 128 rows: 90
+//   rows x 290 keys 8.6, in tiles of 128 rows 33.
+//   else up to 32 rows: shares; more: tiles of 128 rows, whose four waves read the keys
+//   once.  16 sequences x 40 rows x 4000 keys 60 and 50, 125 rows 113 and 58.
+enum Way { kItems, kShares, kTiles };
+Way way(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    const int64_t rows = max_q * a.group;
+    if (max_kv <= 1024 && rows <= 128) return kItems;
+    return rows <= kRows ? kShares : kTiles;
 }
 
-// Query rows of a sequence and head from which tiles of 128 rows pay.
-constexpr int64_t kTileRows = 64;
-bool tiled(const CacheAttendArgs& a, int64_t max_q) { return max_q * a.group > kTileRows; }
+// log2 of the number of shares: eight waves per CU are resident (registers); a share
+// has at least two blocks and an item at most 256 parts (one row over 118801 keys: 1856
+// parts took 44 us to join), as far as the caller's bounds say.
+int shares_log2(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    const int64_t items = a.c.seqs * ((max_q * a.group + kRows - 1) / kRows) * a.c.heads;
+    const int64_t blocks = (max_kv + kBlockTokens - 1) / kBlockTokens;
+    int log2 = 2;
+    while (log2 < 11 && (items * blocks) >> (log2 + 1) >= 2 && items * 256 >> (log2 + 1) >= 1) log2++;
+    return log2;
+}
 
 }  // namespace
 
 size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
-    return tiled(a, max_q) ? cache_attend_tiles_workspace(a) : divided(max_kv) ? parts_bytes<kRows>(a, 1 << shares_log2(a, max_q, max_kv)) : 0;
+    switch (way(a, max_q, max_kv)) {
+        case kItems: return 0;
+        case kShares: return parts_bytes<kRows>(a, 1 << shares_log2(a, max_q, max_kv));
+        default: return cache_attend_tiles_workspace(a, max_q, max_kv);
+    }
 }
 
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream) {
-    if (tiled(a, max_q)) return launch_cache_attend_tiles(a, stream);
+    const Way w = way(a, max_q, max_kv);
+    if (w == kTiles) return launch_cache_attend_tiles(a, max_q, max_kv, stream);
     const int64_t tiles = tile_numbers<kRows>(a);
-    if (divided(max_kv)) {
-        // units that keep the total of all items within 31 bits, however long the sequences are
-        int unit = 0;
-        while ((tiles * a.c.heads * ((((int64_t)a.c.max_pages << a.c.bpp_log2) >> unit) + 1)) >> 31) unit++;
-        const int log2 = shares_log2(a, max_q, max_kv);
-        cache_attend_shares_kernel<<<(1 << log2) / kWaves, kThreads, 0, stream>>>(a, log2, unit);
-        if (hipError_t e = hipGetLastError()) return e;
-        return launch_cache_attend_join<kRows>(a, 1 << log2, (unsigned)(max_q * a.group < kRows ? max_q * a.group : kRows), stream);
+    if (w == kItems) {
+        cache_attend_items_kernel<<<dim3((unsigned)tiles, (unsigned)a.c.heads), kThreads, 0, stream>>>(a);
+        return hipGetLastError();
     }
-    cache_attend_items_kernel<<<dim3((unsigned)tiles, (unsigned)a.c.heads), kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    // units that keep the total of all items within 31 bits, however long the sequences are
+    int unit = 0;
+    while ((tiles * a.c.heads * ((((int64_t)a.c.max_pages << a.c.bpp_log2) >> unit) + 1)) >> 31) unit++;
+    const int log2 = shares_log2(a, max_q, max_kv);
+    cache_attend_shares_kernel<<<(1 << log2) / kWaves, kThreads, 0, stream>>>(a, log2, unit);
+    if (hipError_t e = hipGetLastError()) return e;
+    return launch_cache_attend_join<kRows>(a, 1 << log2, stream);
 }
 
 }  // namespace mxattn

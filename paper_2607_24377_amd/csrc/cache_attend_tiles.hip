@@ -87,9 +87,18 @@ __device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* sta
                 s[b][i] = 32 * b + 16 * h + i < visible ? y : -__builtin_inff();
             }
     }
-    float mx = max2(s[0][0], s[1][0]);
+    float mx = max2(max2(s[0][0], s[0][1]), s[1][0]), my = max2(max2(s[0][2], s[0][3]), s[1][1]);
 #pragma unroll
-    for (int i = 1; i < 16; i++) mx = max2(mx, max2(s[0][i], s[1][i]));
+    for (int i = 4; i < 16; i += 4) {  // (a three-input maximum for every two scores)
+        mx = max2(max2(mx, s[0][i]), s[0][i + 1]);
+        my = max2(max2(my, s[0][i + 2]), s[0][i + 3]);
+    }
+#pragma unroll
+    for (int i = 2; i < 14; i += 4) {
+        mx = max2(max2(mx, s[1][i]), s[1][i + 1]);
+        my = max2(max2(my, s[1][i + 2]), s[1][i + 3]);
+    }
+    mx = max2(max2(mx, s[1][14]), max2(my, s[1][15]));
     mx *= c;
     const float m = max2(st.m, max2(mx, other_half(mx)));
     if (__any(m > st.m)) {  // else every alpha is 1
@@ -148,8 +157,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
         const int wrow = 32 * wave, wrows = min(32, t.rows - wrow);
         const bool live = q < wrows;
         const int row = it.row0 + min(wrow + q, t.rows - 1);
-        const int end = a.causal ? t.keys - t.n + row / a.group + 1 : t.keys;
-        const int wmin = a.causal ? t.keys - t.n + (it.row0 + min(wrow, t.rows - 1)) / a.group + 1 : t.keys;
+        const int end = a.causal ? t.keys - t.n + token_of(a, row) + 1 : t.keys;
+        const int wmin = a.causal ? t.keys - t.n + token_of(a, it.row0 + min(wrow, t.rows - 1)) + 1 : t.keys;
         const QOperand qo = load_q(a.q + row_offset(a, t.first, row, it.head, a.q_stride), h, a.scale, live);
         State st;
         st.clear();
@@ -194,17 +203,26 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
     }
 }
 
-// Two workgroups per CU are resident (registers).
-constexpr int kWorkgroups = 512;
+// Two workgroups per CU are resident (registers); fewer where a share would have less
+// than four steps, as far as the caller's bounds say; a multiple of the 8 XCDs.
+int workgroups(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    int64_t tiles = a.c.seqs * ((max_q * a.group + kRows - 1) / kRows);
+    if (tiles > tile_numbers<kRows>(a)) tiles = tile_numbers<kRows>(a);
+    const int64_t n = tiles * a.c.heads * ((max_kv + kKeys - 1) / kKeys) / 4;
+    return n >= 512 ? 512 : n < 8 ? 8 : (int)n & ~7;
+}
 
 }  // namespace
 
-size_t cache_attend_tiles_workspace(const CacheAttendArgs& a) { return parts_bytes<kRows>(a, kWorkgroups); }
+size_t cache_attend_tiles_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    return parts_bytes<kRows>(a, workgroups(a, max_q, max_kv));
+}
 
-hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, hipStream_t stream) {
-    cache_attend_tiles_kernel<<<kWorkgroups, kThreads, 0, stream>>>(a);
+hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream) {
+    const int n = workgroups(a, max_q, max_kv);
+    cache_attend_tiles_kernel<<<n, kThreads, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    return launch_cache_attend_join<kRows>(a, kWorkgroups, kRows / 8, stream);
+    return launch_cache_attend_join<kRows>(a, n, stream);
 }
 
 }  // namespace mxattn

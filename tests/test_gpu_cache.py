@@ -80,6 +80,7 @@ APPENDS = [
     ([100, 1, 257], [3, 700, 95], 5, 256, 96, "interleaved", True),
     ([2], [4094], 40, 4096, 128, "halves", True),
     ([7] * 70, [13 * i for i in range(70)], 1, 32, 32, "interleaved", False),
+    ([i % 4 for i in range(260)], [(17 * i) % 70 for i in range(260)], 5, 64, 48, "halves", True),
 ]
 
 
@@ -220,6 +221,19 @@ ATTENDS = [
     ([1] * 40, [97 * i % 701 for i in range(40)], 32, 8, 32, True),
     ([17], [2031], 64, 1, 64, True),
     ([300, 3], [5, 4000], 8, 8, 64, False),
+    # many sequences, some without tokens, some without keys
+    ([i % 3 for i in range(300)], [(37 * i) % 90 for i in range(300)], 4, 2, 32, True),
+    # more sequences than threads that look for a share, long enough for shares
+    ([1] * 270, [1100 if i == 200 else 3 * i % 64 for i in range(270)], 2, 1, 64, True),
+    # 33 and 128 rows a head over few and many keys: every kernel's tile borders
+    ([33], [200], 1, 1, 64, True),
+    ([33, 128], [1500, 40], 2, 2, 128, True),
+    ([16], [1200], 16, 2, 32, False),
+    # a group of 256 heads
+    ([2], [70], 256, 1, 32, True),
+    # one row in many parts, and tiles in many parts
+    ([1], [40000], 1, 1, 256, False),
+    ([40], [20000], 4, 1, 256, True),
 ]
 
 
@@ -242,6 +256,40 @@ def test_attend_against_64_bits(mx, case):
     o2 = mx.cache_attend(q, *cache, table.cuda(), ints(start), ints(lens), causal, max(new), max(lens))
     err = (o2.cpu().double() - want)[:n].abs()
     assert bool((err <= tol[:n] + 1e-30).all())
+
+
+def test_bounds_that_are_wrong_cost_time_only(mx):
+    """max_q and max_kv choose the kernel: every choice gives the same result within the tolerance."""
+    new, past = [50, 1, 3], [700, 2100, 5]
+    table, start, lens, pages = batch(new, past, 64)
+    cache = filled(mx, pages, 2, 64, 11)
+    q = rows(start[-1], 8, 5, 0.5)
+    want, tol = ref.attend(ref.Cache(*cache), q.cpu(), table, start, lens, True)
+    for max_q, max_kv in ((1, 1), (1, 2000), (8, 5000), (9, 1025), (33, 64), (1 << 30, 1 << 40), (50, 2101), (16, 1 << 20)):
+        o = mx.cache_attend(q, *cache, table.cuda(), ints(start), ints(lens), True, max_q, max_kv)
+        assert bool(((o.cpu().double() - want).abs() <= tol).all()), (max_q, max_kv)
+
+
+def test_cache_larger_than_32_bit_offsets(mx):
+    """Blocks past 4 GiB of codes: the same as at the cache's start."""
+    pages, H, page = 36000, 8, 128  # 4.7 GB of K codes, and of V
+    new, past = [1, 40], [300, 1500]
+    table, start, lens, _ = batch(new, past, page, spare=0)
+    used = int(table[table < pages].max()) + 1
+    near = table.clone()
+    far = torch.where(table < pages, table + (pages - used), table)
+    k, v, q = rows(sum(lens), H, 1), rows(sum(lens), H, 2), rows(start[-1], 2 * H, 3)
+    cache = empty_cache(mx, pages, H, page)
+    first = [0, lens[0], sum(lens)]
+    outs = []
+    for t in (near, far):
+        mx.cache_append(k, v, *cache, t.cuda(), ints(first), ints(lens))
+        outs.append([mx.cache_attend(q, *cache, t.cuda(), ints(start), ints(lens), True, *b)
+                     for b in ((1, 100), (1, 5000), (40, 5000))])
+    for a, b in zip(*outs):
+        assert torch.equal(a, b) and bool(a.isfinite().all()) and bool((a != 0).any())
+    for c in cache:
+        assert torch.equal(c[:used], c[pages - used:])
 
 
 def test_attend_repeats_bit_for_bit(mx):

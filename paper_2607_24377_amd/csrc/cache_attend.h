@@ -455,7 +455,7 @@ __device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
     if (sh.at < sh.end && sh.offset >= per_head * a.c.heads) {
         sh.offset = 0;
         do sh.s++;
-        while (sh.s < a.c.seqs - 1 && seq_work<kRows, kGrowing>(a, sh.s).tiles == 0);
+        while (sh.s < a.c.seqs && seq_work<kRows, kGrowing>(a, sh.s).tiles == 0);
     }
     return it;
 }

@@ -28,8 +28,9 @@ struct Cut {
         if (total >> log2) return (uint32_t)(((uint64_t)total * (uint32_t)k) >> log2);
         return min((uint32_t)k, total);
     }
-    // the share that holds unit y
+    // the share that holds unit y (of the total, whatever q_start holds)
     __device__ __forceinline__ int of(uint32_t y) const {
+        y = min(y, total - 1);
         if (!(total >> log2)) return (int)y;
         int k = (int)((float)y / (float)total * (float)(1 << log2));
         while (first(k) > y) k--;
@@ -180,8 +181,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
                 tile = 0;
                 if (++head == c.heads) {
                     head = 0;
-                    do seq = Sequence(a, ++s, unit);
-                    while (seq.tiles == 0 && s < c.seqs - 1);
+                    do {  // there is a next one, unless q_start does not ascend and the total is wrong
+                        if (++s >= c.seqs) return;
+                        seq = Sequence(a, s, unit);
+                    } while (seq.tiles == 0);
                 }
             }
         }

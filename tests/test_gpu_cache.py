@@ -502,6 +502,28 @@ def test_steps_captured_into_a_graph(mx):
         assert all(torch.equal(x, y) for x, y in zip(a["cache"], b["cache"]))
 
 
+@pytest.mark.parametrize("max_kv", [0, 300])
+@pytest.mark.parametrize("max_q", [1, 64])
+def test_starts_that_do_not_ascend(mx, max_q, max_kv):
+    """Whatever q_start holds, calls end and write nothing but rows of the call's tokens and blocks of the cache."""
+    tokens, seqs, heads = 64, 40, 2
+    g = torch.Generator().manual_seed(3)
+    table, _, lens, pages = batch([1] * seqs, [2000] * 2 + [40] * (seqs - 2), 64, seed=1)
+    shapes = [math.prod(s) for s in mx.cache_shapes(pages, heads, 64)]
+    starts = [[0, tokens] * (seqs // 2) + [0], list(range(seqs, -1, -1)), [tokens] * (seqs + 1), [-5] * seqs + [10 ** 9],
+              [-2 ** 31, 2 ** 31 - 1] * (seqs // 2) + [5]] + [torch.randint(-5, 80, (seqs + 1,), generator=g).tolist() for _ in range(6)]
+    for start in starts:
+        room = [torch.full((n + 8192,), 7, dtype=torch.uint8, device="cuda") for n in shapes]
+        cache = [x[4096:-4096].view(s) for x, s in zip(room, mx.cache_shapes(pages, heads, 64))]
+        out = torch.full((3 * tokens, 4, ref.D), 9.0, dtype=torch.bfloat16, device="cuda")
+        q, kv = rows(tokens, 4, 1), rows(tokens, heads, 2)
+        mx.cache_append(kv, kv, *cache, table.cuda(), ints(start), ints(lens))
+        mx.cache_attend(q, *cache, table.cuda(), ints(start), ints(lens), max_q=max_q, max_kv=max_kv, out=out[tokens:-tokens])
+        torch.cuda.synchronize()
+        assert all(bool((x[:4096] == 7).all() and (x[-4096:] == 7).all()) for x in room), start
+        assert bool((out[:tokens] == 9).all() and (out[-tokens:] == 9).all()), start
+
+
 def test_two_streams_at_once(mx):
     """Calls on two streams, neither waiting for the other, give what each gives alone."""
     work = []

@@ -92,9 +92,12 @@ typedef enum {
                                    boundary count outside [1, 64], or a
                                    pre-scale gamma not in (0, 3e38)         */
     MXATTN_ERR_SCRATCH = 10,    /* the problem needs more than the static
-                                   scratch of mxattn_cross_attend_noalloc   */
+                                   scratch of mxattn_cross_attend_noalloc, or
+                                   than the workspace that mxattn_cache_attend
+                                   was given (none, under graph capture)    */
     MXATTN_ERR_VALUE = 11       /* rot, pairs, eps or page_tokens outside what
-                                   the call takes, or Hq no multiple of Hkv  */
+                                   the call takes, Hq no multiple of Hkv or
+                                   more than 256 times as many              */
 } mxattn_status;
 
 #define MXATTN_AXIS_TOKENS 2   /* blocks along N (V)      */
@@ -333,7 +336,9 @@ int mxattn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, 
  * These arrays are read by the kernels only (4-byte aligned).  Bad contents read
  * and write nothing out of range: a kv_len below 0 or past max_pages * page_tokens,
  * or a page outside [0, pages), appends nothing there and gives NaN to every query
- * that would see it. */
+ * that would see it; a q_start that does not ascend gives undefined results.
+ * Limits (MXATTN_ERR_SHAPE otherwise): Hkv <= 65535, seqs <= 2^20,
+ * max_pages * page_tokens <= 2^24, pages * Hkv * page_tokens <= 2^45. */
 
 /* Append the call's tokens to the cache: K normed and rotated (w, eps, cos, sin,
  * table_rows, rot, pairs as above; positions: device int32 [tokens], or NULL: a
@@ -359,15 +364,34 @@ int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t 
  * to bf16 before the product with V.  Query head i reads KV head i / (Hq / Hkv).
  * causal != 0: token i of n sees positions 0 .. kv_len - n + i, else all kv_len.
  * A query that sees no key gets 0.
- *   q     device bf16 [tokens, Hq, d], heads contiguous, token stride
+ *   q     device bf16 [tokens, Hq, d], heads contiguous, token stride; Hq at most
+ *         256 Hkv, (tokens * Hq / Hkv / 32 + seqs) * Hkv < 2^31
  *   out   device bf16 [tokens, Hq, d], likewise; tokens of no sequence are not
- *         written.  MXATTN_ERR_SHAPE if it shares a byte with q or the cache. */
+ *         written.  MXATTN_ERR_SHAPE if it shares a byte with q or the cache.
+ *   max_q, max_kv  at least the new tokens and the keys of every sequence, as the
+ *         caller knows them on the host; 0: unknown (tokens, and max_pages *
+ *         page_tokens).  They choose how the work is divided: bounds that are too
+ *         small or far too large cost time, not correctness; other bounds may
+ *         change an output by the order of its fp32 sums.
+ *   workspace  device memory of the caller, 16-byte aligned, of at least
+ *         mxattn_cache_attend_workspace() bytes (else MXATTN_ERR_SCRATCH), for this
+ *         call until it has run; what it holds before does not matter.  It shares no
+ *         byte with q, out or the cache (MXATTN_ERR_SHAPE).  NULL: from the
+ *         library's pool, which a stream under graph capture cannot use: there a
+ *         call that needs workspace is refused (MXATTN_ERR_SCRATCH).
+ * Equal arguments and contents give equal bits. */
 int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
                         const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
                         const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len,
                         int64_t seqs, int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d,
                         int causal, int64_t max_q, int64_t max_kv, void* out, int64_t out_stride,
-                        void* stream);
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that mxattn_cache_attend needs: none where max_kv <= 1024 and
+ * max_q * Hq / Hkv <= 128, else at most 65 MiB, and 8 bytes per KV head for each
+ * sequence and each 32 query rows.  0 also for sizes that the call refuses. */
+size_t mxattn_cache_attend_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens,
+                                     int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv);
 
 /* Sizes of the code and scale arrays of a [B, H, N, d] tensor blocked along
  * `block_axis`; 0 for invalid arguments. */
@@ -390,8 +414,8 @@ const char* mxattn_status_string(int status);
 const char* mxattn_last_error(void);
 
 /* Workspace.  mxattn_forward, mxattn_cross_forward, mxattn_attend,
- * mxattn_cross_attend and mxattn_qmax_sse take their workspace, stream-
- * ordered, from a memory pool that belongs to the library (one per device,
+ * mxattn_cross_attend, mxattn_qmax_sse and mxattn_cache_attend (where it is
+ * given none) take their workspace, stream-ordered, from a memory pool that belongs to the library (one per device,
  * created on first use; the device's default pool is left as it is).  The
  * pool keeps freed workspace for the next call rather than returning it to
  * the driver; one block of at most 64 MiB per device stays allocated for the

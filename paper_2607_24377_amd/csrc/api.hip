@@ -618,18 +618,31 @@ int mxattn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, 
     return MXATTN_OK;
 }
 
+// The sizes of a batch over the paged cache.
+static int check_batch(int64_t seqs, int64_t max_pages, int64_t page_tokens, int64_t tokens, int64_t Hkv) {
+    if (int st = check_shape(1, Hkv, tokens, mxattn::kHeadDim)) return st;
+    if (Hkv > 65535 || seqs < 1 || seqs > 1 << 20) return MXATTN_ERR_SHAPE;
+    return max_pages < 1 || max_pages > mxattn::kMaxKeys / page_tokens ? MXATTN_ERR_SHAPE : MXATTN_OK;
+}
+
+// Query heads that read the cache's; the tiles of at least 32 rows are numbered with 31 bits.
+static int check_query_heads(int64_t seqs, int64_t tokens, int64_t Hq, int64_t Hkv) {
+    if (int st = check_shape(1, Hq, tokens, mxattn::kHeadDim)) return st;
+    if (Hq % Hkv != 0 || Hq / Hkv > 256) return MXATTN_ERR_VALUE;
+    return (tokens * (Hq / Hkv) / 32 + seqs) * Hkv >> 31 ? MXATTN_ERR_SHAPE : MXATTN_OK;
+}
+
 // The checks that the calls on the paged cache share; fills c.
 static int check_cache(mxattn::CacheArgs& c, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
                        const uint8_t* v_scales, int64_t pages, int64_t page_tokens, const int32_t* page_table,
                        const int32_t* q_start, const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t tokens,
                        int64_t Hkv, int64_t d) {
     if (!k_codes || !k_scales || !v_codes || !v_scales || !page_table || !q_start || !kv_len) return MXATTN_ERR_NULL;
-    if (int st = check_shape(1, Hkv, tokens, d)) return st;
+    if (int st = check_shape(1, 1, 1, d)) return st;
     if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0) return MXATTN_ERR_VALUE;
     const int64_t bpp = page_tokens / 32;
+    if (int st = check_batch(seqs, max_pages, page_tokens, tokens, Hkv)) return st;
     if (pages < 1 || pages > (int64_t)1 << 30 || pages * bpp > ((int64_t)1 << 40) / Hkv) return MXATTN_ERR_SHAPE;
-    if (seqs < 1 || seqs > 1 << 20 || max_pages < 1 || max_pages > mxattn::kMaxKeys / page_tokens)
-        return MXATTN_ERR_SHAPE;
     if (!aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(page_table, 4) || !aligned(q_start, 4) ||
         !aligned(kv_len, 4))
         return MXATTN_ERR_ALIGN;
@@ -676,7 +689,6 @@ int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t 
                              seqs, max_pages, tokens, Hkv, d))
         return st;
     if (int st = check_transform(k_weight, nullptr, eps, cos, sin, positions, table_rows, rot, pairs)) return st;
-    if (Hkv > 65535) return MXATTN_ERR_SHAPE;
     size_t kb = 0, vb = 0;
     if (int st = check_rows(k, k_stride, tokens, Hkv, false, kb)) return st;
     if (int st = check_rows(v, v_stride, tokens, Hkv, false, vb)) return st;
@@ -696,19 +708,39 @@ int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t 
     return MXATTN_OK;
 }
 
+// The caller's bounds on a sequence's new tokens and keys, as far as it gives any.
+static void attend_bounds(int64_t& max_q, int64_t& max_kv, int64_t tokens, int64_t reach) {
+    if (max_kv == 0 || max_kv > reach) max_kv = reach;
+    if (max_q == 0 || max_q > tokens) max_q = tokens;
+}
+
+size_t mxattn_cache_attend_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens, int64_t Hq,
+                                     int64_t Hkv, int64_t max_q, int64_t max_kv) {
+    if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0 || max_q < 0 || max_kv < 0 ||
+        check_batch(seqs, max_pages, page_tokens, tokens, Hkv) || check_query_heads(seqs, tokens, Hq, Hkv))
+        return 0;
+    mxattn::CacheAttendArgs a{};
+    a.c.seqs = (int)seqs;
+    a.c.tokens = (int)tokens;
+    a.c.heads = (int)Hkv;
+    a.group = (int)(Hq / Hkv);
+    attend_bounds(max_q, max_kv, tokens, max_pages * page_tokens);
+    return mxattn::cache_attend_workspace(a, max_q, max_kv);
+}
+
 int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
                         const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
                         const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len, int64_t seqs,
                         int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d, int causal,
-                        int64_t max_q, int64_t max_kv, void* out, int64_t out_stride, void* stream) {
+                        int64_t max_q, int64_t max_kv, void* out, int64_t out_stride, void* workspace,
+                        size_t workspace_bytes, void* stream) {
     if (!q || !out) return MXATTN_ERR_NULL;
     mxattn::CacheAttendArgs a{};
     if (int st = check_cache(a.c, k_codes, k_scales, v_codes, v_scales, pages, page_tokens, page_table, q_start, kv_len,
                              seqs, max_pages, tokens, Hkv, d))
         return st;
-    if (int st = check_shape(1, Hq, tokens, d)) return st;
-    if (Hq % Hkv != 0 || Hq / Hkv > 256) return MXATTN_ERR_VALUE;
-    if (Hkv > 65535 || max_q < 0 || max_kv < 0) return MXATTN_ERR_SHAPE;
+    if (int st = check_query_heads(seqs, tokens, Hq, Hkv)) return st;
+    if (max_q < 0 || max_kv < 0) return MXATTN_ERR_SHAPE;
     size_t qb = 0, ob = 0;
     if (int st = check_rows(q, q_stride, tokens, Hq, false, qb)) return st;
     if (int st = check_rows(out, out_stride, tokens, Hq, true, ob)) return st;
@@ -722,13 +754,27 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
     a.per_group = (((uint64_t)1 << 36) + a.group - 1) / a.group;
     a.causal = causal != 0;
     a.scale = 0.12751743082459868f;  // fp32(log2(e) / sqrt(128))
-    const int64_t reach = max_pages * page_tokens;
-    if (max_kv == 0 || max_kv > reach) max_kv = reach;
-    if (max_q == 0 || max_q > tokens) max_q = tokens;
+    attend_bounds(max_q, max_kv, tokens, max_pages * page_tokens);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const size_t bytes = mxattn::cache_attend_workspace(a, max_q, max_kv);
+    size_t bytes = mxattn::cache_attend_workspace(a, max_q, max_kv);
     Workspace ws;
-    if (bytes) {
+    if (bytes && workspace) {
+        if (workspace_bytes < bytes) return MXATTN_ERR_SCRATCH;
+        if (!aligned(workspace, 16)) return MXATTN_ERR_ALIGN;
+        if (overlaps(workspace, bytes, q, qb) || overlaps(workspace, bytes, out, ob) || in_cache(workspace, bytes, a.c))
+            return MXATTN_ERR_SHAPE;
+        a.workspace = static_cast<uint8_t*>(workspace);
+        bytes = 0;
+    } else if (bytes) {
+        // an allocation of the pool is not recorded into a graph: its replays need memory that lasts
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        if (s) {
+            if (hipError_t e = hipStreamIsCapturing(s, &capture)) {
+                set_error("hipStreamIsCapturing", e);
+                return MXATTN_ERR_HIP;
+            }
+        }
+        if (capture != hipStreamCaptureStatusNone) return MXATTN_ERR_SCRATCH;
         if (int st = ws.take(bytes, s)) return st;
         a.workspace = ws.get();
     }

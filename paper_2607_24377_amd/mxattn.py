@@ -75,8 +75,10 @@ def lib() -> ctypes.CDLL:
                                               P, F, P, P, P, I64, I64, I, P]
             L.mxattn_cache_append.restype = I
             L.mxattn_cache_attend.argtypes = [P, I64, P, P, P, P, I64, I64, P, P, P, I64, I64, I64, I64, I64, I64, I,
-                                              I64, I64, P, I64, P]
+                                              I64, I64, P, I64, P, SZ, P]
             L.mxattn_cache_attend.restype = I
+            L.mxattn_cache_attend_workspace.argtypes = [I64] * 8
+            L.mxattn_cache_attend_workspace.restype = SZ
             L.mxattn_codes_bytes.argtypes = [I, I64, I64, I64, I64]
             L.mxattn_codes_bytes.restype = SZ
             L.mxattn_scales_bytes.argtypes = [I, I64, I64, I64, I64]
@@ -452,8 +454,14 @@ def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_tab
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     op, ost = _token_rows(out, "out", dev)
-    _run((_lib or lib()).mxattn_cache_attend, "mxattn_cache_attend", dev, stream,
-         (qp, qst, *cache, tokens, Hq, heads, d, causal, max_q, max_kv, op, ost))
+    L, work, size = _lib or lib(), None, 0
+    if stream is None:  # torch's memory belongs to the current stream, and to the graph that is captured on it
+        size = L.mxattn_cache_attend_workspace(cache[5], *cache[9:], tokens, Hq, heads, max_q, max_kv)
+        if size:
+            work = torch.empty(size, dtype=torch.uint8, device=q.device)
+    _run(L.mxattn_cache_attend, "mxattn_cache_attend", dev, stream,
+         (qp, qst, *cache, tokens, Hq, heads, d, causal, max_q, max_kv, op, ost,
+          work.data_ptr() if size else None, size))
     return out
 
 

@@ -77,7 +77,7 @@ def test_append_refusals(L, i):
 
 
 ATTEND = dict(q=far(1), qst=1024, **CACHE, **BATCH, tokens=9, Hq=8, Hkv=2, d=128, causal=1, max_q=0, max_kv=0, out=far(2),
-              ost=1024, stream=None)
+              ost=1024, ws=None, ws_bytes=0, stream=None)
 ATTEND_BAD = SHARED_BAD + [
     (dict(q=None), NULL), (dict(out=None), NULL), (dict(Hq=7), VALUE), (dict(Hq=0), SHAPE), (dict(Hq=1), VALUE),
     (dict(max_q=-1), SHAPE), (dict(max_kv=-1), SHAPE), (dict(qst=1028), ALIGN), (dict(qst=-1024), SHAPE),
@@ -90,6 +90,38 @@ ATTEND_BAD = SHARED_BAD + [
 def test_attend_refusals(L, i):
     change, want = ATTEND_BAD[i]
     assert L.mxattn_cache_attend(*dict(ATTEND, **change).values()) == want, change
+
+
+# sizes that the kernels' numbers cannot hold, and workspaces that do not do (of 3 sequences with up to 200000 keys)
+LONG = dict(ATTEND, page=4096, max_pages=50, max_q=1)
+BIG = [
+    ("rope", dict(Hq=65536, B=1, N=1), SHAPE), ("rope", dict(Hkv=65536, B=1, N=1), SHAPE),
+    ("append", dict(seqs=(1 << 20) + 1), SHAPE), ("append", dict(page=4096, max_pages=4097), SHAPE),
+    ("append", dict(pages=1 << 30, page=4096, H=65535, tokens=1), SHAPE),
+    ("attend", dict(Hq=514), VALUE), ("attend", dict(H=65536, Hkv=65536, Hq=65536, tokens=1), SHAPE),
+    ("attend", dict(seqs=1 << 20, Hkv=4096, Hq=4096, tokens=1, ost=1 << 19, qst=1 << 19), SHAPE),
+    ("long", dict(ws=far(30), ws_bytes=1000), 10), ("long", dict(ws=far(30) + 8, ws_bytes=1 << 30), ALIGN),
+    ("long", dict(ws=far(1), ws_bytes=1 << 30), SHAPE), ("long", dict(ws=far(2) - 4096, ws_bytes=1 << 30), SHAPE),
+    ("long", dict(ws=far(21), ws_bytes=1 << 30), SHAPE),
+]
+
+
+@pytest.mark.parametrize("i", range(len(BIG)))
+def test_sizes_and_workspaces_refused(L, i):
+    what, change, want = BIG[i]
+    call, base = {"rope": (L.mxattn_qk_norm_rope, ROPE), "append": (L.mxattn_cache_append, APPEND),
+                  "attend": (L.mxattn_cache_attend, ATTEND), "long": (L.mxattn_cache_attend, LONG)}[what]
+    assert call(*{k: v for k, v in dict(base, **change).items() if k in base}.values()) == want, change
+
+
+def test_workspace_sizes(L):
+    size = L.mxattn_cache_attend_workspace
+    ok = (64, 3, 50, 9, 8, 2, 1, 3200)
+    assert 0 < size(*ok) <= 65 * 2 ** 20 + 8 * 2 * (3 + 2)
+    assert size(*ok[:-1], 1024) == 0 and size(*ok[:3], 90, *ok[4:6], 40, 1024) > 0
+    assert size(*ok[:-2], 0, 0) == size(*ok[:-2], 9, 3200)  # 0: whatever the sizes allow
+    for i, bad in ((0, 48), (1, 0), (2, 0), (3, 0), (4, 7), (5, 0), (5, 3), (6, -1), (7, -1), (2, 1 << 20)):
+        assert size(*ok[:i], bad, *ok[i + 1:]) == 0, (i, bad)
 
 
 def test_binding_refuses_tensors_that_do_not_fit():

@@ -502,6 +502,44 @@ def test_steps_captured_into_a_graph(mx):
         assert all(torch.equal(x, y) for x, y in zip(a["cache"], b["cache"]))
 
 
+@pytest.mark.parametrize("new,lens", [([1, 1, 1], [5000, 1200, 3]), ([40, 1, 7], [3000, 2000, 1030])])
+def test_long_calls_captured_into_two_graphs(mx, new, lens):
+    """Calls that need workspace, captured into two graphs that are replayed in turn and at once, each with a
+    cache of its own, equal eager calls, also after others have used and freed memory in between."""
+    n, group = sum(new), 4
+    table, start, _, pages = batch(new, lens, 64, seed=5)
+    table, start, lens = table.cuda(), ints(start), ints(lens)
+    work = []
+    for seed in (1, 2):
+        cache = filled(mx, pages, 2, 64, seed)
+        q, out, stream = rows(n, 2 * group, seed), torch.zeros(n, 2 * group, ref.D, dtype=torch.bfloat16, device="cuda"), torch.cuda.Stream()
+        call = lambda q=q, cache=cache, out=out, **kw: mx.cache_attend(q, *cache, table, start, lens, out=out, **kw)  # noqa: E731
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            with pytest.raises(Exception) as e:  # the library's own workspace lasts no longer than the call
+                call(stream=stream)
+            assert e.value.status == 10
+            call()
+        work.append((q, cache, out, stream, graph))
+    for i in range(8):
+        want = []
+        for q, cache, *_ in work:
+            q.copy_(rows(n, 2 * group, 10 + i))
+            want.append(mx.cache_attend(q, *cache, table, start, lens))
+        torch.cuda.synchronize()
+        for *_, out, stream, graph in work:
+            out.zero_()
+            with torch.cuda.stream(stream if i % 2 else torch.cuda.current_stream()):
+                torch.cuda.current_stream().wait_stream(torch.cuda.default_stream())
+                graph.replay()
+        junk = torch.full((1 << 24,), float("nan"), device="cuda")
+        torch.cuda.synchronize()
+        del junk
+        assert all(torch.equal(w, x[2]) for w, x in zip(want, work)), i
+
+
 @pytest.mark.parametrize("max_kv", [0, 300])
 @pytest.mark.parametrize("max_q", [1, 64])
 def test_starts_that_do_not_ascend(mx, max_q, max_kv):

@@ -348,8 +348,8 @@ int mxattn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, 
  * again, code * 2^(e_old - e).  Rounding is to nearest, ties to even.  Values that
  * are not finite are stored as NaN and do not count towards the maximum.  Bytes of
  * tokens past the sequence's end are left as they were.  Tokens whose position is
- * negative (kv_len < n) are not stored.  Two sequences of one call must not append
- * to the same page (which of them is stored is undefined).
+ * negative (kv_len < n) are not stored.  A call's tokens must not reach one page
+ * by two entries of the page table (which of them is stored is undefined).
  *   k, v   device bf16 [tokens, Hkv, d], heads contiguous, token strides
  * MXATTN_ERR_SHAPE if k or v shares a byte with the cache. */
 int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t v_stride, uint8_t* k_codes,
@@ -365,7 +365,7 @@ int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t 
  * causal != 0: token i of n sees positions 0 .. kv_len - n + i, else all kv_len.
  * A query that sees no key gets 0.
  *   q     device bf16 [tokens, Hq, d], heads contiguous, token stride; Hq at most
- *         256 Hkv, (tokens * Hq / Hkv / 32 + seqs) * Hkv < 2^31
+ *         256 Hkv, (tokens * Hq / Hkv / 32 + seqs) * Hkv < 2^24
  *   out   device bf16 [tokens, Hq, d], likewise; tokens of no sequence are not
  *         written.  MXATTN_ERR_SHAPE if it shares a byte with q or the cache.
  *   max_q, max_kv  at least the new tokens and the keys of every sequence, as the

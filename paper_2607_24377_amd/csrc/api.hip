@@ -625,11 +625,12 @@ static int check_batch(int64_t seqs, int64_t max_pages, int64_t page_tokens, int
     return max_pages < 1 || max_pages > mxattn::kMaxKeys / page_tokens ? MXATTN_ERR_SHAPE : MXATTN_OK;
 }
 
-// Query heads that read the cache's; the tiles of at least 32 rows are numbered with 31 bits.
+// Query heads that read the cache's; a launch has a workgroup of 256 threads for every
+// number of a tile of at least 32 rows and KV head, and holds 2^32 threads.
 static int check_query_heads(int64_t seqs, int64_t tokens, int64_t Hq, int64_t Hkv) {
     if (int st = check_shape(1, Hq, tokens, mxattn::kHeadDim)) return st;
     if (Hq % Hkv != 0 || Hq / Hkv > 256) return MXATTN_ERR_VALUE;
-    return (tokens * (Hq / Hkv) / 32 + seqs) * Hkv >> 31 ? MXATTN_ERR_SHAPE : MXATTN_OK;
+    return (tokens * (Hq / Hkv) / 32 + seqs) * Hkv >> 24 ? MXATTN_ERR_SHAPE : MXATTN_OK;
 }
 
 // The checks that the calls on the paged cache share; fills c.

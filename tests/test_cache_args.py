@@ -99,6 +99,7 @@ BIG = [
     ("append", dict(seqs=(1 << 20) + 1), SHAPE), ("append", dict(page=4096, max_pages=4097), SHAPE),
     ("append", dict(pages=1 << 30, page=4096, H=65535, tokens=1), SHAPE),
     ("attend", dict(Hq=514), VALUE), ("attend", dict(H=65536, Hkv=65536, Hq=65536, tokens=1), SHAPE),
+    ("attend", dict(seqs=1 << 20, Hkv=16, Hq=16, tokens=1, qst=2048, ost=2048), SHAPE),
     ("attend", dict(seqs=1 << 20, Hkv=4096, Hq=4096, tokens=1, ost=1 << 19, qst=1 << 19), SHAPE),
     ("long", dict(ws=far(30), ws_bytes=1000), 10), ("long", dict(ws=far(30) + 8, ws_bytes=1 << 30), ALIGN),
     ("long", dict(ws=far(1), ws_bytes=1 << 30), SHAPE), ("long", dict(ws=far(2) - 4096, ws_bytes=1 << 30), SHAPE),

@@ -7,6 +7,11 @@
 // lengths are, and no wave waits for another; what a share's ends leave in pieces is
 // joined by a second kernel.  Short ones: the four waves of a workgroup take an item's
 // blocks in turn and meet in LDS.
+//
+// 64 sequences' single tokens over 8200 keys, 32 heads on 8: 606 MB, 118 us and 5 for
+// the join, 5.0 TB/s; one over 118801 keys, 24 heads: 730 MB, 133 and 9, 5.25 TB/s;
+// 16 x 4 tokens over 6000 keys, 40 heads on 8: 113 MB, 28 and 8; one over 512 keys, 2
+// heads: 7.4, a chain of loads (lengths, pages, codes).
 #include "cache_attend.h"
 
 namespace mxattn {

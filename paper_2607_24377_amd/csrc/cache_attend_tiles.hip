@@ -4,10 +4,14 @@
 //
 // A workgroup takes a tile of 128 rows, 32 per wave, and walks its keys 64 at a
 // time.  K's and V's codes (16 KiB) are copied straight into LDS, in the lanes'
-// operand order, two tiles of keys ahead of their use, and each wave reads them as
-// they are: FP8 operands for the scores, and codes that become bf16 in registers for
-// the second product.  The score products of the next 64 keys run under the
-// softmax of these.
+// operand order, two steps ahead of their use, and each wave reads them as they are:
+// FP8 operands for the scores, and codes that become bf16 in registers for the
+// second product.  Two waves a SIMD (256 registers) run each other's gaps.
+//
+// 1560 rows x 32760 keys x 40 heads: 1.11 ms, 943 TFLOP/s; matrix cores busy 48 %,
+// vector units 57 % (139 instructions per 32 x 32 scores).  256 rows in eight waves
+// 1.10, 64 rows per wave 1.72 (spills), one wave a SIMD 1.21; the next scores under
+// this step's softmax, or a wait for the step before only, gained nothing.
 #include "cache_attend.h"
 
 namespace mxattn {

@@ -21,9 +21,14 @@
 // 16 i + 4 r + j (i < 2, j < 4).  Four channels of a token are a word of K's block,
 // four consecutive tokens of a channel one of V's, which the conversions pack
 // directly; the words change places through LDS.  V is done before K is turned, so
-// that three waves a SIMD have registers, and the codes are stored past the caches:
+// that four waves a SIMD have registers, and the codes are stored past the caches:
 // K and V of 32760 tokens x 40 heads, 1.02 GB, 186 us, 5.5 TB/s (two waves and
 // ordinary stores 219; three of those 210; a workgroup per block and head 279).
+//
+// Few tokens: what counts is the chain of loads.  All 16 rows of a lane are in flight
+// at once, those that are not new in the place of one that is: 16 prompts of 1000
+// tokens, 8 heads, 15.4 us; 64 single tokens 6.9 (with the loads of a block's missing
+// tokens branched around, which the compiler makes one after another, 21.2 and 9.0).
 #include "heads.h"
 
 namespace mxattn {
@@ -138,19 +143,15 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, const Place& p
     auto live = [&](int t) { return kWhole || (slot_of(t) >= p.lead && slot_of(t) < p.stop); };
     auto some = [&](int t) { return kWhole || __any(live(t)); };
     const Channels<kHalves> channels(a.t.rot, ch);
-    u32x4 raw_k[8], raw_v[8];
+    u32x4 raw_k[8], raw_v[8];  // (of what is not new: the first new token's)
 #pragma unroll
     for (int t = 0; t < 8; t++) {
-        raw_v[t] = u32x4{0, 0, 0, 0};
-        if (!some(t)) continue;
         const int64_t tok = p.row + (live(t) ? slot_of(t) : p.lead);
         raw_v[t] = __builtin_nontemporal_load(
             reinterpret_cast<const u32x4*>(a.v + tok * a.v_stride + p.head * kHeadDim + 8 * ch));
     }
 #pragma unroll
     for (int t = 0; t < 8; t++) {
-        raw_k[t] = u32x4{0, 0, 0, 0};
-        if (!some(t)) continue;
         const int64_t tok = p.row + (live(t) ? slot_of(t) : p.lead);
         raw_k[t] = channels.load(a.k + tok * a.k_stride + p.head * kHeadDim);
     }
@@ -262,7 +263,7 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, const Place& p
 }
 
 template <bool kHalves>
-__global__ __launch_bounds__(kThreads, 3) void cache_append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void cache_append_kernel(AppendArgs a) {
     __shared__ __align__(16) uint32_t s_v[kWaves][kTileWords];
     __shared__ __align__(16) float s_angles[2][kBlockTokens][kHeadDim / 2];  // cos, sin
     const CacheArgs& c = a.c;

@@ -607,7 +607,7 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
     };
     float m, l;
     float4 o;
-    if (count <= 4) {  // a row for each group
+    if (count <= 8) {  // a row for each group (128 items of 8 parts and 32 rows 9.8 us, by all groups 12.1)
         for (int r = 8 * blockIdx.y + g; r < rows; r += 8 * gridDim.y) {
             gather(r, 0, 1, m, l, o);
             finish(r, l, o);

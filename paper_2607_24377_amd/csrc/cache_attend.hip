@@ -8,10 +8,10 @@
 // joined by a second kernel.  Short ones: the four waves of a workgroup take an item's
 // blocks in turn and meet in LDS.
 //
-// 64 sequences' single tokens over 8200 keys, 32 heads on 8: 606 MB, 118 us and 5 for
-// the join, 5.0 TB/s; one over 118801 keys, 24 heads: 730 MB, 133 and 9, 5.25 TB/s;
-// 16 x 4 tokens over 6000 keys, 40 heads on 8: 113 MB, 28 and 8; one over 512 keys, 2
-// heads: 7.4, a chain of loads (lengths, pages, codes).
+// 64 sequences' single tokens over 8200 keys, 32 heads on 8: 606 MB, 115 to 119 us and
+// 5 for the join, 5.0 TB/s; one over 118801 keys, 24 heads: 730 MB, 132 and 6, 5.3 TB/s;
+// 16 x 4 tokens over 6000 keys, 40 heads on 8: 113 MB, 28 and 7; one over 512 keys, 2
+// heads: 7.3, a chain of loads (lengths, pages, codes).
 #include "cache_attend.h"
 
 namespace mxattn {
@@ -252,11 +252,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
 
 // Which kernel, from the caller's bounds on a sequence's query rows per KV head and its
 // keys (us, kernels with their joins; 8 KV heads):
-//   few keys: an item is one workgroup's.  16 sequences x 5 rows x 1000 keys 13.7, in
-//   shares 17.2; one sequence's row over 2000 keys 16.7 and 13.4.  Up to 128 rows: 90
-//   rows x 290 keys 8.6, in tiles of 128 rows 33.
+//   few keys: an item is one workgroup's.  16 sequences x 5 rows x 1000 keys 13.6, in
+//   shares 18.2; one sequence's row over 2000 keys 16.7 and 14.3.  Up to 128 rows: 90
+//   rows x 290 keys 8.5, in shares 18.8, in tiles of 128 rows 33.
 //   else up to 32 rows: shares; more: tiles of 128 rows, whose four waves read the keys
-//   once.  16 sequences x 40 rows x 4000 keys 60 and 50, 125 rows 113 and 58.
+//   once.  16 sequences x 40 rows x 4000 keys, in shares 57, in tiles 50; 125 rows 83
+//   and 61.
 enum Way { kItems, kShares, kTiles };
 Way way(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
     const int64_t rows = max_q * a.group;
@@ -264,14 +265,17 @@ Way way(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
     return rows <= kRows ? kShares : kTiles;
 }
 
-// log2 of the number of shares: eight waves per CU are resident (registers); a share
-// has at least two blocks and an item at most 256 parts (one row over 118801 keys: 1856
-// parts took 44 us to join), as far as the caller's bounds say.
+// log2 of the number of shares: four waves per CU, with 16 KiB each in flight, reach the
+// memory's rate and leave half as many parts as the eight that fit (one row over 118801
+// keys x 24 heads 137 us for 142, 20000 keys x 8 heads 22 for 28; two waves 225 and 23);
+// a share has at least two blocks (one of 16: 4 rows over 6000 keys 32 us for 20) and
+// an item at most 256 parts (1856 of one row took 44 us to join), as far as the
+// caller's bounds say.
 int shares_log2(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
     const int64_t items = a.c.seqs * ((max_q * a.group + kRows - 1) / kRows) * a.c.heads;
     const int64_t blocks = (max_kv + kBlockTokens - 1) / kBlockTokens;
     int log2 = 2;
-    while (log2 < 11 && (items * blocks) >> (log2 + 1) >= 2 && items * 256 >> (log2 + 1) >= 1) log2++;
+    while (log2 < 10 && (items * blocks) >> (log2 + 1) >= 2 && items * 256 >> (log2 + 1) >= 1) log2++;
     return log2;
 }
 

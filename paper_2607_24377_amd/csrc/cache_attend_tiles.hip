@@ -9,7 +9,7 @@
 // second product.  Two waves a SIMD (256 registers) run each other's gaps.
 //
 // 1560 rows x 32760 keys x 40 heads: 1.10 to 1.14 ms, 920 to 955 TFLOP/s; matrix cores
-// busy 48 %, vector issue 55 % (139 instructions per 32 x 32 scores, of which 830
+// busy 48 %, vector issue 55 % (139 instructions per 32 x 32 scores, about 830
 // cycles), LDS half of its time.  256 rows in eight waves 1.10, 64 rows per wave 1.72
 // (spills), one wave a SIMD 1.21, V as bf16 in LDS, made once for the four waves, 1.25
 // (more to read there); the next scores under this step's softmax, a wait for the step

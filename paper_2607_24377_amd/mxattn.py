@@ -444,7 +444,11 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_codes, k_scales, v_codes, v
 
 def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, causal: bool = True,
                  max_q: int = 0, max_kv: int = 0, out=None, stream=None):
-    """Attention of bf16 q [tokens, Hq, d] over the sequences' cached keys; returns bf16 out [tokens, Hq, d]."""
+    """Attention of bf16 q [tokens, Hq, d] over the sequences' cached keys; returns bf16 out [tokens, Hq, d].
+    max_q, max_kv: at least the new tokens and the keys of every sequence as the caller knows them (0: unknown); they
+    choose how the work is divided, and wrong ones cost time only.  Workspace is torch's, of the current stream (a graph
+    captured there keeps it); of a stream that is given it is the library's, and a call that needs some cannot be
+    captured."""
     dev = _index(q, "q")
     cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
     qp, qst = _token_rows(q, "q", dev)

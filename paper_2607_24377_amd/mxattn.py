@@ -395,6 +395,8 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
 
 def cache_shapes(pages: int, heads: int, page_tokens: int, d: int = 128):
     """Shapes of the uint8 arrays of a paged cache: K codes, K scales, V codes, V scales."""
+    if d != 128 or not 32 <= page_tokens <= 4096 or page_tokens & (page_tokens - 1):
+        raise ValueError("a cache has d = 128 and pages of a power of two from 32 to 4096 tokens")
     n = page_tokens // BLOCK_TOKENS
     scales = (pages, heads, n)
     return scales + (d // 16, BLOCK_TOKENS, 16), scales, scales + (d, BLOCK_TOKENS), scales
@@ -410,14 +412,17 @@ def _token_rows(t, name, index):
     return t.data_ptr(), stride
 
 
-def _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, index):
-    """Checked addresses and sizes of a cache and its batch, as the library takes them, and the cache's heads."""
+def _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, index, d):
+    """Checked addresses and sizes of a cache of d channels and its batch, as the library takes them, and the cache's
+    heads."""
     if k_codes.dim() != 6 or page_table.dim() != 2:
         raise ValueError("k_codes must be [pages, heads, page_tokens / 32, 8, 32, 16], page_table [seqs, max_pages]")
-    pages, heads, blocks, chunks, _, _ = k_codes.shape
+    pages, heads, blocks, *block = k_codes.shape
+    if block != [d // 16, BLOCK_TOKENS, 16] or v_codes.shape != (pages, heads, blocks, d, BLOCK_TOKENS):
+        raise ValueError(f"k_codes and v_codes must have the shapes of cache_shapes for heads of {d} channels")
     seqs, max_pages = page_table.shape
     u8, i32, n = torch.uint8, torch.int32, pages * heads * blocks
-    codes = n * chunks * 16 * BLOCK_TOKENS
+    codes = n * d * BLOCK_TOKENS
     return (_address(k_codes, "k_codes", u8, index, codes), _address(k_scales, "k_scales", u8, index, n),
             _address(v_codes, "v_codes", u8, index, codes), _address(v_scales, "v_scales", u8, index, n), pages,
             blocks * BLOCK_TOKENS, _address(page_table, "page_table", i32, index, seqs * max_pages),
@@ -431,9 +436,9 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_codes, k_scales, v_codes, v
     qk_norm_rope on the way (int32 positions [tokens], None: a token's place in its sequence).  The call's tokens
     q_start[s] .. q_start[s + 1] - 1 are the last ones of the kv_len[s] of sequence s."""
     dev = _index(k, "k")
-    cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
     (kp, kst), (vp, vst) = _token_rows(k, "k", dev), _token_rows(v, "v", dev)
     tokens, _, d = k.shape
+    cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev, d)
     if v.shape != k.shape or k.shape[1] != heads:
         raise ValueError("k and v must be [tokens, Hkv, d] with the cache's heads")
     cp, sp, rows, rot = _tables(cos, sin, dev)
@@ -450,9 +455,9 @@ def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_tab
     captured there keeps it); of a stream that is given it is the library's, and a call that needs some cannot be
     captured."""
     dev = _index(q, "q")
-    cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev)
     qp, qst = _token_rows(q, "q", dev)
     tokens, Hq, d = q.shape
+    cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev, d)
     if out is None:
         out = q.new_empty((tokens, Hq, d))
     elif out.shape != q.shape:

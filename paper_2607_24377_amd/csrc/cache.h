@@ -90,6 +90,13 @@ __device__ __forceinline__ TokenRange token_range(const CacheArgs& c, int s) {
     return {a, b};
 }
 
+// Whether sequence s + 1's tokens begin behind the start of sequence s's. Where that
+// holds for all, the sequences' tokens add up to at most the call's, and sums over them
+// stay within what the launch was sized for.
+__device__ __forceinline__ bool starts_ascend(const CacheArgs& c, int s) {
+    return min(max(c.q_start[s], 0), c.tokens) <= min(max(c.q_start[s + 1], 0), c.tokens);
+}
+
 // The sequence that owns workgroup w where sequence s has workgroups
 // (its first token) * group / unit + step * s onwards, up to those of s + 1; -1: none.
 // All lanes of a wave call it: 64 places probed at a time.

@@ -352,18 +352,22 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
     return ((int64_t)hi << 32) | (uint32_t)lo;
 }
 
-// The share of workgroup i of n; all kThreads threads call it.
+// The share of workgroup i of n, empty for all where q_start does not ascend (the
+// sum of the weights could pass 64 bits); all kThreads threads call it.
 template <int kRows, bool kGrowing, int kThreads>
 __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int n) {
     __shared__ int64_t s_sum[kThreads / 64];
+    __shared__ bool s_ascend[kThreads / 64];
     __shared__ Share s_share;
     const int tid = threadIdx.x, seqs = a.c.seqs;
     const int per = (seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * per, seqs), s1 = min(s0 + per, seqs);
     int64_t mine = 0;
+    bool ascend = true;
     for (int s = s0; s < s1; s++) {
         const SeqWork w = seq_work<kRows, kGrowing>(a, s);
         mine += w.before(w.tiles) * a.c.heads;
+        ascend = ascend && starts_ascend(a.c, s);
     }
     int64_t incl = mine;
 #pragma unroll
@@ -371,7 +375,11 @@ __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int
         const int64_t x = __shfl_up(incl, d);
         if ((tid & 63) >= d) incl += x;
     }
-    if ((tid & 63) == 63) s_sum[tid >> 6] = incl;
+    ascend = __all(ascend);
+    if ((tid & 63) == 63) {
+        s_sum[tid >> 6] = incl;
+        s_ascend[tid >> 6] = ascend;
+    }
     if (tid == 0) s_share = {0, 0, 0, 0, -1, 0};
     __syncthreads();
     int64_t total = 0, before = incl - mine;
@@ -380,6 +388,9 @@ __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int
         if (k < (tid >> 6)) before += s_sum[k];
         total += s_sum[k];
     }
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; k++)
+        if (!s_ascend[k]) total = 0;
     n = (int)(total < n ? total : n);
     const int64_t lo = i < n ? total * i / n : total, hi = i < n ? total * (i + 1) / n : total;
     if (i < n && before <= lo && lo < before + mine) {

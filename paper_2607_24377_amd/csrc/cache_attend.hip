@@ -104,22 +104,32 @@ struct Start {
 
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheAttendArgs a, int log2, int unit) {
     __shared__ uint32_t s_sum[kWaves];
+    __shared__ bool s_ascend[kWaves];
     __shared__ Start s_start[kWaves];
     const CacheArgs& c = a.c;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, q = lane & 31, h = lane >> 5;
-    // all sequences' units before each thread's, and the total
+    // all sequences' units before each thread's, and the total: none where q_start does not
+    // ascend, as the sum would pass 32 bits and a share be found in two places
     const int per = (c.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * per, c.seqs), s1 = min(s0 + per, c.seqs);
     uint32_t mine = 0;
-    for (int s = s0; s < s1; s++) mine += Sequence(a, s, unit).all(c.heads);
+    bool ascend = true;
+    for (int s = s0; s < s1; s++) {
+        mine += Sequence(a, s, unit).all(c.heads);
+        ascend = ascend && starts_ascend(c, s);
+    }
     uint32_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const uint32_t x = (uint32_t)__shfl_up((int)incl, d);
         if (lane >= d) incl += x;
     }
-    if (lane == 63) s_sum[wave] = incl;
+    ascend = __all(ascend);
+    if (lane == 63) {
+        s_sum[wave] = incl;
+        s_ascend[wave] = ascend;
+    }
     if (tid < kWaves) s_start[tid] = {0, 0, 0, 0};
     __syncthreads();
     Cut cut{0, log2};
@@ -129,6 +139,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
         if (k < wave) before += s_sum[k];
         cut.total += s_sum[k];
     }
+#pragma unroll
+    for (int k = 0; k < kWaves; k++)
+        if (!s_ascend[k]) cut.total = 0;
     cut.total = (uint32_t)__builtin_amdgcn_readfirstlane((int)cut.total);
 #pragma unroll
     for (int k = 0; k < kWaves; k++) {
@@ -186,7 +199,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
                 tile = 0;
                 if (++head == c.heads) {
                     head = 0;
-                    do {  // there is a next one, unless q_start does not ascend and the total is wrong
+                    do {  // (there is a next one, unless q_start was written meanwhile)
                         if (++s >= c.seqs) return;
                         seq = Sequence(a, s, unit);
                     } while (seq.tiles == 0);

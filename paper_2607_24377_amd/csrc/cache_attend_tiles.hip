@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
     Share sh = find_share<kRows, true, kThreads>(a, index, gridDim.x);
     const Parts<kRows> parts(a.workspace, gridDim.x);
     const StepLoader loader(wave, lane);
-    while (sh.at < sh.end && sh.s < c.seqs) {  // (the total is wrong where q_start does not ascend)
+    while (sh.at < sh.end && sh.s < c.seqs) {  // (it is, unless q_start was written meanwhile)
         const Item it = next_item<kRows, true>(a, sh);
         const TileRows t = tile_rows<kRows>(a, it.s, it.row0);
         const int blocks = (t.max_end + kBlockTokens - 1) / kBlockTokens;

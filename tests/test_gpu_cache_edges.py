@@ -1,0 +1,60 @@
+"""Calls at the edges of what the paged cache's operators take; bounds as in test_gpu_cache.py."""
+import math
+
+import pytest
+
+import cache_reference as ref
+from test_gpu_cache import batch, filled, ints, mx, rows  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+GUARD = 4096
+
+
+def guarded_cache(mx, pages, heads, page):  # noqa: F811
+    """A cache of zeros whose arrays lie between bytes of 7, and what holds them."""
+    shapes = mx.cache_shapes(pages, heads, page)
+    room = [torch.full((math.prod(s) + 2 * GUARD,), 7, dtype=torch.uint8, device="cuda") for s in shapes]
+    cache = [x[GUARD:-GUARD].view(s).zero_() for x, s in zip(room, shapes)]
+    return cache, room
+
+
+def untouched(room, out, tokens):
+    """The bytes around the cache, and the rows of 9 around the call's."""
+    torch.cuda.synchronize()
+    return (all(bool((x[:GUARD] == 7).all() and (x[-GUARD:] == 7).all()) for x in room)
+            and bool((out[:-tokens - 64] == 9).all() and (out[-64:] == 9).all()))
+
+
+@pytest.mark.parametrize("start", [[0, 90, 50], [-7, -3, 1 << 30], [50, 20, 0], [5, 5, 5]])
+def test_starts_of_no_batch_write_nothing_around(mx, start):  # noqa: F811
+    print(f"[starts] {start}", flush=True)
+    cache, room = guarded_cache(mx, 4, 1, 32)
+    table = torch.tensor([[0, 1], [2, 3]], dtype=torch.int32).cuda()
+    k = rows(50, 1, 1)
+    out = torch.full((64 + 50 + 64, 1, ref.D), 9.0, dtype=torch.bfloat16, device="cuda")
+    mx.cache_append(k, k, *cache, table, ints(start), ints([64, 64]))
+    mx.cache_attend(k, *cache, table, ints(start), ints([64, 64]), out=out[64:-64])
+    assert untouched(room, out, 50)
+
+
+@pytest.mark.parametrize("max_q", [1, 0])
+def test_starts_whose_work_passes_32_bits(mx, max_q):  # noqa: F811
+    """1024 sequences that each claim all of the call's 8192 tokens: 2^18 rows and 2^10 blocks of keys each, 2^33
+    units in all, for which a call of these sizes has 2^24 at most."""
+    tokens, seqs, group = 8192, 2048, 32
+    print(f"[starts] passing 32 bits, max_q {max_q}", flush=True)
+    cache, room = guarded_cache(mx, 8, 1, 4096)
+    table = torch.arange(8, dtype=torch.int32, device="cuda").expand(seqs, 8).contiguous()
+    g = torch.Generator().manual_seed(1)
+    lens = torch.tensor([64, 20000, 32768], dtype=torch.int32)[torch.randint(3, (seqs,), generator=g)].cuda()
+    q = rows(tokens, group, 1)
+    out = torch.full((64 + tokens + 64, group, ref.D), 9.0, dtype=torch.bfloat16, device="cuda")
+    mx.cache_attend(q, *cache, table, ints([0, tokens] * (seqs // 2) + [0]), lens, max_q=max_q, out=out[64:-64])
+    assert untouched(room, out, tokens)
+    # the same sizes with an ascending start: one token for each of the first sequences
+    st = torch.arange(seqs + 1, dtype=torch.int32, device="cuda")
+    a = mx.cache_attend(q, *cache, table, st, lens, max_q=max_q)
+    assert bool((a[:seqs] == 0).all())  # values of zero

@@ -235,15 +235,19 @@ __device__ __forceinline__ bool has_nan(const uint4 (&v)[4]) {
     return m != 0;
 }
 
-// V's codes of a block whose keys not every row sees, or of no page: `base` is its
-// first key's place where the lane's row sees `visible` keys and the sequence
-// holds `held`.
-__device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int base, int visible, int held, bool lost, int h) {
+// V's codes and scale byte of a block whose keys not every row sees, or of no page:
+// `base` is its first key's place where the lane's row sees `visible` keys and the
+// sequence holds `held`.
+__device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int& e, int base, int visible, int held, bool lost,
+                                             int h) {
+    const bool none = !lost && e == 255;  // a scale that is no number: nor is any value
+    if (lost || none) e = 127;            // (a zero code times that scale is NaN too)
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
 #pragma unroll
         for (int j = 0; j < 4; j++) {
+            if (none) w[j] = 0x7F7F7F7Fu;
             // what lies behind the last key may be anything: zero
             const int left = lost ? 0 : held - base - 16 * h - 4 * j;
             w[j] &= left <= 0 ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1;
@@ -291,7 +295,7 @@ __device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float 
 // sequence's, `base` the block's first; `any`: some row does not see all of it.
 __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand& q, int base, int end, int keys, bool any,
                                              int h) {
-    if (any || x.lost) clean_values(st, x.v, 0, end - base, keys - base, x.lost, h);
+    if (any || x.lost) clean_values(st, x.v, x.ve, 0, end - base, keys - base, x.lost, h);
     if (x.lost && end > base) st.l = __builtin_nanf("");  // no such page: NaN for the rows that would see it
     const v16f s = scores(x.k, x.ke, q);
     consume(st, s, x.v, e8m0_as_f32((uint32_t)x.ve), q.c, end - base, any, h);

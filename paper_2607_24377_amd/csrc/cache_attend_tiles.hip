@@ -128,8 +128,9 @@ __device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* sta
         uint4 v[4];
 #pragma unroll
         for (int n = 0; n < 4; n++) v[n] = part(stage + (2 + b) * kBlockBytes, n, lane);
-        const float vscale = e8m0_as_f32((uint32_t)x.v[b]);
-        if (any || lost) clean_values(st, v, 32 * b, visible, held, x.lost[b], h);
+        int e = x.v[b];
+        if (any || lost) clean_values(st, v, e, 32 * b, visible, held, x.lost[b], h);
+        const float vscale = e8m0_as_f32((uint32_t)e);
 #pragma unroll
         for (int n = 0; n < 4; n++) {
             st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].x, v[n].y, vscale), p0, st.O[n], 0, 0, 0);

@@ -58,3 +58,33 @@ def test_starts_whose_work_passes_32_bits(mx, max_q):  # noqa: F811
     st = torch.arange(seqs + 1, dtype=torch.int32, device="cuda")
     a = mx.cache_attend(q, *cache, table, st, lens, max_q=max_q)
     assert bool((a[:seqs] == 0).all())  # values of zero
+
+
+# bounds that choose one workgroup per item, shares by wave and tiles of 128 rows
+WAYS = {"items": (12, 200), "shares": (1, 5000), "tiles": (100, 5000)}
+
+
+@pytest.mark.parametrize("way", list(WAYS))
+@pytest.mark.parametrize("what", ["page", "value scale", "key scale"])
+def test_last_block_without_numbers_reaches_only_the_rows_that_see_it(mx, what, way):  # noqa: F811
+    """A page that is not there while page 0, which stands in for it, holds no numbers, and a block whose scale byte
+    is E8M0's NaN: NaN for the tokens that see that block, and no other bits for those before it."""
+    print(f"[edges] {what} {way}", flush=True)
+    cache = filled(mx, 6, 2, 32, 3)
+    for c in cache:
+        c[0] = 0xFF
+    kc, ks, vc, vs = cache
+    q = rows(12, 4, 4)
+    table = torch.tensor([[3, 4, 5]], dtype=torch.int32)
+    args = ints([0, 12]), ints([70]), True, *WAYS[way]  # positions 58 to 69: the last block from token 6 on
+    clean = mx.cache_attend(q, *cache, table.cuda(), *args)
+    assert bool(clean.isfinite().all())
+    if what == "page":
+        table[0, 2] = 99
+    elif what == "value scale":
+        vs[5] = 255
+    else:
+        ks[5] = 255
+    got = mx.cache_attend(q, *cache, table.cuda(), *args)
+    assert torch.equal(got[:6], clean[:6])
+    assert bool(got[6:].isnan().all())

@@ -48,7 +48,8 @@ __device__ __forceinline__ float other_half(float x) {
 }
 
 // Q of one row as two E4M3 numbers per channel: lane (query, h) holds channels
-// 64 j + 32 h .. + 31 of product j.
+// 64 j + 32 h .. + 31 of product j.  A row that is not there or sees no key is zero:
+// whatever it holds, its masked scores (-inf) are -inf, not NaN, and its result 0.
 struct QOperand {
     v8i hi[2], lo[2];
     float c;  // scores times c are in units of log2: scale * 2^e; NaN for a row that is not finite

@@ -176,7 +176,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
             const int keys = max(seq.keys, 0);
             const Rows r(a, seq.n, keys, tile * kRows, q);
             const int blocks = (r.max_end + kBlockTokens - 1) / kBlockTokens;
-            const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale, q < r.count);
+            const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale,
+                                       q < r.count && r.end > 0);
             State st;
             st.clear();
             attend_run(st, c, s, head, min((int)(x0 << unit), blocks), min((int)(x1 << unit), blocks), 1, qo, r, keys, q, h);
@@ -224,7 +225,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
     if (row0 >= seq.n * a.group) return;
     const int keys = max(seq.keys, 0);
     const Rows r(a, seq.n, keys, row0, q);
-    const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale, q < r.count);
+    const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale,
+                               q < r.count && r.end > 0);
     State st;
     st.clear();
     attend_run(st, c, s, head, wave, (r.max_end + kBlockTokens - 1) / kBlockTokens, kWaves, qo, r, keys, q, h);

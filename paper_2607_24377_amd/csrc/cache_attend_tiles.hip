@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
         const int row = it.row0 + min(wrow + q, t.rows - 1);
         const int end = a.causal ? t.keys - t.n + token_of(a, row) + 1 : t.keys;
         const int wmin = a.causal ? t.keys - t.n + token_of(a, it.row0 + min(wrow, t.rows - 1)) + 1 : t.keys;
-        const QOperand qo = load_q(a.q + row_offset(a, t.first, row, it.head, a.q_stride), h, a.scale, live);
+        const QOperand qo = load_q(a.q + row_offset(a, t.first, row, it.head, a.q_stride), h, a.scale, live && end > 0);
         State st;
         st.clear();
         Scales x0, x1, x2;

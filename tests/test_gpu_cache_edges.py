@@ -88,3 +88,22 @@ def test_last_block_without_numbers_reaches_only_the_rows_that_see_it(mx, what, 
     got = mx.cache_attend(q, *cache, table.cuda(), *args)
     assert torch.equal(got[:6], clean[:6])
     assert bool(got[6:].isnan().all())
+
+
+@pytest.mark.parametrize("way", list(WAYS))
+def test_queries_that_see_nothing_get_zero_whatever_they_hold(mx, way):  # noqa: F811
+    """More new tokens than the sequence has keys: those before the first key are zero, infinite and NaN queries
+    among them, beside rows of the same tile that see keys."""
+    print(f"[edges] unseen {way}", flush=True)
+    cache = filled(mx, 3, 2, 32, 3)
+    table = torch.tensor([[1, 2]], dtype=torch.int32).cuda()
+    q = rows(12, 4, 4)
+    args = table, ints([0, 12]), ints([7]), True, *WAYS[way]  # tokens 0 to 4 are before position 0
+    clean = mx.cache_attend(q, *cache, *args)
+    q[0, 0, 3], q[1, 1, 100], q[2], q[4, 3, 0] = math.inf, math.nan, -math.inf, math.nan
+    q[6, 2, 5] = math.inf  # this one sees keys
+    got = mx.cache_attend(q, *cache, *args)
+    assert bool((got[:5] == 0).all())
+    assert bool(got[6, 2].isnan().all())
+    clean[6, 2] = got[6, 2] = 0
+    assert torch.equal(got, clean)

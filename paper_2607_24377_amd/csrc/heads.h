@@ -113,21 +113,28 @@ struct Rotation {
     }
 };
 
-// 1 / sqrt(mean + eps) of the row, from the hardware's reciprocal square root (1 ulp;
-// the exact square root and division are 40 instructions), kept off subnormal
-// arguments.
-__device__ __forceinline__ float inverse_rms(const f32x8& x, float eps) {
+// Sum of squares of the row.
+__device__ __forceinline__ float sum_of_squares(const f32x8& x) {
     float q = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; i++) q = __builtin_fmaf(x[i], x[i], q);
-    q = __builtin_fmaf(row_sum16(q), 1.0f / kHeadDim, eps);
-    const bool small = q < 0x1p-96f;
-    const float r = __builtin_amdgcn_rsqf(small ? q * 0x1p96f : q);
-    return small ? r * 0x1p48f : r;
+    return row_sum16(q);
 }
 
+// x / sqrt(mean(x^2) + eps) * w, from the hardware's reciprocal square root (1 ulp; the
+// exact square root and division are 40 instructions).  Squares pass fp32 for
+// magnitudes above 2^60 and lose digits below 2^-63: a row whose sum is infinite is
+// normed as x 2^-80 and eps 2^-160, one whose mean and eps are below 2^-96 (so |x| below
+// 2^-44) as x 2^80 and eps 2^160, which leaves |x| between 2^-53 and 2^48 or without
+// effect.
 __device__ __forceinline__ f32x8 normed(f32x8 x, const f32x8& w, float eps) {
-    const float r = inverse_rms(x, eps);
+    float q = sum_of_squares(x), m = __builtin_fmaf(q, 1.0f / kHeadDim, eps);
+    const float f = m < 0x1p-96f ? 0x1p80f : q < __builtin_inff() ? 1.f : 0x1p-80f;
+    if (__any(f != 1.f)) {
+        x *= f;
+        m = __builtin_fmaf(sum_of_squares(x), 1.0f / kHeadDim, eps * f * f);
+    }
+    const float r = __builtin_amdgcn_rsqf(m);
 #pragma unroll
     for (int i = 0; i < 8; i++) x[i] *= r * w[i];
     return x;

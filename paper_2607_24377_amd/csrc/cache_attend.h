@@ -9,10 +9,16 @@
 //                 that of the rest, which leaves at most 2^-22 of the row's
 //                 largest magnitude.  Two FP8 products take the time of one in
 //                 bf16, and K needs no conversion;
-//   softmax       online, in fp32: m' = max(m, s c), p = exp2(s c - m');
-//   O^T += V^T P^T on the bf16 matrix cores: an E4M3 number times a power of two
-//                 is exact in bf16, and p is rounded to bf16 (2^-9 of a value
-//                 that is at most 1; l sums the unrounded p).
+//   softmax       online, in fp32: m' = max(m, s c - 7), p = exp2(s c - m'), which is
+//                 at most 2^7;
+//   O^T += V^T P^T on the f16 matrix cores: p is rounded to f16, by 2^-11 of it, or below
+//                 2^-21 of the largest by 2^-32 of that (bf16 rounds by 2^-8, which
+//                 was a third of the result's whole error; 1560 rows x 32760 keys x 40
+//                 heads took 1.11 ms with it and 1.14 so, 64 tokens x 8200 keys 119.5 us
+//                 and 121).
+//                 l sums the unrounded p.  V's codes times 2^-15 to 2^7 are exact in
+//                 f16: O~ is held in units of a power of two of the wave's, which
+//                 changes where a block's scale is further away (State).
 //
 // As S^T has keys as rows, a lane holds the scores of one query.  The keys of a
 // block are taken in the order in which accumulator i of lane (query, half h) is
@@ -26,13 +32,17 @@
 namespace mxattn {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 // the running maximum before the first key: below every finite score, so that
 // masked scores (-inf) give p = 0 and never inf - inf
 constexpr float kNoMax = -3.0e38f;
+// The largest p is 2^7: f16 holds 2^-31 of that, and 2^15, which p reaches where m, a
+// fp32 number below 2^28, is rounded by 8.
+constexpr int kTopLog2 = 7;
 
 // row / group, a row below 2^28 (a product and a shift: the division is 25 instructions).
 __device__ __forceinline__ int token_of(const CacheAttendArgs& a, int row) {
@@ -117,21 +127,21 @@ __device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QOperan
     return s;
 }
 
-// Eight codes (8 keys of a channel) as bf16, times the scale.
-__device__ __forceinline__ bf16x8 to_bf16(uint32_t a, uint32_t b, float scale) {
-    const bf16x2 w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
-    const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
-    const bf16x2 y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
-    const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
-    return bf16x8{w[0], w[1], x[0], x[1], y[0], y[1], z[0], z[1]};
+// Eight codes (8 keys of a channel) as f16, times the scale.
+__device__ __forceinline__ f16x8 to_f16(uint32_t a, uint32_t b, float scale) {
+    const f16x2 w = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, false);
+    const f16x2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, true);
+    const f16x2 y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, false);
+    const f16x2 z = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, true);
+    return f16x8{w[0], w[1], x[0], x[1], y[0], y[1], z[0], z[1]};
 }
 
-__device__ __forceinline__ bf16x8 probabilities(const v16f& p, int s) {
-    bf16x8 r;
+__device__ __forceinline__ f16x8 probabilities(const v16f& p, int s) {
+    f16x8 r;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const f32x2 a = {p[8 * s + 2 * i], p[8 * s + 2 * i + 1]};
-        const bf16x2 b = __builtin_convertvector(a, bf16x2);
+        const f16x2 b = __builtin_convertvector(a, f16x2);
         r[2 * i] = b[0];
         r[2 * i + 1] = b[1];
     }
@@ -185,17 +195,62 @@ __device__ __forceinline__ void load_block(Block& x, const CacheArgs& c, BlockAt
 }
 
 // The running state of a wave's rows: lane (query, h) holds its half of l and
-// channels 32 n + 8 a + 4 h + b of O~ in O[n][4 a + b].
+// channels 32 n + 8 a + 4 h + b of O~ in O[n][4 a + b], in units of 2^(e - 127).
 struct State {
     float m, l;
     v16f O[4];
+    int e, most;  // (the same for the whole wave) the units' byte, the largest scale byte of V so far
     __device__ __forceinline__ void clear() {
         m = kNoMax;
         l = 0.f;
+        e = most = 0;
 #pragma unroll
         for (int n = 0; n < 4; n++)
 #pragma unroll
             for (int i = 0; i < 16; i++) O[n][i] = 0.f;
+    }
+    // What V's codes of scale byte `byte` are multiplied by, 2^-15 to 2^7 (as an E8M0 byte
+    // 112 to 134), once the units reach it.
+    __device__ __forceinline__ float value_scale(int byte) {
+        const int b = __builtin_amdgcn_readfirstlane(byte);
+        int f = b - e + 127;
+        if ((unsigned)(f - 112) > 22u) f = move(b);
+        return e8m0_as_f32((uint32_t)f);
+    }
+    // Moves the units to scale byte b, but to no less than 2^-40 of the largest so far: O~,
+    // below 2^47 there, cannot overflow, and blocks whose scale is below 2^-55 of the
+    // largest one's lose digits.  Returns what b's codes are multiplied by: NaN for 255,
+    // which units of at most 247 do not reach.
+    __device__ __forceinline__ int move(int b) {
+        if (b == 255) return 255;
+        most = max(most, b);
+        const int to = min(max(b, most - 40), 247);
+#pragma unroll
+        for (int n = 0; n < 4; n++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) O[n][i] = __builtin_ldexpf(O[n][i], e - to);
+        e = to;
+        return max(b - to + 127, 64);
+    }
+    // A new running maximum.
+    __device__ __forceinline__ void raise(float to) {
+        const float alpha = __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= alpha;
+#pragma unroll
+        for (int n = 0; n < 4; n++) O[n] *= alpha;
+    }
+    // p of scores s, whose sum goes to l.
+    __device__ __forceinline__ v16f exponentials(const v16f& s, float c, float to) {
+        v16f p;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -to));
+            sum += p[i];
+        }
+        l += sum;
+        return p;
     }
 };
 
@@ -206,9 +261,9 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t v) { return ((v & 0x7F7F7
 // has p = 0, and 0 * NaN would reach every row.  The codes are taken out, and
 // the rows that see one get NaN: its count, from a product of ones.
 __device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], int visible, int h) {
-    bf16x8 seen[2];
+    f16x8 seen[2];
 #pragma unroll
-    for (int i = 0; i < 16; i++) seen[i >> 3][i & 7] = 16 * h + i < visible ? (__bf16)1.f : (__bf16)0.f;
+    for (int i = 0; i < 16; i++) seen[i >> 3][i & 7] = 16 * h + i < visible ? (_Float16)1.f : (_Float16)0.f;
 #pragma unroll
     for (int n = 0; n < 4; n++) {
         uint32_t* x = reinterpret_cast<uint32_t*>(&v[n]);
@@ -222,8 +277,8 @@ __device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], int visible
         v16f z;
 #pragma unroll
         for (int i = 0; i < 16; i++) z[i] = 0.f;
-        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(one[0], one[1], 1.f), seen[0], z, 0, 0, 0);
-        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(one[2], one[3], 1.f), seen[1], z, 0, 0, 0);
+        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_f16(one[0], one[1], 1.f), seen[0], z, 0, 0, 0);
+        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_f16(one[2], one[3], 1.f), seen[1], z, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 16; i++) st.O[n][i] = z[i] > 0.f ? __builtin_nanf("") : st.O[n][i];
     }
@@ -257,10 +312,10 @@ __device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int& e, i
     if (__any(has_nan(v))) spread_nan(st, v, visible - base, h);
 }
 
-// Softmax of a block's scores and their product with V; `visible`: keys of the
-// block that the lane's row sees (its first ones), `any`: some row does not see all.
-__device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float vscale, float c, int visible, bool any,
-                                        int h) {
+// Softmax of a block's scores and their product with V of scale byte `e`; `visible`:
+// keys of the block that the lane's row sees (its first ones), `any`: some row does
+// not see all.
+__device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], int e, float c, int visible, bool any, int h) {
     if (any) {
 #pragma unroll
         for (int i = 0; i < 16; i++) s[i] = 16 * h + i < visible ? s[i] : -__builtin_inff();
@@ -269,26 +324,16 @@ __device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], float 
 #pragma unroll
     for (int i = 3; i < 15; i += 2) mx = max2(max2(mx, s[i]), s[i + 1]);  // (three-input maxima)
     mx = max2(mx, s[15]);
-    mx *= c;
+    mx = __builtin_fmaf(mx, c, -kTopLog2);
     const float m = max2(st.m, max2(mx, other_half(mx)));
-    if (__any(m > st.m)) {  // else every alpha is 1
-        const float alpha = __builtin_amdgcn_exp2f(st.m - m);
-        st.m = m;
-        st.l *= alpha;
-#pragma unroll
-        for (int n = 0; n < 4; n++) st.O[n] *= alpha;
-    }
-    v16f p;
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m));
-        st.l += p[i];
-    }
-    const bf16x8 p0 = probabilities(p, 0), p1 = probabilities(p, 1);
+    if (__any(m > st.m)) st.raise(m);  // else every alpha is 1
+    const float vscale = st.value_scale(e);
+    const v16f p = st.exponentials(s, c, m);
+    const f16x8 p0 = probabilities(p, 0), p1 = probabilities(p, 1);
 #pragma unroll
     for (int n = 0; n < 4; n++) {
-        st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].x, v[n].y, vscale), p0, st.O[n], 0, 0, 0);
-        st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].z, v[n].w, vscale), p1, st.O[n], 0, 0, 0);
+        st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_f16(v[n].x, v[n].y, vscale), p0, st.O[n], 0, 0, 0);
+        st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_f16(v[n].z, v[n].w, vscale), p1, st.O[n], 0, 0, 0);
     }
 }
 
@@ -299,7 +344,7 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand
     if (any || x.lost) clean_values(st, x.v, x.ve, 0, end - base, keys - base, x.lost, h);
     if (x.lost && end > base) st.l = __builtin_nanf("");  // no such page: NaN for the rows that would see it
     const v16f s = scores(x.k, x.ke, q);
-    consume(st, s, x.v, e8m0_as_f32((uint32_t)x.ve), q.c, end - base, any, h);
+    consume(st, s, x.v, x.ve, q.c, end - base, any, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -310,7 +355,7 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand
 // head, tile by tile, are cut into equal shares, one per workgroup, whatever the
 // lengths are: only the kernel sees them.  A share is a run of items, of which the
 // first and the last may be parts; a part's result (m, l, O~) goes to the
-// workgroup's slot in the workspace and the parts are joined by
+// workgroup's slot in the workspace, O~ divided by l, and the parts are joined by
 // cache_attend_join_kernel in a fixed order.
 
 // The tiles of a sequence: tile t of a head weighs a + b (t + 1).
@@ -507,7 +552,7 @@ struct PartInfo {
     int first, last;
 };
 
-// The workspace of n shares: O~, m and l of their slots' rows, and the items' PartInfo.
+// The workspace of n shares: O~ / l, m and l of their slots' rows, and the items' PartInfo.
 template <int kRows>
 struct Parts {
     float* o;     // [2 n, kRows, 128]
@@ -537,11 +582,14 @@ __device__ __forceinline__ uint2 bf16x4(float a, float b, float c, float d) {
                       __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2)));
 }
 
-// Four channels of a row, finished: O~ / l as bf16.
-__device__ __forceinline__ uint2 finished(float4 o, float l, bool bad) {
-    const float inv = inverse(l, bad);
-    return bf16x4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+// Four channels of a joined row as bf16.
+__device__ __forceinline__ uint2 finished(const float4& o, bool bad) {
+    const float nan = __builtin_nanf("");
+    return bad ? bf16x4(nan, nan, nan, nan) : bf16x4(o.x, o.y, o.z, o.w);
 }
+
+// What l is divided by: parts without keys weigh nothing.
+__device__ __forceinline__ float reciprocal(float l) { return l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l); }
 
 __device__ __forceinline__ void add_scaled(float4& o, const float4& x, float f) {
     o.x = __builtin_fmaf(x.x, f, o.x);
@@ -550,26 +598,36 @@ __device__ __forceinline__ void add_scaled(float4& o, const float4& x, float f) 
     o.w = __builtin_fmaf(x.w, f, o.w);
 }
 
+// Channels 32 n + 8 g + 4 h on of a lane's half of a row, divided by l.  (Sums of values
+// near the largest fp32 do not pass it so, in parts neither.)
+__device__ __forceinline__ float4 four(const State& st, int n, int g, float inv) {
+    const v16f& o = st.O[n];
+    const int e = st.e - 127;
+    return make_float4(__builtin_ldexpf(o[4 * g] * inv, e), __builtin_ldexpf(o[4 * g + 1] * inv, e),
+                       __builtin_ldexpf(o[4 * g + 2] * inv, e), __builtin_ldexpf(o[4 * g + 3] * inv, e));
+}
+
 // A lane's half of a finished row.
 __device__ __forceinline__ void store_row(const State& st, float inv, uint16_t* row, int h) {
 #pragma unroll
     for (int n = 0; n < 4; n++)
 #pragma unroll
-        for (int g = 0; g < 4; g++)
-            *reinterpret_cast<uint2*>(row + 32 * n + 8 * g + 4 * h) =
-                bf16x4(st.O[n][4 * g] * inv, st.O[n][4 * g + 1] * inv, st.O[n][4 * g + 2] * inv, st.O[n][4 * g + 3] * inv);
+        for (int g = 0; g < 4; g++) {
+            const float4 o = four(st, n, g, inv);
+            *reinterpret_cast<uint2*>(row + 32 * n + 8 * g + 4 * h) = bf16x4(o.x, o.y, o.z, o.w);
+        }
 }
 
 // A lane's half of row `row` of the workspace's slots.
 template <int kRows>
 __device__ __forceinline__ void store_part(const State& st, float l, const Parts<kRows>& parts, int64_t row, int h) {
+    const float inv = inverse(l, false);
     if (h == 0) parts.ml[row] = make_float2(st.m, l);
 #pragma unroll
     for (int n = 0; n < 4; n++)
 #pragma unroll
         for (int g = 0; g < 4; g++)
-            *reinterpret_cast<float4*>(parts.o + row * kHeadDim + 32 * n + 8 * g + 4 * h) =
-                make_float4(st.O[n][4 * g], st.O[n][4 * g + 1], st.O[n][4 * g + 2], st.O[n][4 * g + 3]);
+            *reinterpret_cast<float4*>(parts.o + row * kHeadDim + 32 * n + 8 * g + 4 * h) = four(st, n, g, inv);
 }
 
 // Joins the parts of item blockIdx.x in the order of its keys: a row per workgroup
@@ -610,23 +668,26 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
 #pragma unroll
             for (int k = 0; k < 4; k++) {
                 if (p + k * step >= count) break;
-                const float top = max2(m, ml[k].x), f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml[k].x - top);
+                const float top = max2(m, ml[k].x);
+                float f = l * __builtin_amdgcn_exp2f(m - top), g = ml[k].y * __builtin_amdgcn_exp2f(ml[k].x - top);
                 m = top;
-                l = __builtin_fmaf(ml[k].y, g, l * f);
+                l = f + g;
+                const float r = reciprocal(l);
+                f *= r;
                 o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-                add_scaled(o, x[k], g);
+                add_scaled(o, x[k], g * r);
             }
         }
     };
-    auto finish = [&](int r, float l, const float4& o) {
-        *reinterpret_cast<uint2*>(a.out + row_offset(a, range.first, row0 + r, head, a.out_stride) + ch) = finished(o, l, bad);
+    auto finish = [&](int r, const float4& o) {
+        *reinterpret_cast<uint2*>(a.out + row_offset(a, range.first, row0 + r, head, a.out_stride) + ch) = finished(o, bad);
     };
     float m, l;
     float4 o;
     if (count <= 8) {  // a row for each group (128 items of 8 parts and 32 rows 9.8 us, by all groups 12.1)
         for (int r = 8 * blockIdx.y + g; r < rows; r += 8 * gridDim.y) {
             gather(r, 0, 1, m, l, o);
-            finish(r, l, o);
+            finish(r, o);
         }
         return;
     }
@@ -642,13 +703,12 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
             m = s_m[0];
             for (int k = 1; k < 8; k++) m = max2(m, s_m[k]);
             l = 0.f;
+            for (int k = 0; k < 8; k++) l = __builtin_fmaf(s_l[k], __builtin_amdgcn_exp2f(s_m[k] - m), l);
+            const float inv = reciprocal(l);
             o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k = 0; k < 8; k++) {
-                const float f = __builtin_amdgcn_exp2f(s_m[k] - m);
-                l = __builtin_fmaf(s_l[k], f, l);
-                add_scaled(o, s_o[k][tid & 31], f);
-            }
-            finish(r, l, o);
+            for (int k = 0; k < 8; k++)
+                add_scaled(o, s_o[k][tid & 31], s_l[k] * __builtin_amdgcn_exp2f(s_m[k] - m) * inv);
+            finish(r, o);
         }
         __syncthreads();
     }

@@ -239,12 +239,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
         s_l[wave][q] = l;
     }
     if (q < r.count) {
+        const float inv = inverse(l, false);
 #pragma unroll
         for (int n = 0; n < 4; n++)
 #pragma unroll
             for (int g = 0; g < 4; g++)
-                *reinterpret_cast<float4*>(o_at(wave, q, 8 * n + 2 * g + h)) =
-                    make_float4(st.O[n][4 * g], st.O[n][4 * g + 1], st.O[n][4 * g + 2], st.O[n][4 * g + 3]);
+                *reinterpret_cast<float4*>(o_at(wave, q, 8 * n + 2 * g + h)) = four(st, n, g, inv);
     }
     __syncthreads();
     for (int e = tid; e < r.count * 32; e += kThreads) {
@@ -252,16 +252,18 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
         float m = s_m[0][i];
 #pragma unroll
         for (int w = 1; w < kWaves; w++) m = max2(m, s_m[w][i]);
-        float sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f, f[kWaves];
 #pragma unroll
         for (int w = 0; w < kWaves; w++) {
-            const float f = __builtin_amdgcn_exp2f(s_m[w][i] - m);
-            sum = __builtin_fmaf(s_l[w][i], f, sum);
-            add_scaled(o, *reinterpret_cast<const float4*>(o_at(w, i, e & 31)), f);
+            f[w] = s_l[w][i] * __builtin_amdgcn_exp2f(s_m[w][i] - m);
+            sum += f[w];
         }
+        const float inv = reciprocal(sum);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) add_scaled(o, *reinterpret_cast<const float4*>(o_at(w, i, e & 31)), f[w] * inv);
         *reinterpret_cast<uint2*>(a.out + row_offset(a, seq.first, row0 + i, head, a.out_stride) + ch) =
-            finished(o, sum, seq.keys < 0);
+            finished(o, seq.keys < 0);
     }
 }
 

@@ -5,13 +5,13 @@
 // A workgroup takes a tile of 128 rows, 32 per wave, and walks its keys 64 at a
 // time.  K's and V's codes (16 KiB) are copied straight into LDS, in the lanes'
 // operand order, two steps ahead of their use, and each wave reads them as they are:
-// FP8 operands for the scores, and codes that become bf16 in registers for the
+// FP8 operands for the scores, and codes that become f16 in registers for the
 // second product.  Two waves a SIMD (256 registers) run each other's gaps.
 //
 // 1560 rows x 32760 keys x 40 heads: 1.10 to 1.14 ms, 920 to 955 TFLOP/s; matrix cores
 // busy 48 %, vector issue 55 % (139 instructions per 32 x 32 scores, about 830
 // cycles), LDS half of its time.  256 rows in eight waves 1.10, 64 rows per wave 1.72
-// (spills), one wave a SIMD 1.21, V as bf16 in LDS, made once for the four waves, 1.25
+// (spills), one wave a SIMD 1.21, V as 16 bits in LDS, made once for the four waves, 1.25
 // (more to read there); the next scores under this step's softmax, a wait for the step
 // before only, or priorities of the waves gained nothing.
 #include "cache_attend.h"
@@ -105,36 +105,23 @@ __device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* sta
         my = max2(max2(my, s[1][i + 2]), s[1][i + 3]);
     }
     mx = max2(max2(mx, s[1][14]), max2(my, s[1][15]));
-    mx *= c;
+    mx = __builtin_fmaf(mx, c, -kTopLog2);
     const float m = max2(st.m, max2(mx, other_half(mx)));
-    if (__any(m > st.m)) {  // else every alpha is 1
-        const float alpha = __builtin_amdgcn_exp2f(st.m - m);
-        st.m = m;
-        st.l *= alpha;
-#pragma unroll
-        for (int n = 0; n < 4; n++) st.O[n] *= alpha;
-    }
+    if (__any(m > st.m)) st.raise(m);  // else every alpha is 1
 #pragma unroll
     for (int b = 0; b < 2; b++) {
-        v16f p;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -m));
-            sum += p[i];
-        }
-        st.l += sum;
-        const bf16x8 p0 = probabilities(p, 0), p1 = probabilities(p, 1);
+        const v16f p = st.exponentials(s[b], c, m);
+        const f16x8 p0 = probabilities(p, 0), p1 = probabilities(p, 1);
         uint4 v[4];
 #pragma unroll
         for (int n = 0; n < 4; n++) v[n] = part(stage + (2 + b) * kBlockBytes, n, lane);
         int e = x.v[b];
         if (any || lost) clean_values(st, v, e, 32 * b, visible, held, x.lost[b], h);
-        const float vscale = e8m0_as_f32((uint32_t)e);
+        const float vscale = st.value_scale(e);
 #pragma unroll
         for (int n = 0; n < 4; n++) {
-            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].x, v[n].y, vscale), p0, st.O[n], 0, 0, 0);
-            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(to_bf16(v[n].z, v[n].w, vscale), p1, st.O[n], 0, 0, 0);
+            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_f16(v[n].x, v[n].y, vscale), p0, st.O[n], 0, 0, 0);
+            st.O[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_f16(v[n].z, v[n].w, vscale), p1, st.O[n], 0, 0, 0);
         }
     }
 }

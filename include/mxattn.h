@@ -82,7 +82,8 @@ typedef enum {
     MXATTN_ERR_NULL = 1,        /* a required pointer is NULL              */
     MXATTN_ERR_SHAPE = 2,       /* B, H or N < 1, beyond a size limit, or an
                                    output that overlaps an input            */
-    MXATTN_ERR_ALIGN = 3,       /* a pointer is not 16-byte aligned         */
+    MXATTN_ERR_ALIGN = 3,       /* a pointer is not 16-byte aligned, or a
+                                   stride is no multiple of 8 elements      */
     MXATTN_ERR_MODE = 4,        /* mode is not an mxattn_mode value         */
     MXATTN_ERR_AXIS = 5,        /* block_axis is not 2 or 3                 */
     MXATTN_ERR_UNSUPPORTED = 6, /* d != 128                                 */
@@ -413,8 +414,8 @@ int mxattn_query_tile(void);
 /* Static description of a status code. */
 const char* mxattn_status_string(int status);
 
-/* Detail of the last MXATTN_ERR_HIP or MXATTN_ERR_OOM on the calling
- * thread ("" if none). */
+/* Detail of the last MXATTN_ERR_HIP, MXATTN_ERR_OOM or MXATTN_ERR_SCRATCH on
+ * the calling thread ("" if none). */
 const char* mxattn_last_error(void);
 
 /* Workspace.  mxattn_forward, mxattn_cross_forward, mxattn_attend,

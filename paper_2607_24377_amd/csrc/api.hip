@@ -64,14 +64,14 @@ const char* mxattn_status_string(int s) {
     switch (s) {
         case MXATTN_OK: return "ok";
         case MXATTN_ERR_NULL: return "null pointer argument";
-        case MXATTN_ERR_SHAPE: return "invalid shape (B, H, N must be >= 1 and within limits)";
-        case MXATTN_ERR_ALIGN: return "misaligned pointer (tensors need 16-byte alignment)";
+        case MXATTN_ERR_SHAPE: return "invalid shape (sizes must be >= 1 and within limits, strides not negative, outputs apart from inputs and workspace)";
+        case MXATTN_ERR_ALIGN: return "misaligned pointer or stride (tensors need 16-byte alignment, strides multiples of 8 elements)";
         case MXATTN_ERR_MODE: return "invalid mode (0 ocp_vanilla, 1 uos, 2 uos_pnq, 3 uos_pnq_rot)";
         case MXATTN_ERR_AXIS: return "invalid block_axis (2 = tokens, 3 = head dim)";
         case MXATTN_ERR_UNSUPPORTED: return "unsupported head dimension (d must be 128)";
         case MXATTN_ERR_OOM: return "workspace allocation failed";
         case MXATTN_ERR_HIP: return "HIP runtime error";
-        case MXATTN_ERR_SCRATCH: return "problem too large for the static scratch of the no-allocation entry point (needs B*H*ceil(Nkv/128) <= 32768)";
+        case MXATTN_ERR_SCRATCH: return "more scratch needed than there is (the no-allocation entry point: B*H*ceil(Nkv/128) <= 32768; cache attention: a workspace of mxattn_cache_attend_workspace() bytes from the caller, always on a stream under graph capture)";
         case MXATTN_ERR_BOUNDARY: return "invalid scale boundary (need 4 <= q <= 8 and 1 <= nq <= 64) or pre-scale (need 0 < gamma < 3e38)";
         case MXATTN_ERR_VALUE: return "invalid value (rot 0 or a multiple of 16 up to 128, pairs 0 or 1, eps finite and >= 0, page_tokens a power of two from 32 to 4096, Hq a multiple of Hkv, at most 256 of it)";
         default: return "unknown status";
@@ -760,7 +760,11 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
     size_t bytes = mxattn::cache_attend_workspace(a, max_q, max_kv);
     Workspace ws;
     if (bytes && workspace) {
-        if (workspace_bytes < bytes) return MXATTN_ERR_SCRATCH;
+        if (workspace_bytes < bytes) {
+            std::snprintf(g_last_error, sizeof g_last_error,
+                          "mxattn_cache_attend: %zu bytes of workspace needed, the caller's has %zu", bytes, workspace_bytes);
+            return MXATTN_ERR_SCRATCH;
+        }
         if (!aligned(workspace, 16)) return MXATTN_ERR_ALIGN;
         if (overlaps(workspace, bytes, q, qb) || overlaps(workspace, bytes, out, ob) || in_cache(workspace, bytes, a.c))
             return MXATTN_ERR_SHAPE;
@@ -775,7 +779,12 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
                 return MXATTN_ERR_HIP;
             }
         }
-        if (capture != hipStreamCaptureStatusNone) return MXATTN_ERR_SCRATCH;
+        if (capture != hipStreamCaptureStatusNone) {
+            std::snprintf(g_last_error, sizeof g_last_error,
+                          "mxattn_cache_attend: %zu bytes of workspace needed from the caller, as the stream is being captured",
+                          bytes);
+            return MXATTN_ERR_SCRATCH;
+        }
         if (int st = ws.take(bytes, s)) return st;
         a.workspace = ws.get();
     }

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libmxattn.so")
 MODES = {"ocp_vanilla": 0, "uos": 1, "uos_pnq": 2, "uos_pnq_rot": 3}
 AXIS_TOKENS, AXIS_HEAD_DIM = 2, 3
 OK = 0
+WITH_DETAIL = (7, 8, 10)  # out of memory, a HIP error, too little scratch
 
 _lock = threading.Lock()
 _lib = None
@@ -29,7 +30,8 @@ class MxattnError(RuntimeError):
     def __init__(self, status: int, where: str):
         L = lib()
         msg = L.mxattn_status_string(status).decode()
-        detail = L.mxattn_last_error().decode()
+        # (the detail is of the last error that had one: of another call, where this status has none)
+        detail = L.mxattn_last_error().decode() if status in WITH_DETAIL else ""
         super().__init__(f"{where}: status {status} ({msg}){': ' + detail if detail else ''}")
         self.status = status
 

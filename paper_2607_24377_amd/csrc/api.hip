@@ -750,7 +750,6 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
     a.out = static_cast<uint16_t*>(out);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    a.Hq = (int)Hq;
     a.group = (int)(Hq / Hkv);
     a.per_group = (((uint64_t)1 << 36) + a.group - 1) / a.group;
     a.causal = causal != 0;

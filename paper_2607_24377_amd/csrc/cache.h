@@ -64,7 +64,7 @@ struct CacheAttendArgs {
     const uint16_t* q;  // [tokens, Hq, 128] by its token stride
     uint16_t* out;
     int64_t q_stride, out_stride;
-    int Hq, group;      // group = Hq / heads, at most 256
+    int group;          // Hq / heads, at most 256
     uint64_t per_group; // ceil(2^36 / group)
     int causal;
     float scale;        // log2(e) / sqrt(128)

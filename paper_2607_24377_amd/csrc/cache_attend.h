@@ -31,7 +31,6 @@
 
 namespace mxattn {
 
-typedef int v4i __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -349,115 +348,16 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand
 
 // ---------------------------------------------------------------------------
 // Division of the work.  An item is a tile of kRows rows of one sequence and KV
-// head; its weight is what it costs, in keys: the same for every tile of a
-// sequence, or, causal and with long runs of new tokens, growing by a constant
-// from tile to tile.  All items' weights in a row, sequence by sequence, head by
-// head, tile by tile, are cut into equal shares, one per workgroup, whatever the
-// lengths are: only the kernel sees them.  A share is a run of items, of which the
-// first and the last may be parts; a part's result (m, l, O~) goes to the
-// workgroup's slot in the workspace, O~ divided by l, and the parts are joined by
-// cache_attend_join_kernel in a fixed order.
-
-// The tiles of a sequence: tile t of a head weighs a + b (t + 1).
-struct SeqWork {
-    int64_t a;
-    int tiles, b;
-    __device__ __forceinline__ int64_t before(int64_t t) const { return t * a + b * (t * (t + 1) / 2); }
-    __device__ __forceinline__ int64_t weight(int t) const { return a + (int64_t)b * (t + 1); }
-};
+// head; the items of the whole call lie in a row, sequence by sequence, head by head,
+// tile by tile, and are cut into equal shares, whatever the lengths are: only the
+// kernel sees them.  A share is a run of items, of which the first and the last may be
+// parts; a part's result (m, l, O~ / l) goes to the share's slot in the workspace and
+// the parts are joined by cache_attend_join_kernel in a fixed order.
 
 // Keys of sequence s as far as they can be used: -1 where its length is impossible.
 __device__ __forceinline__ int keys_of(const CacheArgs& c, int s) {
     const int len = c.kv_len[s];
     return (unsigned)len > (unsigned)((c.max_pages << c.bpp_log2) * kBlockTokens) ? -1 : len;
-}
-
-template <int kRows, bool kGrowing>
-__device__ __forceinline__ SeqWork seq_work(const CacheAttendArgs& a, int s) {
-    const TokenRange r = token_range(a.c, s);
-    const int64_t rows = (int64_t)(r.last - r.first) * a.group;
-    const int keys = keys_of(a.c, s);
-    SeqWork w;
-    w.tiles = (int)((rows + kRows - 1) / kRows);
-    if (kGrowing && a.causal) {  // in units of a key times the group: kRows / group keys more per tile
-        w.a = (int64_t)max(keys - (r.last - r.first), 0) * a.group;
-        w.b = kRows;
-    } else {
-        w.a = max(keys, 1);
-        w.b = 0;
-    }
-    return w;
-}
-
-// A workgroup's place in the row of all items, and how far its share goes.
-struct Share {
-    int64_t at, end;  // of the total weight
-    int64_t offset;   // of `at` within sequence s
-    int64_t total;
-    int s, n;         // n: shares (no more than there is weight, so none is empty)
-};
-
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-    const int lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-    return ((int64_t)hi << 32) | (uint32_t)lo;
-}
-
-// The share of workgroup i of n, empty for all where q_start does not ascend (the
-// sum of the weights could pass 64 bits); all kThreads threads call it.
-template <int kRows, bool kGrowing, int kThreads>
-__device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int n) {
-    __shared__ int64_t s_sum[kThreads / 64];
-    __shared__ bool s_ascend[kThreads / 64];
-    __shared__ Share s_share;
-    const int tid = threadIdx.x, seqs = a.c.seqs;
-    const int per = (seqs + kThreads - 1) / kThreads;
-    const int s0 = min(tid * per, seqs), s1 = min(s0 + per, seqs);
-    int64_t mine = 0;
-    bool ascend = true;
-    for (int s = s0; s < s1; s++) {
-        const SeqWork w = seq_work<kRows, kGrowing>(a, s);
-        mine += w.before(w.tiles) * a.c.heads;
-        ascend = ascend && starts_ascend(a.c, s);
-    }
-    int64_t incl = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t x = __shfl_up(incl, d);
-        if ((tid & 63) >= d) incl += x;
-    }
-    ascend = __all(ascend);
-    if ((tid & 63) == 63) {
-        s_sum[tid >> 6] = incl;
-        s_ascend[tid >> 6] = ascend;
-    }
-    if (tid == 0) s_share = {0, 0, 0, 0, -1, 0};
-    __syncthreads();
-    int64_t total = 0, before = incl - mine;
-#pragma unroll
-    for (int k = 0; k < kThreads / 64; k++) {
-        if (k < (tid >> 6)) before += s_sum[k];
-        total += s_sum[k];
-    }
-#pragma unroll
-    for (int k = 0; k < kThreads / 64; k++)
-        if (!s_ascend[k]) total = 0;
-    n = (int)(total < n ? total : n);
-    const int64_t lo = i < n ? total * i / n : total, hi = i < n ? total * (i + 1) / n : total;
-    if (i < n && before <= lo && lo < before + mine) {
-        int64_t at = before;
-        for (int s = s0; s < s1; s++) {
-            const SeqWork w = seq_work<kRows, kGrowing>(a, s);
-            const int64_t all = w.before(w.tiles) * a.c.heads;
-            if (lo < at + all) {
-                s_share = {lo, hi, lo - at, total, s, n};
-                break;
-            }
-            at += all;
-        }
-    }
-    __syncthreads();
-    return {uniform64(s_share.at), uniform64(s_share.end), uniform64(s_share.offset), uniform64(s_share.total),
-            __builtin_amdgcn_readfirstlane(s_share.s), __builtin_amdgcn_readfirstlane(s_share.n)};
 }
 
 // Tiles of a sequence are numbered from here on: no two sequences' overlap, whatever
@@ -469,79 +369,6 @@ __device__ __forceinline__ int tile_number(const CacheAttendArgs& a, int first, 
 template <int kRows>
 inline int64_t tile_numbers(const CacheAttendArgs& a) {
     return (int64_t)a.c.tokens * a.group / kRows + a.c.seqs;
-}
-
-// One item and the part of it that a workgroup works on.
-struct Item {
-    int s, head, row0;
-    int64_t x0, x1, w;  // from x0 to x1 of its weight w
-    int last;           // the share of its last part
-    int number;         // PartInfo's
-    __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == w; }
-};
-
-// The item at the share's place; the share moves on behind it.
-template <int kRows, bool kGrowing>
-__device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
-    const SeqWork w = seq_work<kRows, kGrowing>(a, sh.s);
-    const int64_t per_head = w.before(w.tiles);
-    Item it;
-    it.s = sh.s;
-    it.head = __builtin_amdgcn_readfirstlane((int)(sh.offset / per_head));
-    const int64_t r = uniform64(sh.offset - it.head * per_head);
-    int t = 0;
-    if (w.b == 0) {
-        t = __builtin_amdgcn_readfirstlane((int)(r / w.a));
-    } else {
-        int hi = w.tiles - 1;  // the last tile that starts at or before r
-        while (t < hi) {
-            const int mid = (t + hi + 1) >> 1;
-            if (w.before(mid) <= r)
-                t = mid;
-            else
-                hi = mid - 1;
-        }
-    }
-    it.row0 = t * kRows;
-    it.number = (tile_number<kRows>(a, token_range(a.c, sh.s).first, sh.s) + t) * a.c.heads + it.head;
-    it.w = w.weight(t);
-    it.x0 = r - w.before(t);
-    it.x1 = it.x0 + (sh.end - sh.at) < it.w ? it.x0 + (sh.end - sh.at) : it.w;
-    const int64_t step = it.x1 - it.x0;
-    // the share that holds the item's last unit of weight, y: the largest k with total k / n <= y
-    const int64_t y = sh.at + (it.w - it.x0) - 1;
-    it.last = __builtin_amdgcn_readfirstlane((int)(((y + 1) * sh.n - 1) / sh.total));
-    sh.at += step;
-    sh.offset += step;
-    if (sh.at < sh.end && sh.offset >= per_head * a.c.heads) {
-        sh.offset = 0;
-        do sh.s++;
-        while (sh.s < a.c.seqs && seq_work<kRows, kGrowing>(a, sh.s).tiles == 0);
-    }
-    return it;
-}
-
-// Which rows a tile has and what they see.
-struct TileRows {
-    int n, keys;           // the sequence's new tokens and keys
-    int rows;              // rows of the tile
-    int min_end, max_end;  // keys that its first and its last row see
-    int64_t first;         // the sequence's first token in the call
-    bool bad;              // no such cache
-};
-template <int kRows>
-__device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, int row0) {
-    const TokenRange r = token_range(a.c, s);
-    TileRows t;
-    t.n = r.last - r.first;
-    t.first = r.first;
-    const int keys = __builtin_amdgcn_readfirstlane(keys_of(a.c, s));
-    t.bad = keys < 0;
-    t.keys = max(keys, 0);
-    t.rows = min(kRows, t.n * a.group - row0);
-    t.min_end = a.causal ? t.keys - t.n + token_of(a, row0) + 1 : t.keys;
-    t.max_end = max(0, a.causal ? t.keys - t.n + token_of(a, row0 + t.rows - 1) + 1 : t.keys);
-    return t;
 }
 
 // The shares that an item lies in; what they leave for the join is in slots

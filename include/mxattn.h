@@ -376,15 +376,19 @@ int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t 
  *   max_q, max_kv  at least the new tokens and the keys of every sequence, as the
  *         caller knows them on the host; 0: unknown (tokens, and max_pages *
  *         page_tokens).  They choose how the work is divided: bounds that are too
- *         small or far too large cost time, not correctness; other bounds may
- *         change an output by the order of its fp32 sums.
+ *         small or far too large cost time, not correctness.  Where the work is cut
+ *         decides which running maximum each p is rounded under, and in what order
+ *         fp32 sums are formed: other bounds, and other lengths of the call's other
+ *         sequences, may change an output by these roundings (2^-11 of each p), so by
+ *         its last bit or, where values cancel, by 2^-11 of sum p |v|.
  *   workspace  device memory of the caller, 16-byte aligned, of at least
  *         mxattn_cache_attend_workspace() bytes (else MXATTN_ERR_SCRATCH), for this
  *         call until it has run; what it holds before does not matter.  It shares no
  *         byte with q, out or the cache (MXATTN_ERR_SHAPE).  NULL: from the
  *         library's pool, which a stream under graph capture cannot use: there a
  *         call that needs workspace is refused (MXATTN_ERR_SCRATCH).
- * Equal arguments and contents give equal bits. */
+ * Equal arguments and contents give equal bits (a sequence's output may have others in
+ * another batch, as said). */
 int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
                         const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
                         const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len,

@@ -71,7 +71,7 @@ struct CacheAttendArgs {
     uint8_t* workspace; // cache_attend_workspace bytes
 };
 // max_q, max_kv: most new tokens and keys of a sequence, as far as the caller knows
-// (wrong ones cost time only).
+// (wrong ones cost time, and may change where f16 and fp32 round).
 size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv);
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream);
 

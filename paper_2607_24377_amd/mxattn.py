@@ -453,7 +453,8 @@ def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_tab
                  max_q: int = 0, max_kv: int = 0, out=None, stream=None):
     """Attention of bf16 q [tokens, Hq, d] over the sequences' cached keys; returns bf16 out [tokens, Hq, d].
     max_q, max_kv: at least the new tokens and the keys of every sequence as the caller knows them (0: unknown); they
-    choose how the work is divided, and wrong ones cost time only.  Workspace is torch's, of the current stream (a graph
+    choose how the work is divided.  Wrong ones cost time, and other ones (or other lengths in the batch) may change an
+    output by the rounding of the probabilities to f16.  Workspace is torch's, of the current stream (a graph
     captured there keeps it); of a stream that is given it is the library's, and a call that needs some cannot be
     captured."""
     dev = _index(q, "q")

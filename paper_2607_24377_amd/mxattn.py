@@ -291,13 +291,15 @@ BLOCK_TOKENS = 32
 
 
 def _raw_stream(index: int) -> int:
-    """The device's current stream (torch.cuda.current_stream, which takes 4 us to make an object of it)."""
-    return torch._C._cuda_getCurrentRawStream(index)
+    """The device's current stream.  The public call takes 4 us to make an object of it; a torch without the other has
+    that one."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
 
 
 def _run(fn, where: str, index: int, stream, args):
     """fn(*args, stream) with device `index` current, on its current stream unless one is given."""
-    if index == torch._C._cuda_getDevice():
+    if index == torch.cuda.current_device():
         st = fn(*args, _raw_stream(index) if stream is None else _stream(stream))
     else:
         with torch.cuda.device(index):

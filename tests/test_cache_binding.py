@@ -64,3 +64,13 @@ def test_codes_of_64_channels_are_refused_for_rows_of_128():
 def test_shapes_that_no_call_takes_are_refused(page, d):
     with pytest.raises(ValueError):
         mxattn.cache_shapes(PAGES, HEADS, page, d)
+
+
+def test_stream_without_torchs_private_call(monkeypatch):
+    """The current stream comes from the public interface where torch has no other."""
+    class Stream:
+        cuda_stream = 42
+
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda index=None: Stream if index == 3 else None)
+    assert mxattn._raw_stream(3) == 42

@@ -6,9 +6,10 @@
 //   S^T = K Q^T   on the FP8 matrix cores (32x32x64), K's codes as they are.  A
 //                 bf16 number has 8 significant bits, two E4M3 numbers' worth:
 //                 Q = 2^e (hi + lo), hi the nearest E4M3 number to q 2^-e and lo
-//                 that of the rest, which leaves at most 2^-22 of the row's
-//                 largest magnitude.  Two FP8 products take the time of one in
-//                 bf16, and K needs no conversion;
+//                 that of the rest in steps of 2^-13 2^e at least: exact for
+//                 magnitudes from 2^-6 2^e on, else off by up to 2^-14 2^e, less than
+//                 2^-21 of the row's largest.  Two FP8 products take the time of one
+//                 in bf16, and K needs no conversion;
 //   softmax       online, in fp32: m' = max(m, s c - 7), p = exp2(s c - m'), which is
 //                 at most 2^7;
 //   O^T += V^T P^T on the f16 matrix cores: p is rounded to f16, by 2^-11 of it, or below
@@ -76,8 +77,8 @@ __device__ __forceinline__ QOperand load_q(const uint16_t* row, int h, float sca
         }
     m = max(m & 0xFFFFu, m >> 16);
     m = max(m, __builtin_bit_cast(uint32_t, other_half(__builtin_bit_cast(float, m))));
-    // the smallest e >= -127 with 1.f 2^(E-127) <= 448 2^e; lo in steps 2^-4 of hi's, or as
-    // small as they get
+    // the smallest e >= -122 with 1.f 2^(E-127) <= 448 2^e (lo's scale, 2^-4 of hi's, is then
+    // a number too)
     const int e = max((int)(m >> 7) - 135 + ((m & 0x7Fu) > 0x60u ? 1 : 0), -122);
     const float fh = e8m0_as_f32((uint32_t)(e + 127)), fl = e8m0_as_f32((uint32_t)(e + 123));
     QOperand q;

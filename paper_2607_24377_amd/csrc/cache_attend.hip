@@ -8,10 +8,11 @@
 // joined by a second kernel.  Short ones: the four waves of a workgroup take an item's
 // blocks in turn and meet in LDS.
 //
-// 64 sequences' single tokens over 8200 keys, 32 heads on 8: 606 MB, 115 to 119 us and
-// 5 for the join, 5.0 TB/s; one over 118801 keys, 24 heads: 730 MB, 132 and 6, 5.3 TB/s;
-// 16 x 4 tokens over 6000 keys, 40 heads on 8: 113 MB, 28 and 7; one over 512 keys, 2
-// heads: 7.3, a chain of loads (lengths, pages, codes).
+// 64 sequences' single tokens over 8200 keys, 32 heads on 8: 606 MB, 117 to 120 us and
+// 5 for the join, 5.0 TB/s; one over 118801 keys, 24 heads: 730 MB, 134 and 6, 5.4 TB/s
+// (reading alone reaches 6.4 TB/s on this card); 16 x 4 tokens over 6000 keys, 40 heads
+// on 8: 113 MB, 28 and 7; one over 512 keys, 2 heads: 8.0, a chain of loads (lengths,
+// pages, codes).
 #include "cache_attend.h"
 
 namespace mxattn {

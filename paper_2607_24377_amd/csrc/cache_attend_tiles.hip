@@ -8,12 +8,14 @@
 // FP8 operands for the scores, and codes that become f16 in registers for the
 // second product.  Two waves a SIMD (256 registers) run each other's gaps.
 //
-// 1560 rows x 32760 keys x 40 heads: 1.10 to 1.14 ms, 920 to 955 TFLOP/s; matrix cores
-// busy 48 %, vector issue 55 % (139 instructions per 32 x 32 scores, about 830
-// cycles), LDS half of its time.  256 rows in eight waves 1.10, 64 rows per wave 1.72
-// (spills), one wave a SIMD 1.21, V as 16 bits in LDS, made once for the four waves, 1.25
-// (more to read there); the next scores under this step's softmax, a wait for the step
-// before only, or priorities of the waves gained nothing.
+// 1560 rows x 32760 keys x 40 heads: 1.11 to 1.15 ms, 910 to 940 TFLOP/s; matrix cores
+// busy 47 %, vector issue 55 % (141 instructions per 32 x 32 scores, about 830
+// cycles), LDS half of its time; 3.4 GB fetched, ten times the keys and values, 3 TB/s
+// beside the products.  Other forms, measured with probabilities in bf16 (1.10 to 1.13):
+// 256 rows in eight waves 1.10, 64 rows per wave 1.72 (spills), one wave a SIMD 1.21, V as
+// 16 bits in LDS, made once for the four waves, 1.25 (more to read there); the next scores
+// under this step's softmax, a wait for the step before only, or priorities of the waves
+// gained nothing.
 #include "cache_attend.h"
 
 namespace mxattn {

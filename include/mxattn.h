@@ -364,9 +364,10 @@ int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t 
  * among them, appended before): O = softmax(Q K^T / sqrt(d)) V with fp32 scores,
  * softmax and sums.  Query head i reads KV head i / (Hq / Hkv).  Three choices hold
  * less than fp32: P is rounded to f16 before its product with V (by 2^-11 of each p,
- * or 2^-32 of the row's largest below 2^-21 of that); Q is held to 2^-21 of its row's
+ * or 2^-36 of the row's largest below 2^-25 of that); Q is held to 2^-21 of its row's
  * largest magnitude; and blocks of V whose scale is below 2^-55 of the largest one of
- * their sequence lose digits.  Scores of 2^27 and more in magnitude may give inf or NaN.
+ * their sequence lose digits.  Scores of 2^26 and more in magnitude, and keys of 2^112
+ * and more, may give inf or NaN.
  * causal != 0: token i of n sees positions 0 .. kv_len - n + i, else all kv_len.
  * A query that sees no key gets 0.
  *   q     device bf16 [tokens, Hq, d], heads contiguous, token stride; Hq at most

@@ -10,10 +10,10 @@
 //                 magnitudes from 2^-6 2^e on, else off by up to 2^-14 2^e, less than
 //                 2^-21 of the row's largest.  Two FP8 products take the time of one
 //                 in bf16, and K needs no conversion;
-//   softmax       online, in fp32: m' = max(m, s c - 7), p = exp2(s c - m'), which is
-//                 at most 2^7;
+//   softmax       online, in fp32: m' = max(m, s c - 11), p = exp2(s c - m'), which is
+//                 at most 2^11;
 //   O^T += V^T P^T on the f16 matrix cores: p is rounded to f16, by 2^-11 of it, or below
-//                 2^-21 of the largest by 2^-32 of that (bf16 rounds by 2^-8, which
+//                 2^-25 of the largest by 2^-36 of that (bf16 rounds by 2^-8, which
 //                 was a third of the result's whole error; 1560 rows x 32760 keys x 40
 //                 heads took 1.11 ms with it and 1.14 so, 64 tokens x 8200 keys 119.5 us
 //                 and 121).
@@ -40,9 +40,9 @@ typedef short i16x2 __attribute__((ext_vector_type(2)));
 // the running maximum before the first key: below every finite score, so that
 // masked scores (-inf) give p = 0 and never inf - inf
 constexpr float kNoMax = -3.0e38f;
-// The largest p is 2^7: f16 holds 2^-31 of that, and 2^15, which p reaches where m, a
-// fp32 number below 2^28, is rounded by 8.
-constexpr int kTopLog2 = 7;
+// The largest p is 2^11: f16 holds 2^-35 of that, and 2^15, which p reaches where m, a
+// fp32 number below 2^27, is rounded by 4.
+constexpr int kTopLog2 = 11;
 
 // row / group, a row below 2^28 (a product and a shift: the division is 25 instructions).
 __device__ __forceinline__ int token_of(const CacheAttendArgs& a, int row) {
@@ -218,7 +218,7 @@ struct State {
         return e8m0_as_f32((uint32_t)f);
     }
     // Moves the units to scale byte b, but to no less than 2^-40 of the largest so far: O~,
-    // below 2^47 there, cannot overflow, and blocks whose scale is below 2^-55 of the
+    // below 2^51 there, cannot overflow, and blocks whose scale is below 2^-55 of the
     // largest one's lose digits.  Returns what b's codes are multiplied by: NaN for 255,
     // which units of at most 247 do not reach.
     __device__ __forceinline__ int move(int b) {

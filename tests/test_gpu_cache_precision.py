@@ -1,7 +1,7 @@
 """What attention over the cache keeps of its probabilities and values.
 
 Tolerance: cache_reference.attend's bound with p's rounding to f16 in the place of 2^-8: half a step, 2^-11 of each p,
-so 2^-11 of sum p |v|.  (p below 2^-21 of the largest is rounded by 2^-32 of that: no p is so small where the values
+so 2^-11 of sum p |v|.  (p below 2^-25 of the largest is rounded by 2^-36 of that: no p is so small where the values
 differ much.)  The rest of that bound (the result's own rounding 2^-8 |o|, the scores' errors, sums in fp32) stays."""
 import pytest
 
@@ -74,7 +74,7 @@ def test_values_of_very_different_blocks(mx, causal, spread, way):  # noqa: F811
 def test_scores_of_large_magnitude(mx, power, way):  # noqa: F811
     """Sums q.k of up to 3 * 2^(power + 4): the largest takes everything, whatever the rounding of its own product with
     the scale does to p, so the result is its key's value, rounded to f16's product and bf16.  (The scores that the
-    call takes, q.k / sqrt(128), end at 2^27.)"""
+    call takes, q.k / sqrt(128), end at 2^26.)"""
     print(f"[precision] scores 2^{power} {way}", flush=True)
     n = 64
     k = torch.zeros((n, 1, ref.D))

@@ -94,11 +94,13 @@ typedef enum {
                                    pre-scale gamma not in (0, 3e38)         */
     MXATTN_ERR_SCRATCH = 10,    /* the problem needs more than the static
                                    scratch of mxattn_cross_attend_noalloc, or
-                                   than the workspace that mxattn_cache_attend
-                                   was given (none, under graph capture)    */
-    MXATTN_ERR_VALUE = 11       /* rot, pairs, eps or page_tokens outside what
-                                   the call takes, Hq no multiple of Hkv or
-                                   more than 256 times as many              */
+                                   than the workspace that a call of attention
+                                   over the cache was given (none, under graph
+                                   capture)                                 */
+    MXATTN_ERR_VALUE = 11       /* rot, pairs, eps, page_tokens, window, sinks,
+                                   budget or recent outside what the call
+                                   takes, Hq no multiple of Hkv or more than
+                                   256 times as many                        */
 } mxattn_status;
 
 #define MXATTN_AXIS_TOKENS 2   /* blocks along N (V)      */
@@ -403,6 +405,103 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
 size_t mxattn_cache_attend_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens,
                                      int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv);
 
+/* Attention of a call's tokens over part of their sequences' cached keys: as
+ * mxattn_cache_attend (its arguments, limits, workspace and precision, the same keys
+ * in the same order), but with T = kv_len - n + i + 1 (causal) or kv_len, a token
+ * sees the last `window` keys before T, positions T - window .. T - 1, and positions
+ * 0 .. sinks - 1 of those before T.  Page table entries whose pages no token of the
+ * call sees are not read: a program may have given those pages away.
+ *   window  >= 1, sinks >= 0 (MXATTN_ERR_VALUE otherwise)
+ * mxattn_cache_attend_workspace() bytes with the same max_q and max_kv suffice. */
+int mxattn_cache_attend_window(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                               const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages,
+                               int64_t page_tokens, const int32_t* page_table, const int32_t* q_start,
+                               const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t tokens,
+                               int64_t Hq, int64_t Hkv, int64_t d, int64_t window, int64_t sinks, int causal,
+                               int64_t max_q, int64_t max_kv, void* out, int64_t out_stride, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* Attention for drafted tokens that form trees: as mxattn_cache_attend, but token i of n
+ * sees positions 0 .. kv_len - n - 1, and of the n new ones (position kv_len - n + j)
+ * those whose bit j is set in its mask: its ancestors and, where it is to see itself,
+ * bit i.
+ *   tree        device int32 [tokens, tree_words]: bit j & 31 of word j >> 5.  New tokens
+ *               from 32 tree_words on are seen by none; bits from n on do not count.
+ *   tree_words  1 .. 2^19
+ * Rotation by depth is the caller's: give mxattn_cache_append the positions.
+ * mxattn_cache_compact moves the tokens that were accepted to the sequence's end. */
+int mxattn_cache_attend_tree(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                             const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
+                             const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len,
+                             int64_t seqs, int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d,
+                             const int32_t* tree, int64_t tree_words, int64_t max_q, int64_t max_kv, void* out,
+                             int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* mxattn_cache_attend that also weighs the keys: for every position j of a sequence
+ * that owns tokens of the call, and every KV head,
+ *   weights_out[j] = (j < kv_len - n ? weights[j] : 0) + sum of p over the n tokens and the
+ *                    Hq / Hkv heads
+ * in fp32, p the probabilities that O is made of.  Weights lie beside the cache, fp32
+ * [pages, Hkv, page_tokens]; those of other positions and sequences are not written.
+ *   weights      NULL: zeros
+ *   weights_out  may be `weights`; must not overlap it otherwise
+ *   max_kv       here a limit: a sequence that is longer counts as one of impossible
+ *                length (its queries get NaN, its weights are not written).
+ * A query that gets NaN (see above) makes the weights of the keys it sees NaN.  Equal
+ * arguments and contents give equal bits.  Two sequences of a call must not share a page
+ * (which one's weights are stored there is undefined).
+ *   workspace    mxattn_cache_attend_weights_workspace() bytes: mxattn_cache_attend's, 8 for
+ *                each token and head, and with few tokens the scores, 4 for each token,
+ *                head and key of max_kv, at most 1 GiB. */
+int mxattn_cache_attend_weights(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                                const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages,
+                                int64_t page_tokens, const int32_t* page_table, const int32_t* q_start,
+                                const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t tokens,
+                                int64_t Hq, int64_t Hkv, int64_t d, const float* weights, float* weights_out,
+                                int causal, int64_t max_q, int64_t max_kv, void* out, int64_t out_stride,
+                                void* workspace, size_t workspace_bytes, void* stream);
+size_t mxattn_cache_attend_weights_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens,
+                                             int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv);
+
+/* Which of a sequence's tokens stay when it is cut to `budget`, for every KV head: all
+ * if there are no more; else the first `sinks`, the last `recent` and, of those between,
+ * the ones of the largest weight (of equal ones the first; NaN and pages that do not
+ * exist weigh less than every number).
+ *   weights  device fp32 [pages, Hkv, page_tokens]
+ *   kept     device int32 [seqs, Hkv, budget]: their positions, ascending, then -1
+ *   counts   device int32 [seqs]: min(kv_len, budget); 0 for an impossible length
+ *   budget   1 .. 2^24, sinks >= 0, recent >= 0, sinks + recent <= budget
+ *            (MXATTN_ERR_VALUE otherwise); seqs * Hkv < 2^22 */
+int mxattn_cache_select(const float* weights, int64_t pages, int64_t page_tokens, const int32_t* page_table,
+                        const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t Hkv, int64_t budget,
+                        int64_t sinks, int64_t recent, int32_t* kept, int32_t* counts, void* stream);
+
+/* Move kept tokens together: position base + i of a sequence (i < counts) becomes what was
+ * at position kept[i], K, V and weights; the sequence's length is then base + counts.
+ * What is at positions below base stays (in the first block that is written, with the
+ * others' scale).  A block takes the largest scale of the blocks that its tokens come
+ * from, and code * 2^(e_old - e) is rounded to nearest, ties to even: exact unless it
+ * falls below 2^-6.  A block's codes behind the last token become 0.
+ *   kept       device int32 [seqs, kept_heads, width]; kept_heads is Hkv, or 1: the same for
+ *              all heads.  A position that the page table does not have, or whose page
+ *              does not exist, or whose scale is no number gives NaN codes (and weight 0
+ *              without a page).
+ *   counts     device int32 [seqs]; nothing is done for a sequence of a count outside
+ *              1 .. width, or that does not fit the table
+ *   base       device int32 [seqs], or NULL: 0
+ *   out_table  device int32 [seqs, out_pages]: where the tokens go, on pages that hold
+ *              none of the call's sources; nothing is written to a page that does not
+ *              exist.  NULL or page_table: in place, where kept ascends and kept[i] >= base + i
+ *              (anything else gives undefined contents there; nothing out of range).
+ *   weights    device fp32 [pages, Hkv, page_tokens], or NULL
+ * In place a head's blocks are moved one turn after another; to other pages all at once.
+ * Sequences of a call must not share pages that are written.  seqs * Hkv < 2^22. */
+int mxattn_cache_compact(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int64_t pages,
+                         int64_t page_tokens, const int32_t* page_table, int64_t seqs, int64_t max_pages,
+                         const int32_t* out_table, int64_t out_pages, int64_t Hkv, int64_t d, const int32_t* kept,
+                         int64_t kept_heads, int64_t width, const int32_t* counts, const int32_t* base,
+                         float* weights, void* stream);
+
 /* Sizes of the code and scale arrays of a [B, H, N, d] tensor blocked along
  * `block_axis`; 0 for invalid arguments. */
 size_t mxattn_codes_bytes(int block_axis, int64_t B, int64_t H, int64_t N, int64_t d);
@@ -424,8 +523,8 @@ const char* mxattn_status_string(int status);
 const char* mxattn_last_error(void);
 
 /* Workspace.  mxattn_forward, mxattn_cross_forward, mxattn_attend,
- * mxattn_cross_attend, mxattn_qmax_sse and mxattn_cache_attend (where it is
- * given none) take their workspace, stream-ordered, from a memory pool that belongs to the library (one per device,
+ * mxattn_cross_attend, mxattn_qmax_sse and the calls of attention over the cache
+ * (where they are given none) take their workspace, stream-ordered, from a memory pool that belongs to the library (one per device,
  * created on first use; the device's default pool is left as it is).  The
  * pool keeps freed workspace for the next call rather than returning it to
  * the driver; one block of at most 64 MiB per device stays allocated for the

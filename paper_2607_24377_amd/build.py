@@ -14,7 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmxattn.so")
 SOURCES = ["api.hip", "quantize.hip", "attention.hip", "qmax.hip", "rowsum.hip", "rope.hip", "cache_append.hip",
-           "cache_attend.hip", "cache_attend_tiles.hip"]
+           "cache_attend.hip", "cache_attend_tiles.hip", "cache_weigh.hip", "cache_evict.hip"]
 ARCH = "gfx950"
 
 

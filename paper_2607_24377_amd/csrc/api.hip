@@ -5,6 +5,7 @@
 // (workspace.h) and the static scratch of the no-allocation entry point.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdio>
 #include <mutex>
 
@@ -52,7 +53,7 @@ int rule_of(int mode) { return mode == MXATTN_OCP_VANILLA ? mxattn::kRuleOcp : m
 
 extern "C" {
 
-int mxattn_version(void) { return 102; }
+int mxattn_version(void) { return 103; }
 
 int mxattn_release_workspace(void) { return mxattn::release_workspace(); }
 
@@ -71,9 +72,9 @@ const char* mxattn_status_string(int s) {
         case MXATTN_ERR_UNSUPPORTED: return "unsupported head dimension (d must be 128)";
         case MXATTN_ERR_OOM: return "workspace allocation failed";
         case MXATTN_ERR_HIP: return "HIP runtime error";
-        case MXATTN_ERR_SCRATCH: return "more scratch needed than there is (the no-allocation entry point: B*H*ceil(Nkv/128) <= 32768; cache attention: a workspace of mxattn_cache_attend_workspace() bytes from the caller, always on a stream under graph capture)";
+        case MXATTN_ERR_SCRATCH: return "more scratch needed than there is (the no-allocation entry point: B*H*ceil(Nkv/128) <= 32768; cache attention: a workspace of mxattn_cache_attend_workspace() or mxattn_cache_attend_weights_workspace() bytes from the caller, always on a stream under graph capture)";
         case MXATTN_ERR_BOUNDARY: return "invalid scale boundary (need 4 <= q <= 8 and 1 <= nq <= 64) or pre-scale (need 0 < gamma < 3e38)";
-        case MXATTN_ERR_VALUE: return "invalid value (rot 0 or a multiple of 16 up to 128, pairs 0 or 1, eps finite and >= 0, page_tokens a power of two from 32 to 4096, Hq a multiple of Hkv, at most 256 of it)";
+        case MXATTN_ERR_VALUE: return "invalid value (rot 0 or a multiple of 16 up to 128, pairs 0 or 1, eps finite and >= 0, page_tokens a power of two from 32 to 4096, Hq a multiple of Hkv, at most 256 of it, window >= 1, sinks and recent >= 0 and together at most a budget of 1 to 2^24)";
         default: return "unknown status";
     }
 }
@@ -633,6 +634,34 @@ static int check_query_heads(int64_t seqs, int64_t tokens, int64_t Hq, int64_t H
     return (tokens * (Hq / Hkv) / 32 + seqs) * Hkv >> 24 ? MXATTN_ERR_SHAPE : MXATTN_OK;
 }
 
+// The sizes of a cache's pages and of a batch over it; fills c.
+static int check_pages(mxattn::CacheArgs& c, int64_t pages, int64_t page_tokens, const int32_t* page_table, int64_t seqs,
+                       int64_t max_pages, int64_t tokens, int64_t Hkv) {
+    if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0) return MXATTN_ERR_VALUE;
+    const int64_t bpp = page_tokens / 32;
+    if (int st = check_batch(seqs, max_pages, page_tokens, tokens, Hkv)) return st;
+    if (pages < 1 || pages > (int64_t)1 << 30 || pages * bpp > ((int64_t)1 << 40) / Hkv) return MXATTN_ERR_SHAPE;
+    if (!aligned(page_table, 4)) return MXATTN_ERR_ALIGN;
+    c.page_table = page_table;
+    c.seqs = (int)seqs;
+    c.tokens = (int)tokens;
+    c.heads = (int)Hkv;
+    c.pages = (int)pages;
+    c.max_pages = (int)max_pages;
+    c.bpp_log2 = __builtin_ctzll((unsigned long long)bpp);
+    return MXATTN_OK;
+}
+
+static int check_codes(mxattn::CacheArgs& c, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                       const uint8_t* v_scales) {
+    if (!aligned(k_codes, 16) || !aligned(v_codes, 16)) return MXATTN_ERR_ALIGN;
+    c.kc = const_cast<uint8_t*>(k_codes);
+    c.vc = const_cast<uint8_t*>(v_codes);
+    c.ks = const_cast<uint8_t*>(k_scales);
+    c.vs = const_cast<uint8_t*>(v_scales);
+    return MXATTN_OK;
+}
+
 // The checks that the calls on the paged cache share; fills c.
 static int check_cache(mxattn::CacheArgs& c, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
                        const uint8_t* v_scales, int64_t pages, int64_t page_tokens, const int32_t* page_table,
@@ -640,26 +669,11 @@ static int check_cache(mxattn::CacheArgs& c, const uint8_t* k_codes, const uint8
                        int64_t Hkv, int64_t d) {
     if (!k_codes || !k_scales || !v_codes || !v_scales || !page_table || !q_start || !kv_len) return MXATTN_ERR_NULL;
     if (int st = check_shape(1, 1, 1, d)) return st;
-    if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0) return MXATTN_ERR_VALUE;
-    const int64_t bpp = page_tokens / 32;
-    if (int st = check_batch(seqs, max_pages, page_tokens, tokens, Hkv)) return st;
-    if (pages < 1 || pages > (int64_t)1 << 30 || pages * bpp > ((int64_t)1 << 40) / Hkv) return MXATTN_ERR_SHAPE;
-    if (!aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(page_table, 4) || !aligned(q_start, 4) ||
-        !aligned(kv_len, 4))
-        return MXATTN_ERR_ALIGN;
-    c.kc = const_cast<uint8_t*>(k_codes);
-    c.vc = const_cast<uint8_t*>(v_codes);
-    c.ks = const_cast<uint8_t*>(k_scales);
-    c.vs = const_cast<uint8_t*>(v_scales);
-    c.page_table = page_table;
+    if (int st = check_pages(c, pages, page_tokens, page_table, seqs, max_pages, tokens, Hkv)) return st;
+    if (int st = check_codes(c, k_codes, k_scales, v_codes, v_scales)) return st;
+    if (!aligned(q_start, 4) || !aligned(kv_len, 4)) return MXATTN_ERR_ALIGN;
     c.q_start = q_start;
     c.kv_len = kv_len;
-    c.seqs = (int)seqs;
-    c.tokens = (int)tokens;
-    c.heads = (int)Hkv;
-    c.pages = (int)pages;
-    c.max_pages = (int)max_pages;
-    c.bpp_log2 = __builtin_ctzll((unsigned long long)bpp);
     return MXATTN_OK;
 }
 
@@ -715,18 +729,126 @@ static void attend_bounds(int64_t& max_q, int64_t& max_kv, int64_t tokens, int64
     if (max_q == 0 || max_q > tokens) max_q = tokens;
 }
 
-size_t mxattn_cache_attend_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens, int64_t Hq,
-                                     int64_t Hkv, int64_t max_q, int64_t max_kv) {
+// The sizes of a call of attention over the cache, without its memory; false where it is refused.
+static bool sized_attend(mxattn::CacheAttendArgs& a, int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens,
+                         int64_t Hq, int64_t Hkv, int64_t& max_q, int64_t& max_kv) {
     if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0 || max_q < 0 || max_kv < 0 ||
         check_batch(seqs, max_pages, page_tokens, tokens, Hkv) || check_query_heads(seqs, tokens, Hq, Hkv))
-        return 0;
-    mxattn::CacheAttendArgs a{};
+        return false;
     a.c.seqs = (int)seqs;
     a.c.tokens = (int)tokens;
     a.c.heads = (int)Hkv;
     a.group = (int)(Hq / Hkv);
     attend_bounds(max_q, max_kv, tokens, max_pages * page_tokens);
+    return true;
+}
+
+size_t mxattn_cache_attend_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens, int64_t Hq,
+                                     int64_t Hkv, int64_t max_q, int64_t max_kv) {
+    mxattn::CacheAttendArgs a{};
+    if (!sized_attend(a, page_tokens, seqs, max_pages, tokens, Hq, Hkv, max_q, max_kv)) return 0;
     return mxattn::cache_attend_workspace(a, max_q, max_kv);
+}
+
+size_t mxattn_cache_attend_weights_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens,
+                                             int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv) {
+    mxattn::CacheAttendArgs a{};
+    if (!sized_attend(a, page_tokens, seqs, max_pages, tokens, Hq, Hkv, max_q, max_kv)) return 0;
+    return mxattn::cache_weigh_workspace(a, max_q, max_kv);
+}
+
+// The arguments that the calls of attention over the cache share.
+struct AttendCall {
+    const char* name;
+    const void* q;
+    int64_t q_stride;
+    const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int64_t pages, page_tokens;
+    const int32_t *page_table, *q_start, *kv_len;
+    int64_t seqs, max_pages, tokens, Hq, Hkv, d;
+    int causal;
+    int64_t max_q, max_kv;
+    void* out;
+    int64_t out_stride;
+    void* workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+    size_t q_bytes, out_bytes;  // set by check_attend
+};
+
+// The checks that they share; fills a.
+static int check_attend(AttendCall& x, mxattn::CacheAttendArgs& a) {
+    if (!x.q || !x.out) return MXATTN_ERR_NULL;
+    if (int st = check_cache(a.c, x.k_codes, x.k_scales, x.v_codes, x.v_scales, x.pages, x.page_tokens, x.page_table,
+                             x.q_start, x.kv_len, x.seqs, x.max_pages, x.tokens, x.Hkv, x.d))
+        return st;
+    if (int st = check_query_heads(x.seqs, x.tokens, x.Hq, x.Hkv)) return st;
+    if (x.max_q < 0 || x.max_kv < 0) return MXATTN_ERR_SHAPE;
+    if (int st = check_rows(x.q, x.q_stride, x.tokens, x.Hq, false, x.q_bytes)) return st;
+    if (int st = check_rows(x.out, x.out_stride, x.tokens, x.Hq, true, x.out_bytes)) return st;
+    if (overlaps(x.out, x.out_bytes, x.q, x.q_bytes) || in_cache(x.out, x.out_bytes, a.c)) return MXATTN_ERR_SHAPE;
+    a.q = static_cast<const uint16_t*>(x.q);
+    a.out = static_cast<uint16_t*>(x.out);
+    a.q_stride = x.q_stride;
+    a.out_stride = x.out_stride;
+    a.group = (int)(x.Hq / x.Hkv);
+    a.per_group = (((uint64_t)1 << 36) + a.group - 1) / a.group;
+    a.causal = x.causal != 0;
+    a.scale = 0.12751743082459868f;  // fp32(log2(e) / sqrt(128))
+    attend_bounds(x.max_q, x.max_kv, x.tokens, x.max_pages * x.page_tokens);
+    return MXATTN_OK;
+}
+
+extern "C++" {  // (a template)
+// Runs `launch(workspace)` with `bytes` of workspace: the caller's, or the library's where it gives none.
+template <class Launch>
+static int run_attend(const AttendCall& x, const mxattn::CacheArgs& c, size_t bytes, Launch launch) {
+    uint8_t* memory = nullptr;
+    Workspace ws;
+    if (bytes && x.workspace) {
+        if (x.workspace_bytes < bytes) {
+            std::snprintf(g_last_error, sizeof g_last_error, "%s: %zu bytes of workspace needed, the caller's has %zu", x.name,
+                          bytes, x.workspace_bytes);
+            return MXATTN_ERR_SCRATCH;
+        }
+        if (!aligned(x.workspace, 16)) return MXATTN_ERR_ALIGN;
+        if (overlaps(x.workspace, bytes, x.q, x.q_bytes) || overlaps(x.workspace, bytes, x.out, x.out_bytes) ||
+            in_cache(x.workspace, bytes, c))
+            return MXATTN_ERR_SHAPE;
+        memory = static_cast<uint8_t*>(x.workspace);
+        bytes = 0;
+    } else if (bytes) {
+        // an allocation of the pool is not recorded into a graph: its replays need memory that lasts
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        if (x.stream) {
+            if (hipError_t e = hipStreamIsCapturing(x.stream, &capture)) {
+                set_error("hipStreamIsCapturing", e);
+                return MXATTN_ERR_HIP;
+            }
+        }
+        if (capture != hipStreamCaptureStatusNone) {
+            std::snprintf(g_last_error, sizeof g_last_error,
+                          "%s: %zu bytes of workspace needed from the caller, as the stream is being captured", x.name, bytes);
+            return MXATTN_ERR_SCRATCH;
+        }
+        if (int st = ws.take(bytes, x.stream)) return st;
+        memory = ws.get();
+    }
+    int st = MXATTN_OK;
+    hipError_t e = launch(memory);
+    if (e != hipSuccess) {
+        set_error("cache attention launch", e);
+        st = MXATTN_ERR_HIP;
+    }
+    return bytes ? ws.give_back(st) : st;
+}
+}  // extern "C++"
+
+static int run_plain_attend(AttendCall& x, mxattn::CacheAttendArgs& a) {
+    return run_attend(x, a.c, mxattn::cache_attend_workspace(a, x.max_q, x.max_kv), [&](uint8_t* memory) {
+        a.workspace = memory;
+        return mxattn::launch_cache_attend(a, x.max_q, x.max_kv, x.stream);
+    });
 }
 
 int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
@@ -735,65 +857,154 @@ int mxattn_cache_attend(const void* q, int64_t q_stride, const uint8_t* k_codes,
                         int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d, int causal,
                         int64_t max_q, int64_t max_kv, void* out, int64_t out_stride, void* workspace,
                         size_t workspace_bytes, void* stream) {
-    if (!q || !out) return MXATTN_ERR_NULL;
+    AttendCall x{"mxattn_cache_attend", q, q_stride, k_codes, k_scales, v_codes, v_scales, pages, page_tokens, page_table,
+                 q_start, kv_len, seqs, max_pages, tokens, Hq, Hkv, d, causal, max_q, max_kv, out, out_stride, workspace,
+                 workspace_bytes, reinterpret_cast<hipStream_t>(stream), 0, 0};
     mxattn::CacheAttendArgs a{};
-    if (int st = check_cache(a.c, k_codes, k_scales, v_codes, v_scales, pages, page_tokens, page_table, q_start, kv_len,
-                             seqs, max_pages, tokens, Hkv, d))
-        return st;
-    if (int st = check_query_heads(seqs, tokens, Hq, Hkv)) return st;
-    if (max_q < 0 || max_kv < 0) return MXATTN_ERR_SHAPE;
-    size_t qb = 0, ob = 0;
-    if (int st = check_rows(q, q_stride, tokens, Hq, false, qb)) return st;
-    if (int st = check_rows(out, out_stride, tokens, Hq, true, ob)) return st;
-    if (overlaps(out, ob, q, qb) || in_cache(out, ob, a.c)) return MXATTN_ERR_SHAPE;
-    a.q = static_cast<const uint16_t*>(q);
-    a.out = static_cast<uint16_t*>(out);
-    a.q_stride = q_stride;
-    a.out_stride = out_stride;
-    a.group = (int)(Hq / Hkv);
-    a.per_group = (((uint64_t)1 << 36) + a.group - 1) / a.group;
-    a.causal = causal != 0;
-    a.scale = 0.12751743082459868f;  // fp32(log2(e) / sqrt(128))
-    attend_bounds(max_q, max_kv, tokens, max_pages * page_tokens);
-    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    size_t bytes = mxattn::cache_attend_workspace(a, max_q, max_kv);
-    Workspace ws;
-    if (bytes && workspace) {
-        if (workspace_bytes < bytes) {
-            std::snprintf(g_last_error, sizeof g_last_error,
-                          "mxattn_cache_attend: %zu bytes of workspace needed, the caller's has %zu", bytes, workspace_bytes);
-            return MXATTN_ERR_SCRATCH;
-        }
-        if (!aligned(workspace, 16)) return MXATTN_ERR_ALIGN;
-        if (overlaps(workspace, bytes, q, qb) || overlaps(workspace, bytes, out, ob) || in_cache(workspace, bytes, a.c))
-            return MXATTN_ERR_SHAPE;
-        a.workspace = static_cast<uint8_t*>(workspace);
-        bytes = 0;
-    } else if (bytes) {
-        // an allocation of the pool is not recorded into a graph: its replays need memory that lasts
-        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-        if (s) {
-            if (hipError_t e = hipStreamIsCapturing(s, &capture)) {
-                set_error("hipStreamIsCapturing", e);
-                return MXATTN_ERR_HIP;
-            }
-        }
-        if (capture != hipStreamCaptureStatusNone) {
-            std::snprintf(g_last_error, sizeof g_last_error,
-                          "mxattn_cache_attend: %zu bytes of workspace needed from the caller, as the stream is being captured",
-                          bytes);
-            return MXATTN_ERR_SCRATCH;
-        }
-        if (int st = ws.take(bytes, s)) return st;
-        a.workspace = ws.get();
-    }
-    int st = MXATTN_OK;
-    hipError_t e = mxattn::launch_cache_attend(a, max_q, max_kv, s);
+    if (int st = check_attend(x, a)) return st;
+    return run_plain_attend(x, a);
+}
+
+int mxattn_cache_attend_window(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                               const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
+                               const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len, int64_t seqs,
+                               int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d, int64_t window,
+                               int64_t sinks, int causal, int64_t max_q, int64_t max_kv, void* out, int64_t out_stride,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    AttendCall x{"mxattn_cache_attend_window", q, q_stride, k_codes, k_scales, v_codes, v_scales, pages, page_tokens,
+                 page_table, q_start, kv_len, seqs, max_pages, tokens, Hq, Hkv, d, causal, max_q, max_kv, out, out_stride,
+                 workspace, workspace_bytes, reinterpret_cast<hipStream_t>(stream), 0, 0};
+    mxattn::CacheAttendArgs a{};
+    if (int st = check_attend(x, a)) return st;
+    if (window < 1 || sinks < 0) return MXATTN_ERR_VALUE;
+    a.kind = mxattn::kWindow;
+    a.window = (int)std::min(window, mxattn::kMaxKeys);  // (no sequence is longer)
+    a.sinks = (int)std::min(sinks, mxattn::kMaxKeys);
+    return run_plain_attend(x, a);
+}
+
+int mxattn_cache_attend_tree(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                             const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
+                             const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len, int64_t seqs,
+                             int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d, const int32_t* tree,
+                             int64_t tree_words, int64_t max_q, int64_t max_kv, void* out, int64_t out_stride,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+    AttendCall x{"mxattn_cache_attend_tree", q, q_stride, k_codes, k_scales, v_codes, v_scales, pages, page_tokens,
+                 page_table, q_start, kv_len, seqs, max_pages, tokens, Hq, Hkv, d, 0, max_q, max_kv, out, out_stride,
+                 workspace, workspace_bytes, reinterpret_cast<hipStream_t>(stream), 0, 0};
+    if (!tree) return MXATTN_ERR_NULL;
+    mxattn::CacheAttendArgs a{};
+    if (int st = check_attend(x, a)) return st;
+    if (tree_words < 1 || tree_words > mxattn::kMaxKeys / 32) return MXATTN_ERR_SHAPE;
+    if (!aligned(tree, 4)) return MXATTN_ERR_ALIGN;
+    if (overlaps(out, x.out_bytes, tree, (size_t)tokens * tree_words * 4)) return MXATTN_ERR_SHAPE;
+    a.kind = mxattn::kTree;
+    a.tree = tree;
+    a.tree_words = (int)tree_words;
+    return run_plain_attend(x, a);
+}
+
+// Bytes of weights beside a cache.
+static size_t weights_bytes(const mxattn::CacheArgs& c) {
+    return (((size_t)c.pages * (size_t)c.heads) << c.bpp_log2) * mxattn::kBlockTokens * sizeof(float);
+}
+
+int mxattn_cache_attend_weights(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
+                                const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages, int64_t page_tokens,
+                                const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len, int64_t seqs,
+                                int64_t max_pages, int64_t tokens, int64_t Hq, int64_t Hkv, int64_t d, const float* weights,
+                                float* weights_out, int causal, int64_t max_q, int64_t max_kv, void* out,
+                                int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream) {
+    AttendCall x{"mxattn_cache_attend_weights", q, q_stride, k_codes, k_scales, v_codes, v_scales, pages, page_tokens,
+                 page_table, q_start, kv_len, seqs, max_pages, tokens, Hq, Hkv, d, causal, max_q, max_kv, out, out_stride,
+                 workspace, workspace_bytes, reinterpret_cast<hipStream_t>(stream), 0, 0};
+    if (!weights_out) return MXATTN_ERR_NULL;
+    mxattn::CacheWeighArgs w{};
+    if (int st = check_attend(x, w.a)) return st;
+    if (!aligned(weights, 4) || !aligned(weights_out, 4)) return MXATTN_ERR_ALIGN;
+    const size_t wb = weights_bytes(w.a.c);
+    if (overlaps(weights_out, wb, q, x.q_bytes) || overlaps(weights_out, wb, out, x.out_bytes) ||
+        in_cache(weights_out, wb, w.a.c) || (weights && overlaps(weights, wb, out, x.out_bytes)) ||
+        (weights && weights != weights_out && overlaps(weights_out, wb, weights, wb)))
+        return MXATTN_ERR_SHAPE;
+    const size_t bytes = mxattn::cache_weigh_workspace(w.a, x.max_q, x.max_kv);
+    if (workspace && (overlaps(workspace, bytes, weights_out, wb) || (weights && overlaps(workspace, bytes, weights, wb))))
+        return MXATTN_ERR_SHAPE;
+    w.before = weights;
+    w.after = weights_out;
+    return run_attend(x, w.a.c, bytes, [&](uint8_t* memory) {
+        w.a.workspace = memory;
+        return mxattn::launch_cache_weigh(w, x.max_q, x.max_kv, x.stream);
+    });
+}
+
+// A launch has up to 1024 threads for every sequence and KV head, and holds 2^32.
+static int check_items(int64_t seqs, int64_t Hkv) { return seqs * Hkv >> 22 ? MXATTN_ERR_SHAPE : MXATTN_OK; }
+
+int mxattn_cache_select(const float* weights, int64_t pages, int64_t page_tokens, const int32_t* page_table,
+                        const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t Hkv, int64_t budget, int64_t sinks,
+                        int64_t recent, int32_t* kept, int32_t* counts, void* stream) {
+    if (!weights || !page_table || !kv_len || !kept || !counts) return MXATTN_ERR_NULL;
+    mxattn::SelectArgs a{};
+    if (int st = check_pages(a.c, pages, page_tokens, page_table, seqs, max_pages, 1, Hkv)) return st;
+    if (int st = check_items(seqs, Hkv)) return st;
+    if (budget < 1 || budget > mxattn::kMaxKeys || sinks < 0 || recent < 0 || sinks > budget || recent > budget - sinks)
+        return MXATTN_ERR_VALUE;
+    if (!aligned(weights, 4) || !aligned(kv_len, 4) || !aligned(kept, 4) || !aligned(counts, 4)) return MXATTN_ERR_ALIGN;
+    const size_t kb = (size_t)seqs * (size_t)Hkv * (size_t)budget * 4, cb = (size_t)seqs * 4, wb = weights_bytes(a.c);
+    const size_t tb = (size_t)seqs * (size_t)max_pages * 4;
+    if (overlaps(kept, kb, weights, wb) || overlaps(kept, kb, counts, cb) || overlaps(kept, kb, kv_len, cb) ||
+        overlaps(kept, kb, page_table, tb) || overlaps(counts, cb, weights, wb) || overlaps(counts, cb, kv_len, cb) ||
+        overlaps(counts, cb, page_table, tb))
+        return MXATTN_ERR_SHAPE;
+    a.c.kv_len = kv_len;
+    a.weights = weights;
+    a.budget = (int)budget;
+    a.sinks = (int)sinks;
+    a.recent = (int)recent;
+    a.kept = kept;
+    a.counts = counts;
+    hipError_t e = mxattn::launch_cache_select(a, reinterpret_cast<hipStream_t>(stream));
     if (e != hipSuccess) {
-        set_error("cache attention launch", e);
-        st = MXATTN_ERR_HIP;
+        set_error("cache selection launch", e);
+        return MXATTN_ERR_HIP;
     }
-    return bytes ? ws.give_back(st) : st;
+    return MXATTN_OK;
+}
+
+int mxattn_cache_compact(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int64_t pages,
+                         int64_t page_tokens, const int32_t* page_table, int64_t seqs, int64_t max_pages,
+                         const int32_t* out_table, int64_t out_pages, int64_t Hkv, int64_t d, const int32_t* kept,
+                         int64_t kept_heads, int64_t width, const int32_t* counts, const int32_t* base, float* weights,
+                         void* stream) {
+    if (!k_codes || !k_scales || !v_codes || !v_scales || !page_table || !kept || !counts) return MXATTN_ERR_NULL;
+    mxattn::CompactArgs a{};
+    if (int st = check_shape(1, 1, 1, d)) return st;
+    if (int st = check_pages(a.c, pages, page_tokens, page_table, seqs, max_pages, 1, Hkv)) return st;
+    if (int st = check_items(seqs, Hkv)) return st;
+    if (out_table && (out_pages < 1 || out_pages > mxattn::kMaxKeys / page_tokens)) return MXATTN_ERR_SHAPE;
+    if ((kept_heads != 1 && kept_heads != Hkv) || width < 1 || width > mxattn::kMaxKeys) return MXATTN_ERR_SHAPE;
+    if (int st = check_codes(a.c, k_codes, k_scales, v_codes, v_scales)) return st;
+    if (!aligned(out_table, 4) || !aligned(kept, 4) || !aligned(counts, 4) || !aligned(base, 4) || !aligned(weights, 4))
+        return MXATTN_ERR_ALIGN;
+    const size_t wb = weights_bytes(a.c);
+    if (weights && in_cache(weights, wb, a.c)) return MXATTN_ERR_SHAPE;
+    a.in_place = !out_table || out_table == page_table;
+    a.out_table = out_table ? out_table : page_table;
+    a.out_pages = (int)(out_table ? out_pages : max_pages);
+    a.kept = kept;
+    a.kept_head = kept_heads == 1 ? 0 : width;
+    a.kept_seq = kept_heads * width;
+    a.width = (int)width;
+    a.counts = counts;
+    a.base = base;
+    a.weights = weights;
+    hipError_t e = mxattn::launch_cache_compact(a, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) {
+        set_error("cache compaction launch", e);
+        return MXATTN_ERR_HIP;
+    }
+    return MXATTN_OK;
 }
 
 }  // extern "C"

@@ -59,6 +59,15 @@ struct AppendArgs {
 };
 hipError_t launch_cache_append(const AppendArgs& a, bool halves, hipStream_t stream);
 
+// What a call of attention over the cache sees and leaves beside its output.
+enum AttendKind {
+    kPlain,       // all keys, or causal
+    kWindow,      // of those the last `window` and the first `sinks`
+    kTree,        // what was there before, and of the new keys those of a row's mask
+    kWeigh,       // as kPlain, and every row's scores and softmax statistics are kept
+    kWeighStats,  // as kPlain, and the statistics alone
+};
+
 struct CacheAttendArgs {
     CacheArgs c;
     const uint16_t* q;  // [tokens, Hq, 128] by its token stride
@@ -69,11 +78,56 @@ struct CacheAttendArgs {
     int causal;
     float scale;        // log2(e) / sqrt(128)
     uint8_t* workspace; // cache_attend_workspace bytes
+    AttendKind kind;
+    int window, sinks;           // kWindow: at most kMaxKeys each, window >= 1
+    const int32_t* tree;         // kTree: [tokens, tree_words]
+    int tree_words;
+    int most_keys;               // kWeigh, kWeighStats: a longer sequence is none
+    float2* stats;               // [tokens * Hq]: m and 1 / l of every row, p = exp2(s c - m) / l
+    float* scores;               // kWeigh: [tokens * Hq, score_stride], s c of the keys that a tile of rows sees
+    int64_t score_stride;        // a multiple of 32
 };
 // max_q, max_kv: most new tokens and keys of a sequence, as far as the caller knows
 // (wrong ones cost time, and may change where f16 and fp32 round).
 size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv);
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream);
+// Whether such a call's kernel can keep the scores (kWeigh; else kWeighStats).
+bool cache_attend_keeps_scores(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv);
+
+// Attention that also adds to every key's weight (cache_weigh.hip); a.kind and what
+// follows it are chosen by the call.
+struct CacheWeighArgs {
+    CacheAttendArgs a;
+    const float* before;  // [pages, heads, page_tokens]; null: zeros
+    float* after;
+};
+size_t cache_weigh_workspace(CacheAttendArgs a, int64_t max_q, int64_t max_kv);
+hipError_t launch_cache_weigh(CacheWeighArgs w, int64_t max_q, int64_t max_kv, hipStream_t stream);
+
+// Which tokens stay, and moving them together (cache_evict.hip).
+struct SelectArgs {
+    CacheArgs c;           // pages, table and lengths alone
+    const float* weights;  // [pages, heads, page_tokens]
+    int budget, sinks, recent;
+    int32_t* kept;         // [seqs, heads, budget]
+    int32_t* counts;       // [seqs]
+};
+hipError_t launch_cache_select(const SelectArgs& a, hipStream_t stream);
+
+struct CompactArgs {
+    CacheArgs c;               // (no q_start and kv_len)
+    const int32_t* out_table;  // [seqs, out_pages]: where the tokens go
+    int out_pages;
+    bool in_place;             // out_table is the page table
+    const int32_t* kept;       // [seqs, heads or 1, width]
+    int64_t kept_head;         // elements from head to head
+    int64_t kept_seq;          // from sequence to sequence
+    int width;
+    const int32_t* counts;     // [seqs]
+    const int32_t* base;       // [seqs] or null: 0
+    float* weights;            // [pages, heads, page_tokens] or null
+};
+hipError_t launch_cache_compact(const CompactArgs& a, hipStream_t stream);
 
 // Tiles of 128 query rows (cache_attend_tiles.hip).
 size_t cache_attend_tiles_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv);

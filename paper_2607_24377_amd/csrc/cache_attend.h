@@ -34,6 +34,7 @@ namespace mxattn {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
@@ -125,6 +126,78 @@ __device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QOperan
     s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k0, q.hi[0], s, 0, 0, 0, e, 0, kOne);
     s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k1, q.hi[1], s, 0, 0, 0, e, 0, kOne);
     return s;
+}
+
+// Q as it is, for scores that are kept or computed again as weights: the FP8 matrix cores
+// keep too few digits of the products that they add up (their sums are off by up to 2^-15
+// of sum |q k|, measured, so probabilities by 1e-5; beside the rounding of P and O that does
+// not count).  K's codes are exact in bf16 and bf16 products are added in fp32 (2^-24), in
+// the time of the two FP8 products and 32 conversions a block, for which attention of a
+// few rows has room.  The operands' channels in the order of the FP8 ones.
+struct QExact {
+    uint4 r[2][4];
+    float c;  // as QOperand's
+};
+
+__device__ __forceinline__ QExact load_q_exact(const uint16_t* row, int h, float scale, bool live) {
+    QExact q;
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            q.r[j][k] = live ? *reinterpret_cast<const uint4*>(row + 64 * j + 32 * h + 8 * k) : make_uint4(0, 0, 0, 0);
+            m = max_halves(m, q.r[j][k]);
+        }
+    m = max(m & 0xFFFFu, m >> 16);
+    m = max(m, __builtin_bit_cast(uint32_t, other_half(__builtin_bit_cast(float, m))));
+    q.c = m < 0x7F80u ? scale : __builtin_nanf("");
+    return q;
+}
+
+// Eight codes of a key as bf16, times the scale.
+__device__ __forceinline__ bf16x8 to_bf16(uint32_t a, uint32_t b, float scale) {
+    const bf16x2 w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
+    const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    const bf16x2 y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
+    const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+    return bf16x8{w[0], w[1], x[0], x[1], y[0], y[1], z[0], z[1]};
+}
+
+// A block of K as the operands of eight products (of 16 channels each).
+struct KExact {
+    bf16x8 k[8];
+};
+__device__ __forceinline__ KExact exact_keys(const uint4 (&k)[4], int e) {
+    KExact x;
+    const float scale = e8m0_as_f32((uint32_t)e);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        x.k[2 * i] = to_bf16(k[i].x, k[i].y, scale);
+        x.k[2 * i + 1] = to_bf16(k[i].z, k[i].w, scale);
+    }
+    return x;
+}
+
+__device__ __forceinline__ v16f scores(const KExact& k, int e, const QExact& q) {
+    v16f s;
+    const float zero = e == 255 ? __builtin_nanf("") : 0.f;  // a scale that is no number: nor is any score
+#pragma unroll
+    for (int i = 0; i < 16; i++) s[i] = zero;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.k[i], __builtin_bit_cast(bf16x8, q.r[i >> 2][i & 3]), s, 0, 0, 0);
+    return s;
+}
+__device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QExact& q) { return scores(exact_keys(k, e), e, q); }
+
+// Q as the kernels of a kind take it.
+template <AttendKind kKind>
+__device__ __forceinline__ auto load_q_of(const uint16_t* row, int h, float scale, bool live) {
+    if constexpr (kKind == kWeigh)
+        return load_q_exact(row, h, scale, live);
+    else
+        return load_q(row, h, scale, live);
 }
 
 // Eight codes (8 keys of a channel) as f16, times the scale.
@@ -257,13 +330,24 @@ struct State {
 // Bytes of v that are NaN codes, as 0x80 in each.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t v) { return ((v & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
+// The keys of a block that the lane's row sees: its first ones, or those of a mask.
+struct Below {
+    int n;
+    __device__ __forceinline__ bool operator()(int key) const { return key < n; }
+};
+struct Bits {
+    uint32_t b;
+    __device__ __forceinline__ bool operator()(int key) const { return (b >> key) & 1u; }
+};
+
 // A block that only some rows see and that holds NaN codes of V: a masked key
 // has p = 0, and 0 * NaN would reach every row.  The codes are taken out, and
 // the rows that see one get NaN: its count, from a product of ones.
-__device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], int visible, int h) {
+template <class Mask>
+__device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], const Mask& sees, int h) {
     f16x8 seen[2];
 #pragma unroll
-    for (int i = 0; i < 16; i++) seen[i >> 3][i & 7] = 16 * h + i < visible ? (_Float16)1.f : (_Float16)0.f;
+    for (int i = 0; i < 16; i++) seen[i >> 3][i & 7] = sees(16 * h + i) ? (_Float16)1.f : (_Float16)0.f;
 #pragma unroll
     for (int n = 0; n < 4; n++) {
         uint32_t* x = reinterpret_cast<uint32_t*>(&v[n]);
@@ -291,11 +375,10 @@ __device__ __forceinline__ bool has_nan(const uint4 (&v)[4]) {
     return m != 0;
 }
 
-// V's codes and scale byte of a block whose keys not every row sees, or of no page:
-// `base` is its first key's place where the lane's row sees `visible` keys and the
-// sequence holds `held`.
-__device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int& e, int base, int visible, int held, bool lost,
-                                             int h) {
+// V's codes and scale byte of a block whose keys not every row sees, or of no page; the
+// sequence holds the first `held` of its keys.
+template <class Mask>
+__device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int& e, const Mask& sees, int held, bool lost, int h) {
     const bool none = !lost && e == 255;  // a scale that is no number: nor is any value
     if (lost || none) e = 127;            // (a zero code times that scale is NaN too)
 #pragma unroll
@@ -305,20 +388,20 @@ __device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int& e, i
         for (int j = 0; j < 4; j++) {
             if (none) w[j] = 0x7F7F7F7Fu;
             // what lies behind the last key may be anything: zero
-            const int left = lost ? 0 : held - base - 16 * h - 4 * j;
+            const int left = lost ? 0 : held - 16 * h - 4 * j;
             w[j] &= left <= 0 ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1;
         }
     }
-    if (__any(has_nan(v))) spread_nan(st, v, visible - base, h);
+    if (__any(has_nan(v))) spread_nan(st, v, sees, h);
 }
 
-// Softmax of a block's scores and their product with V of scale byte `e`; `visible`:
-// keys of the block that the lane's row sees (its first ones), `any`: some row does
-// not see all.
-__device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], int e, float c, int visible, bool any, int h) {
+// Softmax of a block's scores and their product with V of scale byte `e`; `sees`: the
+// keys of the block that the lane's row sees, `any`: some row does not see all.
+template <class Mask>
+__device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], int e, float c, const Mask& sees, bool any, int h) {
     if (any) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) s[i] = 16 * h + i < visible ? s[i] : -__builtin_inff();
+        for (int i = 0; i < 16; i++) s[i] = sees(16 * h + i) ? s[i] : -__builtin_inff();
     }
     float mx = max2(max2(s[0], s[1]), s[2]);
 #pragma unroll
@@ -337,14 +420,113 @@ __device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], int e,
     }
 }
 
-// One block for the wave's rows: `end` keys are the lane's row's, `keys` the
-// sequence's, `base` the block's first; `any`: some row does not see all of it.
-__device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand& q, int base, int end, int keys, bool any,
-                                             int h) {
-    if (any || x.lost) clean_values(st, x.v, x.ve, 0, end - base, keys - base, x.lost, h);
-    if (x.lost && end > base) st.l = __builtin_nanf("");  // no such page: NaN for the rows that would see it
+// What the lane's row sees (end and, by kind, what follows), and the blocks that the rows
+// of the wave or workgroup walk: those of the sinks, then those from the first row's
+// window or from the start on, to the end of the last row.
+template <AttendKind kKind>
+struct Sight {
+    int end, keys;         // the row's keys end here; the sequence's
+    int min_end;           // the end of the first row
+    int low, max_low;      // kWindow: where the row's and the last row's window begin
+    int sinks;
+    const int32_t* mask;   // kTree: the row's
+    int words, past;
+    int near, skip, count; // kWindow: blocks of the sinks, blocks left out after them; the blocks to walk
+
+    // Row `row` of the n * group rows of a sequence of `keys_` keys; rows row0 .. last are
+    // walked together.
+    __device__ __forceinline__ Sight(const CacheAttendArgs& a, int first, int n, int keys_, int row, int row0, int last) {
+        keys = keys_;
+        past = keys - n;
+        const bool causal = kKind != kTree && a.causal;
+        end = causal ? past + token_of(a, row) + 1 : keys;
+        min_end = causal ? past + token_of(a, row0) + 1 : keys;
+        const int max_end = max(0, causal ? past + token_of(a, last) + 1 : keys);
+        count = (max_end + kBlockTokens - 1) / kBlockTokens;
+        if constexpr (kKind == kWindow) {
+            sinks = a.sinks;
+            low = end - a.window;
+            max_low = max_end - a.window;
+            near = (min(sinks, max_end) + kBlockTokens - 1) / kBlockTokens;
+            const int from = max(near, max(0, min_end - a.window) / kBlockTokens);
+            skip = from - near;
+            count = near + max(0, count - from);
+        }
+        if constexpr (kKind == kTree) {
+            words = a.tree_words;
+            mask = a.tree + (int64_t)(first + token_of(a, row)) * words;
+        }
+    }
+    // Whether the row sees any key.
+    __device__ __forceinline__ bool some() const {
+        if constexpr (kKind == kTree) {
+            if (past > 0 || keys <= 0) return keys > 0;
+            uint32_t any = 0;
+            for (int b = 0; b < count; b++) any |= bits(b * kBlockTokens);
+            return any != 0;
+        }
+        return end > 0;
+    }
+    // The block at place v of the walk.
+    __device__ __forceinline__ int block(int v) const {
+        if constexpr (kKind == kWindow) return v < near ? v : v + skip;
+        return v;
+    }
+    // Whether some row may not see all of the block at `base` (of a wave: the same for all
+    // its lanes).
+    __device__ __forceinline__ bool partial(int base) const {
+        if constexpr (kKind == kTree) return base + kBlockTokens > past;
+        if constexpr (kKind == kWindow)
+            return base + kBlockTokens > min_end || (base < max_low && base + kBlockTokens > sinks);
+        return base + kBlockTokens > min_end;
+    }
+    // The keys of the block at `base` that the row sees, as bits.
+    __device__ __forceinline__ uint32_t bits(int base) const {
+        const uint32_t held = ones(min(end, keys) - base);
+        if constexpr (kKind == kWindow) return held & (ones(sinks - base) | ~ones(low - base));
+        if constexpr (kKind == kTree) {
+            const int off = base - past;  // the first key's place among the drafts
+            if (off <= -kBlockTokens) return held;
+            const int w = off >> 5, r = off & 31;  // (off < 0: word -1 is what was there before)
+            const uint32_t lo = w < 0 ? ~0u : w < words ? (uint32_t)mask[w] : 0u;
+            const uint32_t hi = w + 1 < words ? (uint32_t)mask[w + 1] : 0u;
+            return held & (uint32_t)((((uint64_t)hi << 32) | lo) >> r);
+        }
+        return held;
+    }
+    static __device__ __forceinline__ uint32_t ones(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+    // The mask of the block at `base`.
+    __device__ __forceinline__ auto mask_of(int base, bool any) const {
+        if constexpr (kKind == kWindow || kKind == kTree)
+            return Bits{any ? bits(base) : ~0u};
+        else
+            return Below{end - base};
+    }
+};
+
+// One block for the wave's rows at `base`; `scores_at`: where the row's scores are kept
+// (kWeigh; null: nowhere).
+template <AttendKind kKind, class Q>
+__device__ __forceinline__ void attend_block(State& st, Block& x, const Q& q, int base, const Sight<kKind>& sight,
+                                             float* scores_at, int h) {
+    const bool any = sight.partial(base);
+    const auto sees = sight.mask_of(base, any);
+    if (any || x.lost) clean_values(st, x.v, x.ve, sees, sight.keys - base, x.lost, h);
+    if constexpr (kKind == kWindow || kKind == kTree) {
+        if (x.lost && sees.b) st.l = __builtin_nanf("");
+    } else {
+        if (x.lost && sight.end > base) st.l = __builtin_nanf("");  // no such page: NaN for the rows that would see it
+    }
     const v16f s = scores(x.k, x.ke, q);
-    consume(st, s, x.v, x.ve, q.c, end - base, any, h);
+    if constexpr (kKind == kWeigh) {
+        if (scores_at) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4*>(scores_at + base + 16 * h + i) =
+                    make_float4(s[i] * q.c, s[i + 1] * q.c, s[i + 2] * q.c, s[i + 3] * q.c);
+        }
+    }
+    consume(st, s, x.v, x.ve, q.c, sees, any, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -359,6 +541,34 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const QOperand
 __device__ __forceinline__ int keys_of(const CacheArgs& c, int s) {
     const int len = c.kv_len[s];
     return (unsigned)len > (unsigned)((c.max_pages << c.bpp_log2) * kBlockTokens) ? -1 : len;
+}
+template <AttendKind kKind>
+__device__ __forceinline__ int keys_of(const CacheAttendArgs& a, int s) {
+    const int len = keys_of(a.c, s);
+    if constexpr (kKind == kWeigh || kKind == kWeighStats) return len > a.most_keys ? -1 : len;
+    return len;
+}
+
+// Blocks that a tile of `rows` rows of a sequence walks at most (Sight::count).
+template <AttendKind kKind>
+__device__ __forceinline__ int most_blocks(const CacheAttendArgs& a, int keys, int rows) {
+    const int all = (max(keys, 1) + kBlockTokens - 1) / kBlockTokens;
+    if constexpr (kKind == kWindow) {
+        // the tile's tokens but one move the window on
+        const int seen = a.window + (a.causal ? (rows + a.group - 2) / a.group : 0);
+        return min(all, (a.sinks + kBlockTokens - 1) / kBlockTokens + (seen + kBlockTokens - 2) / kBlockTokens + 1);
+    }
+    return all;
+}
+
+// Where a row's statistics and scores lie: its token and head.
+__device__ __forceinline__ int64_t row_number(const CacheAttendArgs& a, int64_t first, int row, int head) {
+    const int token = token_of(a, row);
+    return ((first + token) * a.c.heads + head) * a.group + (row - token * a.group);
+}
+// m and 1 / l, 0 for a row without keys.
+__device__ __forceinline__ float2 statistics(float m, float l) {
+    return l == 0.f ? make_float2(0.f, 0.f) : make_float2(m, 1.0f / l);
 }
 
 // Tiles of a sequence are numbered from here on: no two sequences' overlap, whatever
@@ -460,7 +670,7 @@ __device__ __forceinline__ void store_part(const State& st, float l, const Parts
 
 // Joins the parts of item blockIdx.x in the order of its keys: a row per workgroup
 // and turn, whose eight groups of 32 lanes take every eighth part.
-template <int kRows>
+template <int kRows, AttendKind kKind>
 __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs a, int shares) {
     __shared__ float4 s_o[8][32];
     __shared__ float s_m[8], s_l[8];
@@ -477,7 +687,7 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
     if (rows <= 0) return;
     const int count = info.last - info.first + 1;
     auto slot = [&info](int p) { return p ? 2 * (info.first + p) : 2 * info.first + 1; };
-    const bool bad = keys_of(a.c, s) < 0;
+    const bool bad = keys_of<kKind>(a, s) < 0;
     const int g = tid >> 5, ch = 4 * (tid & 31);
     // the parts from p0 on, every `step`th, four in flight
     auto gather = [&](int r, int p0, int step, float& m, float& l, float4& o) {
@@ -507,7 +717,9 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
             }
         }
     };
-    auto finish = [&](int r, const float4& o) {
+    auto finish = [&](int r, float m, float l, const float4& o) {
+        if constexpr (kKind == kWeigh || kKind == kWeighStats)
+            if (ch == 0) a.stats[row_number(a, range.first, row0 + r, head)] = statistics(m, l);
         *reinterpret_cast<uint2*>(a.out + row_offset(a, range.first, row0 + r, head, a.out_stride) + ch) = finished(o, bad);
     };
     float m, l;
@@ -515,7 +727,7 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
     if (count <= 8) {  // a row for each group (128 items of 8 parts and 32 rows 9.8 us, by all groups 12.1)
         for (int r = 8 * blockIdx.y + g; r < rows; r += 8 * gridDim.y) {
             gather(r, 0, 1, m, l, o);
-            finish(r, o);
+            finish(r, m, l, o);
         }
         return;
     }
@@ -536,18 +748,18 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendArgs 
             o = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < 8; k++)
                 add_scaled(o, s_o[k][tid & 31], s_l[k] * __builtin_amdgcn_exp2f(s_m[k] - m) * inv);
-            finish(r, o);
+            finish(r, m, l, o);
         }
         __syncthreads();
     }
 }
 
-template <int kRows>
+template <int kRows, AttendKind kKind>
 inline hipError_t launch_cache_attend_join(const CacheAttendArgs& a, int shares, hipStream_t stream) {
     const int64_t items = tile_numbers<kRows>(a) * a.c.heads;
     // a row each, or eight where that is a workgroup for every one of 2048 slots
     const int64_t rows = items >= 2048 / (kRows / 8) ? kRows / 8 : kRows;
-    cache_attend_join_kernel<kRows><<<dim3((unsigned)items, (unsigned)rows), 256, 0, stream>>>(a, shares);
+    cache_attend_join_kernel<kRows, kKind><<<dim3((unsigned)items, (unsigned)rows), 256, 0, stream>>>(a, shares);
     return hipGetLastError();
 }
 

@@ -15,6 +15,8 @@
 // pages, codes).
 #include "cache_attend.h"
 
+#include <algorithm>
+
 namespace mxattn {
 namespace {
 
@@ -46,6 +48,7 @@ struct Cut {
 };
 
 // A sequence as the shares see it.
+template <AttendKind kKind>
 struct Sequence {
     int first, n;   // its tokens in the call
     int keys;       // -1: an impossible length
@@ -55,45 +58,53 @@ struct Sequence {
         const TokenRange r = token_range(a.c, s);
         first = r.first;
         n = r.last - r.first;
-        keys = keys_of(a.c, s);
+        keys = keys_of<kKind>(a, s);
         tiles = (n * a.group + kRows - 1) / kRows;
-        const int blocks = (max(keys, 1) + kBlockTokens - 1) / kBlockTokens;
-        units = (uint32_t)((blocks + (1 << unit) - 1) >> unit);
+        units = (uint32_t)((most_blocks<kKind>(a, keys, kRows) + (1 << unit) - 1) >> unit);
     }
     __device__ __forceinline__ uint32_t all(int heads) const { return (uint32_t)tiles * (uint32_t)heads * units; }
 };
 
-// A wave's rows of a tile.
+// A wave's rows of a tile, and what they see.
+template <AttendKind kKind>
 struct Rows {
-    int count, row, end, min_end, max_end;  // this lane's row and the keys that it, the first and the last row see
-    __device__ __forceinline__ Rows(const CacheAttendArgs& a, int n, int keys, int row0, int q) {
-        count = min(kRows, n * a.group - row0);
-        row = row0 + min(q, count - 1);
-        end = a.causal ? keys - n + token_of(a, row) + 1 : keys;
-        min_end = a.causal ? keys - n + token_of(a, row0) + 1 : keys;
-        max_end = max(0, a.causal ? keys - n + token_of(a, row0 + count - 1) + 1 : keys);
-    }
+    int count, row;  // this lane's row
+    Sight<kKind> sight;
+    __device__ __forceinline__ Rows(const CacheAttendArgs& a, int first, int n, int keys, int row0, int q)
+        : count(min(kRows, n * a.group - row0)),
+          row(row0 + min(q, count - 1)),
+          sight(a, first, n, keys, row, row0, row0 + count - 1) {}
 };
 
-// Blocks b0, b0 + step, ... below b1 for the wave's rows, the next one in flight while
-// one is worked on.  (Two in flight through LDS gained nothing, and three copies of
-// this loop's body in the instruction cache cost the short calls.)
-__device__ __forceinline__ void attend_run(State& st, const CacheArgs& c, int s, int head, int b0, int b1, int step,
-                                           const QOperand& qo, const Rows& r, int keys, int q, int h) {
-    if (b0 >= b1) return;
-    const int last = b1 - 1;
+// Places v0, v0 + step, ... below v1 of the walk of the wave's rows, the next block in
+// flight while one is worked on.  (Two in flight through LDS gained nothing, and three
+// copies of this loop's body in the instruction cache cost the short calls.)
+template <AttendKind kKind, class Q>
+__device__ __forceinline__ void attend_run(State& st, const CacheArgs& c, int s, int head, int v0, int v1, int step,
+                                           const Q& qo, const Sight<kKind>& sight, float* scores_at, int q, int h) {
+    if (v0 >= v1) return;
+    const int last = v1 - 1;
     Block x, y;
-    load_block(x, c, block_at(c, page_of(c, s, b0), head, b0), q, h);
-    int page = page_of(c, s, min(b0 + step, last));
-    for (int b = b0;; b += step) {
-        if (b + step < b1) {
-            load_block(y, c, block_at(c, page, head, b + step), q, h);
-            page = page_of(c, s, min(b + 2 * step, last));
+    load_block(x, c, block_at(c, page_of(c, s, sight.block(v0)), head, sight.block(v0)), q, h);
+    int page = page_of(c, s, sight.block(min(v0 + step, last)));
+    for (int v = v0;; v += step) {
+        if (v + step < v1) {
+            load_block(y, c, block_at(c, page, head, sight.block(v + step)), q, h);
+            page = page_of(c, s, sight.block(min(v + 2 * step, last)));
         }
-        attend_block(st, x, qo, b * kBlockTokens, r.end, keys, (b + 1) * kBlockTokens > r.min_end, h);
-        if (b + step >= b1) break;
+        attend_block<kKind>(st, x, qo, sight.block(v) * kBlockTokens, sight, scores_at, h);
+        if (v + step >= v1) break;
         x = y;
     }
+}
+
+// Where the scores of this lane's row are kept; null: nowhere.
+template <AttendKind kKind>
+__device__ __forceinline__ float* scores_of(const CacheAttendArgs& a, int64_t first, int row, int head, bool live) {
+    if constexpr (kKind == kWeigh)
+        return live ? a.scores + row_number(a, first, row, head) * a.score_stride : nullptr;
+    else
+        return nullptr;
 }
 
 // Where a share begins.
@@ -103,6 +114,7 @@ struct Start {
     int s;
 };
 
+template <AttendKind kKind>
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheAttendArgs a, int log2, int unit) {
     __shared__ uint32_t s_sum[kWaves];
     __shared__ bool s_ascend[kWaves];
@@ -117,7 +129,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
     uint32_t mine = 0;
     bool ascend = true;
     for (int s = s0; s < s1; s++) {
-        mine += Sequence(a, s, unit).all(c.heads);
+        mine += Sequence<kKind>(a, s, unit).all(c.heads);
         ascend = ascend && starts_ascend(c, s);
     }
     uint32_t incl = mine;
@@ -150,7 +162,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
         if (lo < hi && before <= lo && lo < before + mine) {
             uint32_t at = before;
             for (int s = s0; s < s1; s++) {
-                const uint32_t all = Sequence(a, s, unit).all(c.heads);
+                const uint32_t all = Sequence<kKind>(a, s, unit).all(c.heads);
                 if (lo < at + all) {
                     s_start[k] = {lo, hi, lo - at, s};
                     break;
@@ -167,7 +179,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
     int s = __builtin_amdgcn_readfirstlane(s_start[wave].s);
     const Parts<kRows> parts(a.workspace, 1 << log2);
     if (at < end) {
-        Sequence seq(a, s, unit);
+        Sequence<kKind> seq(a, s, unit);
         const uint32_t per_head = (uint32_t)seq.tiles * seq.units;
         int head = __builtin_amdgcn_readfirstlane((int)(offset / per_head));
         int tile = __builtin_amdgcn_readfirstlane((int)((offset - head * per_head) / seq.units));
@@ -175,17 +187,20 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
         while (true) {
             const uint32_t x1 = min(seq.units, x0 + (end - at));
             const int keys = max(seq.keys, 0);
-            const Rows r(a, seq.n, keys, tile * kRows, q);
-            const int blocks = (r.max_end + kBlockTokens - 1) / kBlockTokens;
-            const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale,
-                                       q < r.count && r.end > 0);
+            const Rows<kKind> r(a, seq.first, seq.n, keys, tile * kRows, q);
+            const int blocks = r.sight.count;
+            const auto qo = load_q_of<kKind>(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale,
+                                       q < r.count && r.sight.some());
             State st;
             st.clear();
-            attend_run(st, c, s, head, min((int)(x0 << unit), blocks), min((int)(x1 << unit), blocks), 1, qo, r, keys, q, h);
+            attend_run<kKind>(st, c, s, head, min((int)(x0 << unit), blocks), min((int)(x1 << unit), blocks), 1, qo, r.sight,
+                              scores_of<kKind>(a, seq.first, r.row, head, q < r.count), q, h);
             const float l = st.l + other_half(st.l);
             const bool whole = x0 == 0 && x1 == seq.units;
             if (q < r.count) {
                 if (whole) {
+                    if constexpr (kKind == kWeigh || kKind == kWeighStats)
+                        if (h == 0) a.stats[row_number(a, seq.first, r.row, head)] = statistics(st.m, l);
                     store_row(st, inverse(l, seq.keys < 0), a.out + row_offset(a, seq.first, r.row, head, a.out_stride), h);
                 } else {
                     store_part(st, l, parts, (2 * index + (x0 == 0)) * kRows + q, h);
@@ -203,7 +218,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
                     head = 0;
                     do {  // (there is a next one, unless q_start was written meanwhile)
                         if (++s >= c.seqs) return;
-                        seq = Sequence(a, s, unit);
+                        seq = Sequence<kKind>(a, s, unit);
                     } while (seq.tiles == 0);
                 }
             }
@@ -213,6 +228,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_shares_kernel(CacheA
 
 // One workgroup per item, numbered as the workgroups of the append: sequence s has
 // tiles q_start[s] * group / 32 + s onwards.  A wave takes every fourth block.
+template <AttendKind kKind>
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAttendArgs a) {
     __shared__ __align__(16) uint8_t s_o[kWaves][kRows * 512];
     __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
@@ -221,16 +237,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
     const int lane = tid & 63, q = lane & 31, h = lane >> 5;
     const int s = __builtin_amdgcn_readfirstlane(owner_of(c, blockIdx.x, a.group, kRows, 1)), head = blockIdx.y;
     if (s < 0) return;
-    const Sequence seq(a, s, 0);
+    const Sequence<kKind> seq(a, s, 0);
     const int row0 = ((int)blockIdx.x - tile_number<kRows>(a, seq.first, s)) * kRows;
     if (row0 >= seq.n * a.group) return;
     const int keys = max(seq.keys, 0);
-    const Rows r(a, seq.n, keys, row0, q);
-    const QOperand qo = load_q(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale,
-                               q < r.count && r.end > 0);
+    const Rows<kKind> r(a, seq.first, seq.n, keys, row0, q);
+    const auto qo = load_q_of<kKind>(a.q + row_offset(a, seq.first, r.row, head, a.q_stride), h, a.scale,
+                               q < r.count && r.sight.some());
     State st;
     st.clear();
-    attend_run(st, c, s, head, wave, (r.max_end + kBlockTokens - 1) / kBlockTokens, kWaves, qo, r, keys, q, h);
+    attend_run<kKind>(st, c, s, head, wave, r.sight.count, kWaves, qo, r.sight,
+                      scores_of<kKind>(a, seq.first, r.row, head, q < r.count), q, h);
     // the 16-byte chunks of a row in an order of its own, so that rows written at once lie
     // in other banks
     auto o_at = [&](int w, int row, int chunk) { return s_o[w] + row * 512 + (chunk ^ row) * 16; };
@@ -259,6 +276,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
             f[w] = s_l[w][i] * __builtin_amdgcn_exp2f(s_m[w][i] - m);
             sum += f[w];
         }
+        if constexpr (kKind == kWeigh || kKind == kWeighStats)
+            if (ch == 0) a.stats[row_number(a, seq.first, row0 + i, head)] = statistics(m, sum);
         const float inv = reciprocal(sum);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -268,8 +287,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
     }
 }
 
-// Which kernel, from the caller's bounds on a sequence's query rows per KV head and its
-// keys (us, kernels with their joins; 8 KV heads):
+// Which kernel, from the caller's bounds on a sequence's query rows per KV head and the
+// keys that a row sees (us, kernels with their joins; 8 KV heads):
 //   few keys: an item is one workgroup's.  16 sequences x 5 rows x 1000 keys 13.6, in
 //   shares 18.2; one sequence's row over 2000 keys 16.7 and 14.3.  Up to 128 rows: 90
 //   rows x 290 keys 8.5, in shares 18.8, in tiles of 128 rows 33.
@@ -297,9 +316,31 @@ int shares_log2(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
     return log2;
 }
 
+// The keys that a row sees, at most.
+int64_t seen_keys(const CacheAttendArgs& a, int64_t max_kv) {
+    return a.kind == kWindow ? std::min<int64_t>(max_kv, (int64_t)a.window + a.sinks) : max_kv;
+}
+
+template <AttendKind kKind>
+hipError_t launch(const CacheAttendArgs& a, Way w, int64_t max_q, int64_t max_kv, hipStream_t stream) {
+    const int64_t tiles = tile_numbers<kRows>(a);
+    if (w == kItems) {
+        cache_attend_items_kernel<kKind><<<dim3((unsigned)tiles, (unsigned)a.c.heads), kThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    // units that keep the total of all items within 31 bits, however long the sequences are
+    int unit = 0;
+    while ((tiles * a.c.heads * ((((int64_t)a.c.max_pages << a.c.bpp_log2) >> unit) + 1)) >> 31) unit++;
+    const int log2 = shares_log2(a, max_q, max_kv);
+    cache_attend_shares_kernel<kKind><<<(1 << log2) / kWaves, kThreads, 0, stream>>>(a, log2, unit);
+    if (hipError_t e = hipGetLastError()) return e;
+    return launch_cache_attend_join<kRows, kKind>(a, 1 << log2, stream);
+}
+
 }  // namespace
 
 size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    max_kv = seen_keys(a, max_kv);
     switch (way(a, max_q, max_kv)) {
         case kItems: return 0;
         case kShares: return parts_bytes<kRows>(a, 1 << shares_log2(a, max_q, max_kv));
@@ -307,21 +348,21 @@ size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t m
     }
 }
 
+bool cache_attend_keeps_scores(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    return way(a, max_q, max_kv) != kTiles;
+}
+
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream) {
+    max_kv = seen_keys(a, max_kv);
     const Way w = way(a, max_q, max_kv);
     if (w == kTiles) return launch_cache_attend_tiles(a, max_q, max_kv, stream);
-    const int64_t tiles = tile_numbers<kRows>(a);
-    if (w == kItems) {
-        cache_attend_items_kernel<<<dim3((unsigned)tiles, (unsigned)a.c.heads), kThreads, 0, stream>>>(a);
-        return hipGetLastError();
+    switch (a.kind) {
+        case kWindow: return launch<kWindow>(a, w, max_q, max_kv, stream);
+        case kTree: return launch<kTree>(a, w, max_q, max_kv, stream);
+        case kWeigh: return launch<kWeigh>(a, w, max_q, max_kv, stream);
+        case kWeighStats: return launch<kWeighStats>(a, w, max_q, max_kv, stream);
+        default: return launch<kPlain>(a, w, max_q, max_kv, stream);
     }
-    // units that keep the total of all items within 31 bits, however long the sequences are
-    int unit = 0;
-    while ((tiles * a.c.heads * ((((int64_t)a.c.max_pages << a.c.bpp_log2) >> unit) + 1)) >> 31) unit++;
-    const int log2 = shares_log2(a, max_q, max_kv);
-    cache_attend_shares_kernel<<<(1 << log2) / kWaves, kThreads, 0, stream>>>(a, log2, unit);
-    if (hipError_t e = hipGetLastError()) return e;
-    return launch_cache_attend_join<kRows>(a, 1 << log2, stream);
 }
 
 }  // namespace mxattn

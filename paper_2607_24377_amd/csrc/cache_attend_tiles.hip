@@ -34,26 +34,44 @@ typedef __attribute__((address_space(3))) void* lds_ptr_t;
 // sequence, or, causal, growing by a constant from tile to tile.  All items' weights in
 // a row are cut into equal shares, one per workgroup.
 
-// The tiles of a sequence: tile t of a head weighs a + b (t + 1).
+// The tiles of a sequence: tile t of a head weighs a + b (t + 1), but from tile `full` on
+// what tile full - 1 and those behind it would pass: `most`.
+template <AttendKind kKind>
 struct SeqWork {
-    int64_t a;
-    int tiles, b;
-    __device__ __forceinline__ int64_t before(int64_t t) const { return t * a + b * (t * (t + 1) / 2); }
-    __device__ __forceinline__ int64_t weight(int t) const { return a + (int64_t)b * (t + 1); }
+    int64_t a, most;
+    int tiles, b, full;
+    __device__ __forceinline__ int64_t before(int64_t t) const {
+        if constexpr (kKind == kWindow)
+            if (t > full) return full * a + b * ((int64_t)full * (full + 1) / 2) + (t - full) * most;
+        return t * a + b * (t * (t + 1) / 2);
+    }
+    __device__ __forceinline__ int64_t weight(int t) const {
+        if constexpr (kKind == kWindow)
+            if (t >= full) return most;
+        return a + (int64_t)b * (t + 1);
+    }
+    __device__ __forceinline__ bool even() const { return kKind != kWindow && b == 0; }
 };
 
-__device__ __forceinline__ SeqWork seq_work(const CacheAttendArgs& a, int s) {
+template <AttendKind kKind>
+__device__ __forceinline__ SeqWork<kKind> seq_work(const CacheAttendArgs& a, int s) {
     const TokenRange r = token_range(a.c, s);
     const int64_t rows = (int64_t)(r.last - r.first) * a.group;
-    const int keys = keys_of(a.c, s);
-    SeqWork w;
+    const int keys = keys_of<kKind>(a, s);
+    SeqWork<kKind> w;
     w.tiles = (int)((rows + kRows - 1) / kRows);
-    if (a.causal) {  // in units of a key times the group: kRows / group keys more per tile
+    if (kKind != kTree && a.causal) {  // in units of a key times the group: kRows / group keys more per tile
         w.a = (int64_t)max(keys - (r.last - r.first), 0) * a.group;
         w.b = kRows;
     } else {
         w.a = max(keys, 1);
         w.b = 0;
+    }
+    if constexpr (kKind == kWindow) {  // no tile sees more than the window, the sinks and its own rows' span
+        w.most = (int64_t)a.window + a.sinks;
+        if (w.b) w.most = w.most * a.group + kRows;
+        if (!w.b && w.a < w.most) w.most = w.a;
+        w.full = w.b ? (int)min(max((w.most - w.a) / kRows, (int64_t)0), (int64_t)w.tiles) : 0;
     }
     return w;
 }
@@ -73,6 +91,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
 
 // The share of workgroup i of n, empty for all where q_start does not ascend (the
 // sum of the weights could pass 64 bits); all kThreads threads call it.
+template <AttendKind kKind>
 __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int n) {
     __shared__ int64_t s_sum[kThreads / 64];
     __shared__ bool s_ascend[kThreads / 64];
@@ -83,7 +102,7 @@ __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int
     int64_t mine = 0;
     bool ascend = true;
     for (int s = s0; s < s1; s++) {
-        const SeqWork w = seq_work(a, s);
+        const SeqWork<kKind> w = seq_work<kKind>(a, s);
         mine += w.before(w.tiles) * a.c.heads;
         ascend = ascend && starts_ascend(a.c, s);
     }
@@ -114,7 +133,7 @@ __device__ __forceinline__ Share find_share(const CacheAttendArgs& a, int i, int
     if (i < n && before <= lo && lo < before + mine) {
         int64_t at = before;
         for (int s = s0; s < s1; s++) {
-            const SeqWork w = seq_work(a, s);
+            const SeqWork<kKind> w = seq_work<kKind>(a, s);
             const int64_t all = w.before(w.tiles) * a.c.heads;
             if (lo < at + all) {
                 s_share = {lo, hi, lo - at, total, s, n};
@@ -138,15 +157,16 @@ struct Item {
 };
 
 // The item at the share's place; the share moves on behind it.
+template <AttendKind kKind>
 __device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
-    const SeqWork w = seq_work(a, sh.s);
+    const SeqWork<kKind> w = seq_work<kKind>(a, sh.s);
     const int64_t per_head = w.before(w.tiles);
     Item it;
     it.s = sh.s;
     it.head = __builtin_amdgcn_readfirstlane((int)(sh.offset / per_head));
     const int64_t r = uniform64(sh.offset - it.head * per_head);
     int t = 0;
-    if (w.b == 0) {
+    if (w.even()) {
         t = __builtin_amdgcn_readfirstlane((int)(r / w.a));
     } else {
         int hi = w.tiles - 1;  // the last tile that starts at or before r
@@ -172,30 +192,28 @@ __device__ __forceinline__ Item next_item(const CacheAttendArgs& a, Share& sh) {
     if (sh.at < sh.end && sh.offset >= per_head * a.c.heads) {
         sh.offset = 0;
         do sh.s++;
-        while (sh.s < a.c.seqs && seq_work(a, sh.s).tiles == 0);
+        while (sh.s < a.c.seqs && seq_work<kKind>(a, sh.s).tiles == 0);
     }
     return it;
 }
 
-// Which rows a tile has and what they see.
+// Which rows a tile has.
 struct TileRows {
-    int n, keys;           // the sequence's new tokens and keys
-    int rows;              // rows of the tile
-    int min_end, max_end;  // keys that its first and its last row see
-    int64_t first;         // the sequence's first token in the call
-    bool bad;              // no such cache
+    int n, keys;    // the sequence's new tokens and keys
+    int rows;       // rows of the tile
+    int64_t first;  // the sequence's first token in the call
+    bool bad;       // no such cache
 };
+template <AttendKind kKind>
 __device__ __forceinline__ TileRows tile_rows(const CacheAttendArgs& a, int s, int row0) {
     const TokenRange r = token_range(a.c, s);
     TileRows t;
     t.n = r.last - r.first;
     t.first = r.first;
-    const int keys = __builtin_amdgcn_readfirstlane(keys_of(a.c, s));
+    const int keys = __builtin_amdgcn_readfirstlane(keys_of<kKind>(a, s));
     t.bad = keys < 0;
     t.keys = max(keys, 0);
     t.rows = min(kRows, t.n * a.group - row0);
-    t.min_end = a.causal ? t.keys - t.n + token_of(a, row0) + 1 : t.keys;
-    t.max_end = max(0, a.causal ? t.keys - t.n + token_of(a, row0 + t.rows - 1) + 1 : t.keys);
     return t;
 }
 
@@ -219,13 +237,14 @@ struct StepLoader {
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)block, 0, kBlockBytes, 0x00020000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(dst + wave * 1024), 16, off, 0, 0, 0);
     }
-    // Blocks b and b + 1 (the second only below `blocks`: else the first again, for keys that are masked) of
-    // these pages.
+    // The blocks at places v and v + 1 of the walk (the second only where there is one: else the last again, for keys
+    // that are masked), of these pages.
+    template <AttendKind kKind>
     __device__ __forceinline__ void load(Scales& s, uint8_t* stage, const CacheArgs& c, const int (&page)[2], int head,
-                                         int b, int blocks) const {
+                                         int v, const Sight<kKind>& sight) const {
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            const BlockAt p = block_at(c, page[i], head, min(b + i, blocks - 1));
+            const BlockAt p = block_at(c, page[i], head, sight.block(min(v + i, sight.count - 1)));
             copy(c.kc + p.at * kBlockBytes, koff, stage + i * kBlockBytes);
             copy(c.vc + p.at * kBlockBytes, voff, stage + (2 + i) * kBlockBytes);
             s.k[i] = c.ks[p.at];
@@ -233,9 +252,11 @@ struct StepLoader {
             s.lost[i] = p.lost;
         }
     }
-    static __device__ __forceinline__ void pages(int (&page)[2], const CacheArgs& c, int seq, int b, int blocks) {
+    template <AttendKind kKind>
+    static __device__ __forceinline__ void pages(int (&page)[2], const CacheArgs& c, int seq, int v,
+                                                 const Sight<kKind>& sight) {
 #pragma unroll
-        for (int i = 0; i < 2; i++) page[i] = page_of(c, seq, min(b + i, blocks - 1));
+        for (int i = 0; i < 2; i++) page[i] = page_of(c, seq, sight.block(min(v + i, sight.count - 1)));
     }
 };
 
@@ -250,11 +271,12 @@ __device__ __forceinline__ v16f block_scores(const uint8_t* block, int e, const 
     return scores(k, e, q);
 }
 
-// The softmax of a step's scores and its products with V.  `visible`: keys of the
-// step that the lane's row sees; `held`: keys that the sequence has in it; `any`:
+// The softmax of a step's scores and its products with V.  `sees`: the keys of its two
+// blocks that the lane's row sees; `held`: keys that the sequence has in them; `any`:
 // whether some row does not see all.
-__device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* stage, const Scales& x, float c, int visible,
-                                     int held, bool any, int h, int lane) {
+template <class Mask>
+__device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* stage, const Scales& x, float c,
+                                     const Mask (&sees)[2], const int (&held)[2], bool any, int h, int lane) {
     const bool lost = x.lost[0] || x.lost[1];
     if (any || lost) {
 #pragma unroll
@@ -262,7 +284,7 @@ __device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* sta
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 const float y = x.lost[b] ? __builtin_nanf("") : s[b][i];
-                s[b][i] = 32 * b + 16 * h + i < visible ? y : -__builtin_inff();
+                s[b][i] = sees[b](16 * h + i) ? y : -__builtin_inff();
             }
     }
     float mx = max2(max2(s[0][0], s[0][1]), s[1][0]), my = max2(max2(s[0][2], s[0][3]), s[1][1]);
@@ -288,7 +310,7 @@ __device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* sta
 #pragma unroll
         for (int n = 0; n < 4; n++) v[n] = part(stage + (2 + b) * kBlockBytes, n, lane);
         int e = x.v[b];
-        if (any || lost) clean_values(st, v, e, 32 * b, visible, held, x.lost[b], h);
+        if (any || lost) clean_values(st, v, e, sees[b], held[b], x.lost[b], h);
         const float vscale = st.value_scale(e);
 #pragma unroll
         for (int n = 0; n < 4; n++) {
@@ -302,6 +324,7 @@ __device__ __forceinline__ void step(State& st, v16f (&s)[2], const uint8_t* sta
 // read the same keys.
 __device__ __forceinline__ int share_index() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
 
+template <AttendKind kKind>
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAttendArgs a) {
     __shared__ __align__(16) uint8_t st0[kStageBytes];
     __shared__ __align__(16) uint8_t st1[kStageBytes];
@@ -310,44 +333,49 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, q = lane & 31, h = lane >> 5;
     const int index = share_index();
-    Share sh = find_share(a, index, gridDim.x);
+    Share sh = find_share<kKind>(a, index, gridDim.x);
     const Parts<kRows> parts(a.workspace, gridDim.x);
     const StepLoader loader(wave, lane);
     while (sh.at < sh.end && sh.s < c.seqs) {  // (it is, unless q_start was written meanwhile)
-        const Item it = next_item(a, sh);
-        const TileRows t = tile_rows(a, it.s, it.row0);
-        const int blocks = (t.max_end + kBlockTokens - 1) / kBlockTokens;
-        const int steps = (blocks + 1) / 2;
-        const int j0 = (int)(it.x0 * steps / it.w), j1 = (int)(it.x1 * steps / it.w);
-        // this wave's rows
+        const Item it = next_item<kKind>(a, sh);
+        const TileRows t = tile_rows<kKind>(a, it.s, it.row0);
+        // this wave's rows: the tile's last one for those that are not there
         const int wrow = 32 * wave, wrows = min(32, t.rows - wrow);
         const bool live = q < wrows;
         const int row = it.row0 + min(wrow + q, t.rows - 1);
-        const int end = a.causal ? t.keys - t.n + token_of(a, row) + 1 : t.keys;
-        const int wmin = a.causal ? t.keys - t.n + token_of(a, it.row0 + min(wrow, t.rows - 1)) + 1 : t.keys;
-        const QOperand qo = load_q(a.q + row_offset(a, t.first, row, it.head, a.q_stride), h, a.scale, live && end > 0);
+        const Sight<kKind> all(a, (int)t.first, t.n, t.keys, row, it.row0, it.row0 + t.rows - 1);
+        Sight<kKind> sight(a, (int)t.first, t.n, t.keys, row, it.row0 + min(wrow, t.rows - 1),
+                           it.row0 + min(wrow + 31, t.rows - 1));
+        const int steps = (all.count + 1) / 2;
+        const int j0 = (int)(it.x0 * steps / it.w), j1 = (int)(it.x1 * steps / it.w);
+        const QOperand qo = load_q(a.q + row_offset(a, t.first, row, it.head, a.q_stride), h, a.scale, live && sight.some());
         State st;
         st.clear();
         Scales x0, x1, x2;
         __syncthreads();  // the stages are free
         if (j0 < j1) {
             int page[2];
-            StepLoader::pages(page, c, it.s, 2 * j0, blocks);
-            loader.load(x0, st0, c, page, it.head, 2 * j0, blocks);
-            StepLoader::pages(page, c, it.s, 2 * j0 + 2, blocks);
-            if (j0 + 1 < j1) loader.load(x1, st1, c, page, it.head, 2 * j0 + 2, blocks);
-            StepLoader::pages(page, c, it.s, 2 * j0 + 4, blocks);
+            StepLoader::pages(page, c, it.s, 2 * j0, all);
+            loader.load(x0, st0, c, page, it.head, 2 * j0, all);
+            StepLoader::pages(page, c, it.s, 2 * j0 + 2, all);
+            if (j0 + 1 < j1) loader.load(x1, st1, c, page, it.head, 2 * j0 + 2, all);
+            StepLoader::pages(page, c, it.s, 2 * j0 + 4, all);
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
             auto one = [&](int j, const uint8_t* cur, uint8_t* far, const Scales& xc, Scales& xf) {
                 if (j + 2 < j1) {
-                    loader.load(xf, far, c, page, it.head, 2 * j + 4, blocks);
-                    StepLoader::pages(page, c, it.s, 2 * j + 6, blocks);
+                    loader.load(xf, far, c, page, it.head, 2 * j + 4, all);
+                    StepLoader::pages(page, c, it.s, 2 * j + 6, all);
                 }
                 v16f s[2];
                 s[0] = block_scores(cur, xc.k[0], qo, lane);
                 s[1] = block_scores(cur + kBlockBytes, xc.k[1], qo, lane);
-                step(st, s, cur, xc, qo.c, end - j * kKeys, t.keys - j * kKeys, (j + 1) * kKeys > wmin, h, lane);
+                const int at[2] = {all.block(2 * j) * kBlockTokens, all.block(2 * j + 1) * kBlockTokens};
+                const bool any = sight.partial(at[0]) || sight.partial(at[1]);
+                const auto m0 = sight.mask_of(at[0], any), m1 = sight.mask_of(at[1], any);
+                const decltype(m0) sees[2] = {m0, m1};
+                const int held[2] = {t.keys - at[0], t.keys - at[1]};
+                step(st, s, cur, xc, qo.c, sees, held, any, h, lane);
                 __builtin_amdgcn_s_waitcnt(0);  // the next but one landed
                 __syncthreads();
             };
@@ -360,10 +388,13 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
         const float l = st.l + other_half(st.l);
         const bool whole = it.whole();
         if (live) {
-            if (whole)
+            if (whole) {
+                if constexpr (kKind == kWeighStats)
+                    if (h == 0) a.stats[row_number(a, t.first, row, it.head)] = statistics(st.m, l);
                 store_row(st, inverse(l, t.bad), a.out + row_offset(a, t.first, row, it.head, a.out_stride), h);
-            else
+            } else {
                 store_part(st, l, parts, (int64_t)(2 * index + (it.x0 == 0)) * kRows + wrow + q, h);
+            }
         }
         if (it.x0 == 0 && tid == 0) parts.info[it.number] = {index, it.last};
     }
@@ -378,6 +409,13 @@ int workgroups(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
     return n >= 512 ? 512 : n < 8 ? 8 : (int)n & ~7;
 }
 
+template <AttendKind kKind>
+hipError_t launch(const CacheAttendArgs& a, int n, hipStream_t stream) {
+    cache_attend_tiles_kernel<kKind><<<n, kThreads, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    return launch_cache_attend_join<kRows, kKind>(a, n, stream);
+}
+
 }  // namespace
 
 size_t cache_attend_tiles_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
@@ -386,9 +424,13 @@ size_t cache_attend_tiles_workspace(const CacheAttendArgs& a, int64_t max_q, int
 
 hipError_t launch_cache_attend_tiles(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream) {
     const int n = workgroups(a, max_q, max_kv);
-    cache_attend_tiles_kernel<<<n, kThreads, 0, stream>>>(a);
-    if (hipError_t e = hipGetLastError()) return e;
-    return launch_cache_attend_join<kRows>(a, n, stream);
+    switch (a.kind) {
+        case kWindow: return launch<kWindow>(a, n, stream);
+        case kTree: return launch<kTree>(a, n, stream);
+        case kWeighStats: return launch<kWeighStats>(a, n, stream);
+        case kWeigh: return hipErrorInvalidValue;  // (these kernels keep no scores)
+        default: return launch<kPlain>(a, n, stream);
+    }
 }
 
 }  // namespace mxattn

@@ -81,6 +81,19 @@ def lib() -> ctypes.CDLL:
             L.mxattn_cache_attend.restype = I
             L.mxattn_cache_attend_workspace.argtypes = [I64] * 8
             L.mxattn_cache_attend_workspace.restype = SZ
+            batch = [P, I64, P, P, P, P, I64, I64, P, P, P, I64, I64, I64, I64, I64, I64]
+            L.mxattn_cache_attend_window.argtypes = batch + [I64, I64, I, I64, I64, P, I64, P, SZ, P]
+            L.mxattn_cache_attend_window.restype = I
+            L.mxattn_cache_attend_tree.argtypes = batch + [P, I64, I64, I64, P, I64, P, SZ, P]
+            L.mxattn_cache_attend_tree.restype = I
+            L.mxattn_cache_attend_weights.argtypes = batch + [P, P, I, I64, I64, P, I64, P, SZ, P]
+            L.mxattn_cache_attend_weights.restype = I
+            L.mxattn_cache_attend_weights_workspace.argtypes = [I64] * 8
+            L.mxattn_cache_attend_weights_workspace.restype = SZ
+            L.mxattn_cache_select.argtypes = [P, I64, I64, P, P] + [I64] * 6 + [P, P, P]
+            L.mxattn_cache_select.restype = I
+            L.mxattn_cache_compact.argtypes = [P, P, P, P, I64, I64, P, I64, I64, P, I64, I64, I64, P, I64, I64, P, P, P, P]
+            L.mxattn_cache_compact.restype = I
             L.mxattn_codes_bytes.argtypes = [I, I64, I64, I64, I64]
             L.mxattn_codes_bytes.restype = SZ
             L.mxattn_scales_bytes.argtypes = [I, I64, I64, I64, I64]
@@ -416,14 +429,20 @@ def _token_rows(t, name, index):
     return t.data_ptr(), stride
 
 
+def _cache_arrays(k_codes, v_codes, d):
+    """Pages, heads and blocks per page of a cache's code arrays, which must agree."""
+    pages, heads, blocks, *block = k_codes.shape
+    if block != [d // 16, BLOCK_TOKENS, 16] or v_codes.shape != (pages, heads, blocks, d, BLOCK_TOKENS):
+        raise ValueError(f"k_codes and v_codes must have the shapes of cache_shapes for heads of {d} channels")
+    return pages, heads, blocks
+
+
 def _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, index, d):
     """Checked addresses and sizes of a cache of d channels and its batch, as the library takes them, and the cache's
     heads."""
     if k_codes.dim() != 6 or page_table.dim() != 2:
         raise ValueError("k_codes must be [pages, heads, page_tokens / 32, 8, 32, 16], page_table [seqs, max_pages]")
-    pages, heads, blocks, *block = k_codes.shape
-    if block != [d // 16, BLOCK_TOKENS, 16] or v_codes.shape != (pages, heads, blocks, d, BLOCK_TOKENS):
-        raise ValueError(f"k_codes and v_codes must have the shapes of cache_shapes for heads of {d} channels")
+    pages, heads, blocks = _cache_arrays(k_codes, v_codes, d)
     seqs, max_pages = page_table.shape
     u8, i32, n = torch.uint8, torch.int32, pages * heads * blocks
     codes = n * d * BLOCK_TOKENS
@@ -459,10 +478,19 @@ def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_tab
     output by the rounding of the probabilities to f16.  Workspace is torch's, of the current stream (a graph
     captured there keeps it); of a stream that is given it is the library's, and a call that needs some cannot be
     captured."""
+    return _attend("mxattn_cache_attend", q, (k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len), (causal,),
+                   max_q, max_kv, out, stream)
+
+
+def _attend(name, q, batch, middle, max_q, max_kv, out, stream, workspace="mxattn_cache_attend_workspace"):
+    """Attention of q over a cache by the library's call `name`.  `middle`: its arguments between the batch's sizes and
+    the bounds, or a function that checks them and gives them."""
     dev = _index(q, "q")
     qp, qst = _token_rows(q, "q", dev)
     tokens, Hq, d = q.shape
-    cache, heads = _cache(k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, dev, d)
+    cache, heads = _cache(*batch, dev, d)
+    if callable(middle):
+        middle = middle(dev, cache, heads, tokens)
     if out is None:
         out = q.new_empty((tokens, Hq, d))
     elif out.shape != q.shape:
@@ -470,13 +498,120 @@ def cache_attend(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_tab
     op, ost = _token_rows(out, "out", dev)
     L, work, size = _lib or lib(), None, 0
     if stream is None:  # torch's memory belongs to the current stream, and to the graph that is captured on it
-        size = L.mxattn_cache_attend_workspace(cache[5], *cache[9:], tokens, Hq, heads, max_q, max_kv)
+        size = getattr(L, workspace)(cache[5], *cache[9:], tokens, Hq, heads, max_q, max_kv)
         if size:
             work = torch.empty(size, dtype=torch.uint8, device=q.device)
-    _run(L.mxattn_cache_attend, "mxattn_cache_attend", dev, stream,
-         (qp, qst, *cache, tokens, Hq, heads, d, causal, max_q, max_kv, op, ost,
-          work.data_ptr() if size else None, size))
+    _run(getattr(L, name), name, dev, stream, (qp, qst, *cache, tokens, Hq, heads, d, *middle, max_q, max_kv, op, ost,
+                                               work.data_ptr() if size else None, size))
     return out
+
+
+def cache_attend_window(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, window: int,
+                        sinks: int = 0, causal: bool = True, max_q: int = 0, max_kv: int = 0, out=None, stream=None):
+    """cache_attend of the last `window` keys (of a token that sees T keys, positions T - window .. T - 1) and the
+    first `sinks`.  Pages between that no token sees may have been given away: they are not read."""
+    return _attend("mxattn_cache_attend_window", q, (k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len),
+                   (window, sinks, causal), max_q, max_kv, out, stream)
+
+
+def cache_attend_tree(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, tree,
+                      max_q: int = 0, max_kv: int = 0, out=None, stream=None):
+    """cache_attend for drafted tokens that form trees: a sequence's new token sees what was there before and those of
+    its new tokens whose bit is set in its row of `tree`, int32 [tokens, words], bit j & 31 of word j >> 5 for new
+    token j (its ancestors, and itself)."""
+    def middle(dev, cache, heads, tokens):
+        if tree.dim() != 2 or tree.shape[0] != tokens:
+            raise ValueError("tree must be [tokens, words]")
+        return _address(tree, "tree", torch.int32, dev, tree.numel()), tree.shape[1]
+
+    return _attend("mxattn_cache_attend_tree", q, (k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len), middle,
+                   max_q, max_kv, out, stream)
+
+
+def _weights_shape(t, name, shape):
+    if t.shape != shape:
+        raise ValueError(f"{name} must be [pages, heads, page_tokens]: {list(shape)}")
+    return t
+
+
+def cache_attend_weights(q: torch.Tensor, k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len, weights=None,
+                         causal: bool = True, max_q: int = 0, max_kv: int = 0, out=None, weights_out=None, stream=None):
+    """cache_attend that also adds to every key's weight the probabilities that the new tokens and the heads of its
+    group give it; new keys start at 0.  weights: fp32 [pages, Hkv, page_tokens] (None: zeros); weights_out: where
+    the sums go (None: into `weights`, or a new tensor of zeros).  Returns (out, weights_out).  max_kv is a limit
+    here: longer sequences count as impossible."""
+    def middle(dev, cache, heads, tokens):
+        nonlocal weights_out
+        shape = (cache[4], heads, cache[5])
+        if weights is not None:
+            _weights_shape(weights, "weights", shape)
+        if weights_out is None:
+            if weights is None and stream is not None:  # (torch would clear it on another stream)
+                raise ValueError("weights or weights_out must be given with a stream")
+            weights_out = weights if weights is not None else torch.zeros(shape, dtype=torch.float32, device=q.device)
+        n = cache[4] * heads * cache[5]
+        return (_address(weights, "weights", torch.float32, dev, n),
+                _address(_weights_shape(weights_out, "weights_out", shape), "weights_out", torch.float32, dev, n), causal)
+
+    out = _attend("mxattn_cache_attend_weights", q, (k_codes, k_scales, v_codes, v_scales, page_table, q_start, kv_len),
+                  middle, max_q, max_kv, out, stream, "mxattn_cache_attend_weights_workspace")
+    return out, weights_out
+
+
+def cache_select(weights: torch.Tensor, page_table, kv_len, budget: int, sinks: int = 0, recent: int = 0, kept=None,
+                 counts=None, stream=None):
+    """Which tokens stay when every sequence is cut to `budget`, for each KV head of fp32 weights [pages, Hkv,
+    page_tokens]: the first `sinks`, the last `recent` and the heaviest between (ties: the first).  Returns (kept
+    int32 [seqs, Hkv, budget], ascending positions and -1 behind them; counts int32 [seqs])."""
+    if weights.dim() != 3 or page_table.dim() != 2 or not weights.is_cuda:
+        raise ValueError("weights must be a CUDA tensor [pages, heads, page_tokens], page_table [seqs, max_pages]")
+    dev = weights.get_device()
+    pages, heads, page = weights.shape
+    seqs, max_pages = page_table.shape
+    i32 = torch.int32
+    if kept is None:
+        kept = torch.empty((seqs, heads, max(budget, 0)), dtype=i32, device=weights.device)
+    elif kept.shape != (seqs, heads, budget):
+        raise ValueError("kept must be [seqs, heads, budget]")
+    if counts is None:
+        counts = torch.empty((seqs,), dtype=i32, device=weights.device)
+    _run((_lib or lib()).mxattn_cache_select, "mxattn_cache_select", dev, stream,
+         (_address(weights, "weights", torch.float32, dev, weights.numel()), pages, page,
+          _address(page_table, "page_table", i32, dev, seqs * max_pages), _address(kv_len, "kv_len", i32, dev, seqs), seqs,
+          max_pages, heads, budget, sinks, recent, _address(kept, "kept", i32, dev, kept.numel()),
+          _address(counts, "counts", i32, dev, seqs)))
+    return kept, counts
+
+
+def cache_compact(k_codes: torch.Tensor, k_scales, v_codes, v_scales, page_table, kept, counts, base=None, out_table=None,
+                  weights=None, stream=None):
+    """Move kept tokens together: position base + i (i < counts) of a sequence becomes what was at kept[.., i], in K, V
+    and, if given, fp32 weights [pages, Hkv, page_tokens].  kept: int32 [seqs, Hkv or 1, width]; counts, base (None: 0):
+    int32 [seqs].  out_table: the page table of where they go, pages that hold none of the sources; None: in place
+    (kept ascending, kept[i] >= base + i)."""
+    if not k_codes.is_cuda or k_codes.dim() != 6 or kept.dim() != 3:
+        raise ValueError("k_codes must be a CUDA tensor as of cache_shapes, kept [seqs, heads or 1, width]")
+    dev, d = k_codes.get_device(), 128
+    seqs, kept_heads, width = kept.shape
+    i32 = torch.int32
+    # (the batch's starts and lengths are of no concern here: a table and counts are)
+    pages, heads, blocks = _cache_arrays(k_codes, v_codes, d)
+    if page_table.dim() != 2 or page_table.shape[0] != seqs:
+        raise ValueError("page_table must be [seqs, max_pages], kept [seqs, heads or 1, width]")
+    n = pages * heads * blocks
+    u8, codes = torch.uint8, n * d * BLOCK_TOKENS
+    if out_table is not None and (out_table.dim() != 2 or out_table.shape[0] != seqs):
+        raise ValueError("out_table must be [seqs, pages]")
+    if weights is not None:
+        _weights_shape(weights, "weights", (pages, heads, blocks * BLOCK_TOKENS))
+    _run((_lib or lib()).mxattn_cache_compact, "mxattn_cache_compact", dev, stream,
+         (_address(k_codes, "k_codes", u8, dev, codes), _address(k_scales, "k_scales", u8, dev, n),
+          _address(v_codes, "v_codes", u8, dev, codes), _address(v_scales, "v_scales", u8, dev, n), pages,
+          blocks * BLOCK_TOKENS, _address(page_table, "page_table", i32, dev, page_table.numel()), seqs, page_table.shape[1],
+          None if out_table is None else _address(out_table, "out_table", i32, dev, out_table.numel()),
+          0 if out_table is None else out_table.shape[1], heads, d, _address(kept, "kept", i32, dev, kept.numel()),
+          kept_heads, width, _address(counts, "counts", i32, dev, seqs), _address(base, "base", i32, dev, seqs),
+          _address(weights, "weights", torch.float32, dev, n * BLOCK_TOKENS)))
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

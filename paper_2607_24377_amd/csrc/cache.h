@@ -172,4 +172,24 @@ __device__ __forceinline__ int owner_of(const CacheArgs& c, int64_t w, int64_t g
     return w < first_group(c, lo + 1, group, unit, step) ? lo : -1;
 }
 
+// Workgroups of a launch over items (a sequence's heads) and chunks of each.  Workgroups go
+// to the 8 XCDs in turn and there to its shader engines in turn, so an item's chunks follow
+// one another on one XCD, whose L2 holds what they share, and spread over all its engines.
+// (In the order of sequences, one of four that was the longest lay on two XCDs, or on an
+// engine of each: the weights of 4 prompts took 400 and 272 us for what takes 130.)
+struct Placed {
+    int s, head, chunk;  // s < 0: none
+    __device__ __forceinline__ Placed(const CacheArgs& c, int chunks) {
+        const unsigned items = (unsigned)c.seqs * (unsigned)c.heads, id = blockIdx.x, n = (unsigned)chunks;
+        const unsigned t = items < 8 ? id : id >> 3, k = t / n, item = items < 8 ? k : (id & 7) + 8 * k;
+        chunk = (int)(t - k * n);
+        s = item < items ? (int)(item / (unsigned)c.heads) : -1;
+        head = (int)item - s * c.heads;
+    }
+};
+inline unsigned placed_grid(const CacheArgs& c, int64_t chunks) {
+    const int64_t items = (int64_t)c.seqs * c.heads;
+    return (unsigned)((items < 8 ? items : (items + 7) / 8 * 8) * chunks);
+}
+
 }  // namespace mxattn

@@ -135,7 +135,7 @@ __device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QOperan
 // the time of the two FP8 products and 32 conversions a block, for which attention of a
 // few rows has room.  The operands' channels in the order of the FP8 ones.
 struct QExact {
-    uint4 r[2][4];
+    uint4 r[8];
     float c;  // as QOperand's
 };
 
@@ -146,8 +146,8 @@ __device__ __forceinline__ QExact load_q_exact(const uint16_t* row, int h, float
     for (int j = 0; j < 2; j++)
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            q.r[j][k] = live ? *reinterpret_cast<const uint4*>(row + 64 * j + 32 * h + 8 * k) : make_uint4(0, 0, 0, 0);
-            m = max_halves(m, q.r[j][k]);
+            q.r[4 * j + k] = live ? *reinterpret_cast<const uint4*>(row + 64 * j + 32 * h + 8 * k) : make_uint4(0, 0, 0, 0);
+            m = max_halves(m, q.r[4 * j + k]);
         }
     m = max(m & 0xFFFFu, m >> 16);
     m = max(m, __builtin_bit_cast(uint32_t, other_half(__builtin_bit_cast(float, m))));
@@ -171,25 +171,24 @@ struct KExact {
 __device__ __forceinline__ KExact exact_keys(const uint4 (&k)[4], int e) {
     KExact x;
     const float scale = e8m0_as_f32((uint32_t)e);
+    const uint32_t none = __builtin_amdgcn_readfirstlane(e) == 255 ? 0x7F7F7F7Fu : 0u;  // a scale that is no number: nor is any key
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-        x.k[2 * i] = to_bf16(k[i].x, k[i].y, scale);
-        x.k[2 * i + 1] = to_bf16(k[i].z, k[i].w, scale);
+        x.k[2 * i] = to_bf16(k[i].x | none, k[i].y | none, scale);
+        x.k[2 * i + 1] = to_bf16(k[i].z | none, k[i].w | none, scale);
     }
     return x;
 }
 
-__device__ __forceinline__ v16f scores(const KExact& k, int e, const QExact& q) {
+__device__ __forceinline__ v16f scores(const KExact& k, const uint4 (&q)[8]) {
     v16f s;
-    const float zero = e == 255 ? __builtin_nanf("") : 0.f;  // a scale that is no number: nor is any score
 #pragma unroll
-    for (int i = 0; i < 16; i++) s[i] = zero;
+    for (int i = 0; i < 16; i++) s[i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.k[i], __builtin_bit_cast(bf16x8, q.r[i >> 2][i & 3]), s, 0, 0, 0);
+    for (int i = 0; i < 8; i++) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.k[i], __builtin_bit_cast(bf16x8, q[i]), s, 0, 0, 0);
     return s;
 }
-__device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QExact& q) { return scores(exact_keys(k, e), e, q); }
+__device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QExact& q) { return scores(exact_keys(k, e), q.r); }
 
 // Q as the kernels of a kind take it.
 template <AttendKind kKind>

@@ -4,7 +4,9 @@
 // and, of those between, the heaviest, `budget` in all.  A workgroup finds the weight of
 // the last one that stays digit by digit (11, 11 and 10 bits of the number in an order of
 // unsigned integers, a histogram in LDS for each), then writes the kept positions in
-// order: each wave counts its own stretch, and starts where the ones before it end.
+// order: each wave starts where the stretches before its own end.  What shares the digits
+// found so far is put aside in LDS as soon as it fits, so that the weights are read three
+// times (histogram, putting aside, writing).
 //
 // Compaction: position base + i becomes what was at kept[i].  A block of 32 kept tokens
 // takes the largest scale byte of the blocks that they come from, so that no code grows
@@ -22,6 +24,8 @@ namespace {
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kDigits = 2048;
+constexpr int kCopies = 8;      // of the histogram: weights share few of the first digits
+constexpr int kAside = 8192;
 
 // Weights in the order of unsigned integers; NaN below every number, -0 with +0.
 __device__ __forceinline__ uint32_t ordered(float w) {
@@ -29,16 +33,51 @@ __device__ __forceinline__ uint32_t ordered(float w) {
     return w != w ? 0u : u >> 31 ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs a) {
-    __shared__ uint32_t s_hist[kDigits];
-    __shared__ uint32_t s_wave[kSelectWaves];
-    __shared__ uint32_t s_found[2];  // the digit of the last one that stays, and how many of it
-    __shared__ uint32_t s_above[kSelectWaves], s_equal[kSelectWaves];
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+// The weights of a head's stretch j0 .. j1 - 1, j0 a multiple of 4, 1024 at a time: f gets
+// a position and four weights, ordered (of no page: as NaN), position by position of the
+// wave's lanes.  (One at a time: two loads after each other for every 64.)
+template <class F>
+__device__ __forceinline__ void for_weights(const SelectArgs& a, int s, int head, int j0, int j1, const F& f) {
     const CacheArgs& c = a.c;
-    const int s = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
+    const int lane = threadIdx.x & 63, log2 = c.bpp_log2 + 5;
+    const int32_t* table = c.page_table + (int64_t)s * c.max_pages;
+    constexpr int kTurns = 4;
+    for (int j = j0; j < j1; j += 256 * kTurns) {
+        int page[kTurns];
+        f32x4u w[kTurns];
+#pragma unroll
+        for (int i = 0; i < kTurns; i++) page[i] = table[min(j + 256 * i + 4 * lane, j1 - 1) >> log2];
+#pragma unroll
+        for (int i = 0; i < kTurns; i++) {
+            const int at = min(j + 256 * i + 4 * lane, (j1 - 1) & ~3);
+            const bool there = (unsigned)page[i] < (unsigned)c.pages;
+            w[i] = *reinterpret_cast<const f32x4u*>(
+                a.weights + (((int64_t)(there ? page[i] : 0) * c.heads + head) << log2) + (at & ((1 << log2) - 1)));
+            if (!there) w[i] = f32x4u{0.f, 0.f, 0.f, 0.f} * __builtin_nanf("");
+        }
+#pragma unroll
+        for (int i = 0; i < kTurns; i++) {
+            if (j + 256 * i >= j1) break;
+            const uint32_t u[4] = {ordered(w[i][0]), ordered(w[i][1]), ordered(w[i][2]), ordered(w[i][3])};
+            f(j + 256 * i + 4 * lane, u);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs a) {
+    __shared__ __align__(16) uint32_t s_hist[kDigits * kCopies];
+    __shared__ uint32_t s_aside[kAside];
+    __shared__ uint8_t s_whose[kAside];
+    __shared__ uint32_t s_wave[kSelectWaves];
+    __shared__ uint32_t s_found[3];  // the digit of the last one that stays, how many of it do, how many there are
+    __shared__ uint32_t s_above[kSelectWaves], s_equal[kSelectWaves], s_count;
+    const CacheArgs& c = a.c;
+    // (head by head: the XCDs take workgroups in turn, and the heads of a sequence spread over them)
+    const int s = (int)(blockIdx.x / (unsigned)c.heads), head = (int)blockIdx.x - s * c.heads, tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int log2 = c.bpp_log2 + 5;
-    const int len = c.kv_len[s], L = (unsigned)len > (unsigned)(c.max_pages << log2) ? 0 : len;
+    const int len = c.kv_len[s], L = (unsigned)len > (unsigned)(c.max_pages << (c.bpp_log2 + 5)) ? 0 : len;
     const int count = min(L, a.budget);
     int32_t* kept = a.kept + ((int64_t)s * c.heads + head) * a.budget;
     if (head == 0 && tid == 0) a.counts[s] = count;
@@ -48,27 +87,66 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs
         return;
     }
     const int m0 = a.sinks, m1 = L - a.recent;  // what lies between may go
-    auto weight = [&](int j) {
-        const int page = c.page_table[(int64_t)s * c.max_pages + (j >> log2)];
-        if ((unsigned)page >= (unsigned)c.pages) return 0u;  // no such page: as NaN
-        return ordered(a.weights[(((int64_t)page * c.heads + head) << log2) + (j & ((1 << log2) - 1))]);
-    };
+    // a stretch of all positions for each wave
+    const int per = (L + 256 * kSelectWaves - 1) / (256 * kSelectWaves) * 256;
+    const int j0 = min(wave * per, L), j1 = min(j0 + per, L);
+    if (tid < kSelectWaves) s_above[tid] = s_equal[tid] = 0;
+    if (tid == 0) s_count = 0;
     // the weight of the last one that stays, `prefix` in the bits of `known`, and how many
     // of exactly that weight do
     uint32_t prefix = 0, known = 0;
     uint32_t need = (uint32_t)(a.budget - a.sinks - a.recent);  // below the number of those between
     const bool any = need > 0;
+    bool aside = false;  // what shares the known digits is in s_aside, what is above them counted
     for (int pass = 0; any && pass < 3; pass++) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int i = tid; i < kDigits; i += kSelectThreads) s_hist[i] = 0;
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t mask = pass == 2 ? 1023 : 2047;
+        const bool fits = pass > 0 && !aside && s_found[2] <= kAside;
+        for (int i = tid; i < kDigits * kCopies / 4; i += kSelectThreads)
+            reinterpret_cast<uint4*>(s_hist)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        for (int j = m0 + tid; j < m1; j += kSelectThreads) {
-            const uint32_t u = weight(j);
-            if ((u & known) == prefix) atomicAdd(&s_hist[(u >> shift) & ((1u << bits) - 1)], 1u);
+        auto add = [&](uint32_t u) { atomicAdd(&s_hist[((u >> shift) & mask) * kCopies + (lane & (kCopies - 1))], 1u); };
+        if (aside) {
+            const int n = (int)s_count;
+            for (int i = tid; i < n; i += kSelectThreads)
+                if ((s_aside[i] & known) == prefix) add(s_aside[i]);
+        } else {
+            uint32_t above = 0;
+            for_weights(a, s, head, j0, j1, [&](int j, const uint32_t (&u)[4]) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const bool in = j + i < j1;
+                    const bool free = in && j + i >= m0 && j + i < m1;
+                    const bool mine = free && (u[i] & known) == prefix;
+                    if (mine) add(u[i]);
+                    if (fits) {
+                        above += (uint32_t)__popcll(__ballot(in && (!free || (u[i] & known) > prefix)));
+                        const uint64_t all = __ballot(mine);
+                        if (all) {
+                            uint32_t at = 0;
+                            if (lane == 0) at = atomicAdd(&s_count, (uint32_t)__popcll(all));
+                            at = __builtin_amdgcn_readfirstlane((int)at) + (uint32_t)__popcll(all & (((uint64_t)1 << lane) - 1));
+                            if (mine) {
+                                s_aside[at] = u[i];
+                                s_whose[at] = (uint8_t)wave;
+                            }
+                        }
+                    }
+                }
+            });
+            if (fits && lane == 0) s_above[wave] = above;
         }
+        aside = aside || fits;
         __syncthreads();
         // thread t has digits 2 t and 2 t + 1 from the largest down
-        const uint32_t x = s_hist[kDigits - 1 - 2 * tid], y = s_hist[kDigits - 2 - 2 * tid];
+        uint32_t x = 0, y = 0;
+        const uint4* pair = reinterpret_cast<const uint4*>(s_hist + (kDigits - 2 - 2 * tid) * kCopies);
+#pragma unroll
+        for (int k = 0; k < kCopies / 4; k++) {
+            const uint4 v = pair[k], w = pair[kCopies / 4 + k];
+            y += v.x + v.y + v.z + v.w;
+            x += w.x + w.y + w.z + w.w;
+        }
         uint32_t incl = x + y;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -82,39 +160,38 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs
         if (before < need && need <= before + x) {
             s_found[0] = (uint32_t)(kDigits - 1 - 2 * tid);
             s_found[1] = need - before;
+            s_found[2] = x;
         } else if (before + x < need && need <= before + x + y) {
             s_found[0] = (uint32_t)(kDigits - 2 - 2 * tid);
             s_found[1] = need - before - x;
+            s_found[2] = y;
         }
         __syncthreads();
         prefix |= s_found[0] << shift;
         need = s_found[1];
-        known |= ((1u << bits) - 1) << shift;
+        known |= mask << shift;
     }
-    // a stretch of all positions for each wave, in whole turns of 64
-    const int per = ((L + kSelectThreads - 1) / kSelectThreads) * 64;
-    const int j0 = min(wave * per, L), j1 = min(j0 + per, L);
-    auto look = [&](int j, bool& above, bool& equal) {
-        above = equal = false;
-        if (j >= j1) return;
-        if (j < m0 || j >= m1) {
-            above = true;
-        } else if (any) {
-            const uint32_t u = weight(j);
-            above = u > prefix;
-            equal = u == prefix;
+    // how many of each wave's stretch stay for their weight or place, and have the last one's weight
+    if (aside) {
+        const int n = (int)s_count;
+        for (int i = tid; i < n; i += kSelectThreads) {
+            if (s_aside[i] > prefix) atomicAdd(&s_above[s_whose[i]], 1u);
+            if (s_aside[i] == prefix) atomicAdd(&s_equal[s_whose[i]], 1u);
         }
-    };
-    uint32_t above = 0, equal = 0;
-    for (int j = j0; j < j1; j += 64) {
-        bool x, y;
-        look(j + lane, x, y);
-        above += (uint32_t)__popcll(__ballot(x));
-        equal += (uint32_t)__popcll(__ballot(y));
-    }
-    if (lane == 0) {
-        s_above[wave] = above;
-        s_equal[wave] = equal;
+    } else {
+        uint32_t above = 0, equal = 0;
+        for_weights(a, s, head, j0, j1, [&](int j, const uint32_t (&u)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const bool in = j + i < j1, free = in && j + i >= m0 && j + i < m1;
+                above += (uint32_t)__popcll(__ballot(in && (!free || (any && u[i] > prefix))));
+                equal += (uint32_t)__popcll(__ballot(free && any && u[i] == prefix));
+            }
+        });
+        if (lane == 0) {
+            s_above[wave] = above;
+            s_equal[wave] = equal;
+        }
     }
     __syncthreads();
     uint32_t at = 0, same = 0;  // those above and those equal before this place
@@ -123,16 +200,27 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs
         same += s_equal[k];
     }
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for (int j = j0; j < j1; j += 64) {
-        bool x, y;
-        look(j + lane, x, y);
-        const uint64_t bx = __ballot(x), by = __ballot(y);
-        const uint32_t mine = same + (uint32_t)__popcll(by & below);
-        if (x || (y && mine < need))
-            kept[at + (uint32_t)__popcll(bx & below) + min(mine, need)] = j + lane;
-        at += (uint32_t)__popcll(bx);
-        same += (uint32_t)__popcll(by);
-    }
+    for_weights(a, s, head, j0, j1, [&](int j, const uint32_t (&u)[4]) {
+        bool x[4], y[4];
+        uint32_t ax = at, ay = same;  // before this lane's four
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const bool in = j + i < j1, free = in && j + i >= m0 && j + i < m1;
+            x[i] = in && (!free || (any && u[i] > prefix));
+            y[i] = free && any && u[i] == prefix;
+            const uint64_t bx = __ballot(x[i]), by = __ballot(y[i]);
+            ax += (uint32_t)__popcll(bx & below);
+            ay += (uint32_t)__popcll(by & below);
+            at += (uint32_t)__popcll(bx);
+            same += (uint32_t)__popcll(by);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if (x[i] || (y[i] && ay < need)) kept[ax + min(ay, need)] = j + i;
+            ax += x[i];
+            ay += y[i];
+        }
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -191,13 +279,15 @@ __device__ __forceinline__ int max32(int x) {
     return x;
 }
 
-__global__ __launch_bounds__(kThreads) void cache_compact_kernel(CompactArgs a) {
+__global__ __launch_bounds__(kThreads) void cache_compact_kernel(CompactArgs a, int runs) {
     // V: a source block in the order of channels, 17 words for every two
     __shared__ uint32_t s_rows[kWaves][64 * 17];
     const CacheArgs& c = a.c;
-    const int s = blockIdx.x, head = blockIdx.y;
-    const int runs = (int)gridDim.z >> 1, run = (int)blockIdx.z >> 1;
-    const bool values = blockIdx.z & 1;
+    const Placed place(c, 2 * runs);  // the runs of V, which take longer, then those of K
+    const int s = place.s, head = place.head;
+    if (s < 0) return;
+    const bool values = place.chunk < runs;
+    const int run = values ? place.chunk : place.chunk - runs;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int t = lane & 31, h = lane >> 5;
     const int log2 = c.bpp_log2 + 5;
@@ -307,7 +397,7 @@ __global__ __launch_bounds__(kThreads) void cache_compact_kernel(CompactArgs a) 
 }  // namespace
 
 hipError_t launch_cache_select(const SelectArgs& a, hipStream_t stream) {
-    cache_select_kernel<<<dim3((unsigned)a.c.seqs, (unsigned)a.c.heads), kSelectThreads, 0, stream>>>(a);
+    cache_select_kernel<<<(unsigned)a.c.seqs * (unsigned)a.c.heads, kSelectThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -316,7 +406,7 @@ hipError_t launch_cache_compact(const CompactArgs& a, hipStream_t stream) {
     const int64_t turns = (a.width / kBlockTokens + 2 + kWaves - 1) / kWaves;
     const int64_t most = ((int64_t)1 << 22) / ((int64_t)a.c.seqs * a.c.heads);
     const int64_t runs = a.in_place ? 1 : std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(turns, most), 32767));
-    cache_compact_kernel<<<dim3((unsigned)a.c.seqs, (unsigned)a.c.heads, (unsigned)(2 * runs)), kThreads, 0, stream>>>(a);
+    cache_compact_kernel<<<placed_grid(a.c, 2 * runs), kThreads, 0, stream>>>(a, (int)runs);
     return hipGetLastError();
 }
 

@@ -44,14 +44,16 @@ __device__ __forceinline__ float sum_with(const CacheWeighArgs& w, int64_t at, b
 }
 
 // From the scores: four keys a thread, the rows one after another.
-__global__ __launch_bounds__(kThreads) void cache_weigh_scores_kernel(CacheWeighArgs w) {
+__global__ __launch_bounds__(kThreads) void cache_weigh_scores_kernel(CacheWeighArgs w, int chunks) {
     const CacheAttendArgs& a = w.a;
-    const int s = blockIdx.x, head = blockIdx.y;
+    const Placed place(a.c, chunks);
+    const int s = place.s, head = place.head;
+    if (s < 0) return;
     const Keys k(a, s);
     if (k.n == 0) return;
     const int past = k.keys - k.n;
-    for (int64_t j64 = ((int64_t)blockIdx.z * kThreads + threadIdx.x) * 4; j64 < k.keys;
-         j64 += (int64_t)gridDim.z * kThreads * 4) {
+    for (int64_t j64 = ((int64_t)place.chunk * kThreads + threadIdx.x) * 4; j64 < k.keys;
+         j64 += (int64_t)chunks * kThreads * 4) {
         const int j = (int)j64;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int t = a.causal ? max(0, j - past) : 0; t < k.n; t++) {
@@ -75,25 +77,80 @@ __global__ __launch_bounds__(kThreads) void cache_weigh_scores_kernel(CacheWeigh
     }
 }
 
-// From K and Q: a wave holds two blocks of keys and walks all rows that see some of them.
-constexpr int kWaves = 4;
-constexpr int kBlocks = 2;
-constexpr int kGroupKeys = kWaves * kBlocks * kBlockTokens;
+// From K and Q.  A workgroup takes 4 kBlocks blocks of keys, held as operands by its waves,
+// and walks the rows that see some of them, 64 a step: waves w and w + 4 have the same keys
+// and a half of the rows each.  Q comes through LDS, two steps ahead: 16 lanes copy a row,
+// its 16-byte chunks in an order of its own, so that lanes that read a chunk of all rows
+// read all banks.
+constexpr int kWaves = 8;
+constexpr int kKeyWaves = 4;
+constexpr int kStepRows = 64;
+constexpr int kStageBytes = kStepRows * 256;
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef const __attribute__((address_space(1))) void* global_ptr_t;
 
-__global__ __launch_bounds__(64 * kWaves, 2) void cache_weigh_rows_kernel(CacheWeighArgs w) {
+// s_waitcnt: all but two of the wave's loads have landed (vmcnt 2), and all it read from LDS.
+constexpr int kTwoInFlight = 2 | 7 << 4;
+
+// A row of the sequence that moves on by kStepRows, and where what belongs to it lies (the
+// division by the group once: 64-bit products for each row of each step took as many
+// instructions as the sums).
+struct Walk {
+    const uint8_t* p;
+    int row, g;  // (and its head in the group)
+};
+struct Stride {
+    int64_t token, row, step, carry;  // bytes from token to token and head to head, of a step, and where a step passes a token
+    int group, g;
+    __device__ __forceinline__ Stride(const CacheAttendArgs& a, int64_t token_, int64_t row_) : token(token_), row(row_) {
+        const int tokens = token_of(a, kStepRows);
+        group = a.group;
+        g = kStepRows - tokens * group;
+        step = tokens * token + g * row;
+        carry = token - group * row;
+    }
+    // Row r of the sequence whose row 0 is at p.
+    __device__ __forceinline__ Walk at(const CacheAttendArgs& a, const void* p, int r) const {
+        const int t = token_of(a, r), g = r - t * group;
+        return {static_cast<const uint8_t*>(p) + t * token + g * row, r, g};
+    }
+    __device__ __forceinline__ void advance(Walk& w) const {
+        w.row += kStepRows;
+        w.g += g;
+        w.p += step;
+        if (w.g >= group) {
+            w.g -= group;
+            w.p += carry;
+        }
+    }
+};
+
+template <int kBlocks>
+__global__ __launch_bounds__(64 * kWaves, kBlocks == 1 ? 4 : 2) void cache_weigh_rows_kernel(CacheWeighArgs w, int chunks) {
+    __shared__ __align__(16) uint8_t st0[kStageBytes];
+    __shared__ __align__(16) uint8_t st1[kStageBytes];
+    __shared__ __align__(16) uint8_t st2[kStageBytes];
+    __shared__ float s_sum[kKeyWaves * kBlocks * kBlockTokens];
     const CacheAttendArgs& a = w.a;
     const CacheArgs& c = a.c;
-    const int s = blockIdx.x, head = blockIdx.y;
+    const Placed place(a.c, chunks);
+    const int s = place.s, head = place.head;
+    if (s < 0) return;
     const Keys k(a, s);
     if (k.n == 0) return;
     const int past = k.keys - k.n, rows = k.n * a.group;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane & 31, h = lane >> 5;
-    for (int64_t j64 = (int64_t)blockIdx.z * kGroupKeys + wave * kBlocks * kBlockTokens; j64 < k.keys;
-         j64 += (int64_t)gridDim.z * kGroupKeys) {
-        const int base = (int)j64;
-        const int last = (k.keys + kBlockTokens - 1) / kBlockTokens - 1;
+    constexpr int kGroupKeys = kKeyWaves * kBlocks * kBlockTokens;
+    const int last = (k.keys + kBlockTokens - 1) / kBlockTokens - 1;
+    const int mine = (wave & 3) * kBlocks * kBlockTokens, half = wave >> 2;
+    const Stride by_q(a, a.q_stride * 2, kHeadDim * 2), by_stats(a, (int64_t)c.heads * a.group * 8, 8);
+    const uint16_t* q0 = a.q + row_offset(a, k.first, 0, head, a.q_stride);
+    const float2* stats0 = a.stats + row_number(a, k.first, 0, head);
+    const uint8_t* last_q = by_q.at(a, q0, rows - 1).p;
+    const uint8_t* last_stats = by_stats.at(a, stats0, rows - 1).p;
+    for (int64_t j64 = (int64_t)place.chunk * kGroupKeys; j64 < k.keys; j64 += (int64_t)chunks * kGroupKeys) {
+        const int base = (int)j64 + mine;
         KExact keys[kBlocks];
-        int scale[kBlocks];
         float sum[kBlocks][16];
 #pragma unroll
         for (int b = 0; b < kBlocks; b++) {
@@ -103,49 +160,110 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weigh_rows_kernel(CacheW
             uint4 codes[4];
 #pragma unroll
             for (int e = 0; e < 4; e++) codes[e] = *reinterpret_cast<const uint4*>(kb + (4 * (e >> 1) + (e & 1)) * 512);
-            scale[b] = c.ks[p.at];
-            keys[b] = exact_keys(codes, scale[b]);
+            keys[b] = exact_keys(codes, c.ks[p.at]);
 #pragma unroll
             for (int e = 0; e < 16; e++) sum[b][e] = 0.f;
         }
-        // the first row whose token sees key `base`
-        const int from = a.causal ? max(0, base - past) * a.group : 0;
-        for (int row0 = from & ~31; row0 < rows; row0 += 32) {
-            const int row = min(row0 + q, rows - 1);
-            const int end = a.causal ? past + token_of(a, row) + 1 : k.keys;
-            const int min_end = a.causal ? past + token_of(a, row0) + 1 : k.keys;
-            const bool live = row0 + q < rows && end > 0;
-            const QExact qo = load_q_exact(a.q + row_offset(a, k.first, row, head, a.q_stride), h, a.scale, live);
-            float2 ml = make_float2(0.f, 0.f);
-            if (live) ml = a.stats[row_number(a, k.first, row, head)];
+        // the first rows whose tokens see the group's first key
+        const int from = (a.causal ? max(0, (int)j64 - past) * a.group : 0) & ~(kStepRows - 1);
+        const int steps = (rows - from + kStepRows - 1) / kStepRows;
+        Walk r0 = by_q.at(a, q0, from + 8 * wave + (lane >> 4)), r1 = by_q.at(a, q0, from + 8 * wave + 4 + (lane >> 4));
+        Walk rs = by_stats.at(a, stats0, from + 32 * half + q);
+        // the next rows into a stage, 16 lanes a row (behind the last row: that one)
+        auto copy = [&](uint8_t* stage) {
+            const uint8_t* p0 = (r0.row < rows ? r0.p : last_q) + 16 * ((lane ^ r0.row) & 15);
+            const uint8_t* p1 = (r1.row < rows ? r1.p : last_q) + 16 * ((lane ^ r1.row) & 15);
+            __builtin_amdgcn_global_load_lds((global_ptr_t)p0, (lds_ptr_t)(stage + 8 * wave * 256), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr_t)p1, (lds_ptr_t)(stage + (8 * wave + 4) * 256), 16, 0, 0);
+            by_q.advance(r0);
+            by_q.advance(r1);
+        };
+        auto stats = [&] {
+            const float2 x = *reinterpret_cast<const float2*>(rs.row < rows ? rs.p : last_stats);
+            by_stats.advance(rs);
+            return x;
+        };
+        __syncthreads();  // the stages are free
+        copy(st0);
+        if (steps > 1) copy(st1);
+        float2 next = stats();
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        auto one = [&](int step, const uint8_t* cur, uint8_t* far) {
+            const float2 ml = next;
+            if (step + 1 < steps) next = stats();
+            if (step + 2 < steps) copy(far);
+            const int row0 = from + step * kStepRows + 32 * half;
+            // keys that the first and the last row see
+            const int min_end = a.causal ? past + token_of(a, min(row0, rows - 1)) + 1 : k.keys;
+            const int max_end = a.causal ? past + token_of(a, min(row0 + 31, rows - 1)) + 1 : k.keys;
+            if (row0 < rows && max_end > base) {
+                const uint8_t* stage = cur + (32 * half + q) * 256;
+                uint4 qr[8];
 #pragma unroll
-            for (int b = 0; b < kBlocks; b++) {
-                const int at = base + b * kBlockTokens;
-                const v16f x = scores(keys[b], scale[b], qo);
-                const bool any = at + kBlockTokens > min_end;
+                for (int i = 0; i < 8; i++)
+                    qr[i] = *reinterpret_cast<const uint4*>(stage + ((8 * (i >> 2) + 4 * h + (i & 3)) ^ (q & 15)) * 16);
 #pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], qo.c, -ml.x));
-                    const float y = __builtin_fmaf(p, ml.y, sum[b][e]);
-                    sum[b][e] = any && at + 16 * h + e >= end ? sum[b][e] : y;
+                for (int b = 0; b < kBlocks; b++) {
+                    const int at = base + b * kBlockTokens;
+                    v16f x = scores(keys[b], qr);
+                    float2 mb = ml;
+                    if (row0 + 32 > rows || at + kBlockTokens > min_end) {
+                        const int end = row0 + q >= rows ? 0 : a.causal ? past + token_of(a, row0 + q) + 1 : k.keys;
+                        const int seen = end - at - 16 * h;
+#pragma unroll
+                        for (int e = 0; e < 16; e++) x[e] = e < seen ? x[e] : -__builtin_inff();
+                        if (__any(ml.y != ml.y)) {  // a masked key's p is 0, and 0 * NaN would reach it
+                            if (ml.y != ml.y) {
+#pragma unroll
+                                for (int e = 0; e < 16; e++) sum[b][e] = e < seen ? __builtin_nanf("") : sum[b][e];
+                                mb = make_float2(0.f, 0.f);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e++) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.scale, -mb.x));
+                        sum[b][e] = __builtin_fmaf(p, mb.y, sum[b][e]);
+                    }
                 }
             }
+            // the next step's rows landed: what this step copies may still be on its way
+            if (step + 2 < steps)
+                __builtin_amdgcn_s_waitcnt(kTwoInFlight);
+            else
+                __builtin_amdgcn_s_waitcnt(0);
+            // (a fence, as __syncthreads has, would wait for those too)
+            __asm__ volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            __asm__ volatile("" ::: "memory");
+        };
+        for (int step = 0; step < steps; step += 3) {
+            one(step, st0, st2);
+            if (step + 1 < steps) one(step + 1, st1, st0);
+            if (step + 2 < steps) one(step + 2, st2, st1);
         }
-        // the sums of the 32 rows' lanes; lane e of each half keeps that of key 16 h + e
+        // the sums of the 32 rows' lanes; lane e of each half gets that of key 16 h + e
+        float total[kBlocks];
 #pragma unroll
         for (int b = 0; b < kBlocks; b++) {
-            float mine = 0.f;
+            total[b] = 0.f;
 #pragma unroll
             for (int e = 0; e < 16; e++) {
                 float x = sum[b][e];
 #pragma unroll
                 for (int d = 1; d < 32; d *= 2) x += __shfl_xor(x, d);
-                mine = q == e ? x : mine;
+                total[b] = q == e ? x : total[b];
             }
+            if (half && q < 16) s_sum[mine + b * kBlockTokens + 16 * h + q] = total[b];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < kBlocks; b++) {
             const int j = base + b * kBlockTokens + 16 * h + q;
-            if (q >= 16 || j >= k.keys) continue;
+            if (half || q >= 16 || j >= k.keys) continue;
             const int64_t at = weights_at(c, s, head, j);
-            if (at >= 0) w.after[at] = sum_with(w, at, j < past, mine);
+            if (at >= 0) w.after[at] = sum_with(w, at, j < past, total[b] + s_sum[mine + b * kBlockTokens + 16 * h + q]);
         }
     }
 }
@@ -155,10 +273,10 @@ constexpr int64_t kMostScores = (int64_t)1 << 30;
 
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
-// Workgroups along z: one for each `keys` keys, but no launch past 2^32 threads.
-unsigned chunks(const CacheAttendArgs& a, int64_t max_kv, int keys) {
-    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 23) / ((int64_t)a.c.seqs * a.c.heads));
-    return (unsigned)std::min<int64_t>(std::min<int64_t>(most, 65535), (max_kv + keys - 1) / keys);
+// Workgroups of an item: one for each `keys` keys, but no launch past 2^32 threads.
+int chunks_of(const CacheAttendArgs& a, int64_t max_kv, int keys) {
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 22) / ((int64_t)a.c.seqs * a.c.heads));
+    return (int)std::min<int64_t>(most, (max_kv + keys - 1) / keys);
 }
 
 // Chooses the kind, and where what the kernels leave for the sums lies; returns the bytes.
@@ -183,11 +301,12 @@ hipError_t launch_cache_weigh(CacheWeighArgs w, int64_t max_q, int64_t max_kv, h
     lay_out(a, max_q, max_kv);
     if (hipError_t e = launch_cache_attend(a, max_q, max_kv, stream)) return e;
     if (a.kind == kWeigh) {
-        const dim3 grid((unsigned)a.c.seqs, (unsigned)a.c.heads, chunks(a, max_kv, 4 * kThreads));
-        cache_weigh_scores_kernel<<<grid, kThreads, 0, stream>>>(w);
+        const int chunks = chunks_of(a, max_kv, 4 * kThreads);
+        cache_weigh_scores_kernel<<<placed_grid(a.c, chunks), kThreads, 0, stream>>>(w, chunks);
     } else {
-        const dim3 grid((unsigned)a.c.seqs, (unsigned)a.c.heads, chunks(a, max_kv, kGroupKeys));
-        cache_weigh_rows_kernel<<<grid, 64 * kWaves, 0, stream>>>(w);
+        constexpr int kBlocks = 1;
+        const int chunks = chunks_of(a, max_kv, kKeyWaves * kBlocks * kBlockTokens);
+        cache_weigh_rows_kernel<kBlocks><<<placed_grid(a.c, chunks), 64 * kWaves, 0, stream>>>(w, chunks);
     }
     return hipGetLastError();
 }

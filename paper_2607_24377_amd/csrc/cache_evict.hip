@@ -35,11 +35,22 @@ __device__ __forceinline__ uint32_t ordered(float w) {
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// The weights of a head's stretch j0 .. j1 - 1, j0 a multiple of 4, 1024 at a time: f gets
-// a position and four weights, ordered (of no page: as NaN), position by position of the
-// wave's lanes.  (One at a time: two loads after each other for every 64.)
+// The number whose order is u, -0 as +0; NaN for 0.
+__device__ __forceinline__ float number_of(uint32_t u) {
+    return __builtin_bit_cast(float, u >> 31 ? u & 0x7FFFFFFFu : ~u);
+}
+
+// Lanes before this one in a mask.
+__device__ __forceinline__ uint32_t lanes_before(uint64_t mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// The weights of a head's stretch j0 .. j1 - 1, j0 a multiple of 256, four a lane, 1024 at a
+// time: f gets the lane's first position, its four weights (of no page: NaN), and which of
+// them are of the stretch and between m0 and m1 (as bits), or are of it and not between.
+// (One at a time: two loads after each other for every 64.)
 template <class F>
-__device__ __forceinline__ void for_weights(const SelectArgs& a, int s, int head, int j0, int j1, const F& f) {
+__device__ __forceinline__ void for_weights(const SelectArgs& a, int s, int head, int j0, int j1, int m0, int m1, const F& f) {
     const CacheArgs& c = a.c;
     const int lane = threadIdx.x & 63, log2 = c.bpp_log2 + 5;
     const int32_t* table = c.page_table + (int64_t)s * c.max_pages;
@@ -59,11 +70,30 @@ __device__ __forceinline__ void for_weights(const SelectArgs& a, int s, int head
         }
 #pragma unroll
         for (int i = 0; i < kTurns; i++) {
-            if (j + 256 * i >= j1) break;
-            const uint32_t u[4] = {ordered(w[i][0]), ordered(w[i][1]), ordered(w[i][2]), ordered(w[i][3])};
-            f(j + 256 * i + 4 * lane, u);
+            const int at = j + 256 * i, p = at + 4 * lane;
+            if (at >= j1) break;
+            if (at >= m0 && at + 256 <= min(m1, j1)) {
+                f(p, w[i], 15u, 0u);
+            } else {
+                uint32_t free = 0, forced = 0;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    if (p + k >= j1) continue;
+                    if (p + k >= m0 && p + k < m1)
+                        free |= 1u << k;
+                    else
+                        forced |= 1u << k;
+                }
+                f(p, w[i], free, forced);
+            }
         }
     }
+}
+
+__device__ __forceinline__ uint32_t sum64(uint32_t x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += (uint32_t)__shfl_xor((int)x, d);
+    return x;
 }
 
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs a) {
@@ -112,28 +142,41 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs
                 if ((s_aside[i] & known) == prefix) add(s_aside[i]);
         } else {
             uint32_t above = 0;
-            for_weights(a, s, head, j0, j1, [&](int j, const uint32_t (&u)[4]) {
+            for_weights(a, s, head, j0, j1, m0, m1, [&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
+                uint32_t u[4], mine = 0, more = forced;
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    const bool in = j + i < j1;
-                    const bool free = in && j + i >= m0 && j + i < m1;
-                    const bool mine = free && (u[i] & known) == prefix;
-                    if (mine) add(u[i]);
-                    if (fits) {
-                        above += (uint32_t)__popcll(__ballot(in && (!free || (u[i] & known) > prefix)));
-                        const uint64_t all = __ballot(mine);
-                        if (all) {
-                            uint32_t at = 0;
-                            if (lane == 0) at = atomicAdd(&s_count, (uint32_t)__popcll(all));
-                            at = __builtin_amdgcn_readfirstlane((int)at) + (uint32_t)__popcll(all & (((uint64_t)1 << lane) - 1));
-                            if (mine) {
-                                s_aside[at] = u[i];
-                                s_whose[at] = (uint8_t)wave;
-                            }
-                        }
+                    u[i] = ordered(w[i]);
+                    const uint32_t d = u[i] & known;
+                    if (!(free >> i & 1)) continue;
+                    if (d == prefix) {
+                        add(u[i]);
+                        mine |= 1u << i;
+                    }
+                    if (d > prefix) more |= 1u << i;
+                }
+                if (!fits) return;
+                above += (uint32_t)__popc(more);
+                if (__any(mine != 0)) {  // room for the wave's at once
+                    uint32_t before = 0, total = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const uint64_t b = __ballot(mine >> i & 1);
+                        before += lanes_before(b);
+                        total += (uint32_t)__popcll(b);
+                    }
+                    uint32_t at = 0;
+                    if (lane == 0) at = atomicAdd(&s_count, total);
+                    at = __builtin_amdgcn_readfirstlane((int)at) + before;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        if (!(mine >> i & 1)) continue;
+                        s_aside[at] = u[i];
+                        s_whose[at++] = (uint8_t)wave;
                     }
                 }
             });
+            above = sum64(above);
             if (fits && lane == 0) s_above[wave] = above;
         }
         aside = aside || fits;
@@ -171,7 +214,22 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs
         need = s_found[1];
         known |= mask << shift;
     }
-    // how many of each wave's stretch stay for their weight or place, and have the last one's weight
+    // which of a lane's four stay for their weight or place, and which have the last one's weight
+    const float border = number_of(prefix);
+    auto look = [&](const f32x4u& w, uint32_t free, uint32_t forced, uint32_t& x, uint32_t& y) {
+        x = y = 0;
+        if (any) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                // (0 is NaN's place: every number is above it)
+                x |= (uint32_t)(prefix ? w[i] > border : w[i] == w[i]) << i;
+                y |= (uint32_t)(prefix ? w[i] == border : w[i] != w[i]) << i;
+            }
+        }
+        x = (x & free) | forced;
+        y &= free;
+    };
+    // how many of each wave's stretch do
     if (aside) {
         const int n = (int)s_count;
         for (int i = tid; i < n; i += kSelectThreads) {
@@ -180,14 +238,14 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs
         }
     } else {
         uint32_t above = 0, equal = 0;
-        for_weights(a, s, head, j0, j1, [&](int j, const uint32_t (&u)[4]) {
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const bool in = j + i < j1, free = in && j + i >= m0 && j + i < m1;
-                above += (uint32_t)__popcll(__ballot(in && (!free || (any && u[i] > prefix))));
-                equal += (uint32_t)__popcll(__ballot(free && any && u[i] == prefix));
-            }
+        for_weights(a, s, head, j0, j1, m0, m1, [&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
+            uint32_t x, y;
+            look(w, free, forced, x, y);
+            above += (uint32_t)__popc(x);
+            equal += (uint32_t)__popc(y);
         });
+        above = sum64(above);
+        equal = sum64(equal);
         if (lane == 0) {
             s_above[wave] = above;
             s_equal[wave] = equal;
@@ -199,26 +257,31 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs
         at += s_above[k];
         same += s_equal[k];
     }
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for_weights(a, s, head, j0, j1, [&](int j, const uint32_t (&u)[4]) {
-        bool x[4], y[4];
-        uint32_t ax = at, ay = same;  // before this lane's four
+    for_weights(a, s, head, j0, j1, m0, m1, [&](int j, const f32x4u& w, uint32_t free, uint32_t forced) {
+        uint32_t x, y;
+        look(w, free, forced, x, y);
+        uint32_t ax = at;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const bool in = j + i < j1, free = in && j + i >= m0 && j + i < m1;
-            x[i] = in && (!free || (any && u[i] > prefix));
-            y[i] = free && any && u[i] == prefix;
-            const uint64_t bx = __ballot(x[i]), by = __ballot(y[i]);
-            ax += (uint32_t)__popcll(bx & below);
-            ay += (uint32_t)__popcll(by & below);
-            at += (uint32_t)__popcll(bx);
-            same += (uint32_t)__popcll(by);
+            const uint64_t b = __ballot(x >> i & 1);
+            ax += lanes_before(b);
+            at += (uint32_t)__popcll(b);
+        }
+        uint32_t ay = same;
+        if (__any(y != 0)) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint64_t b = __ballot(y >> i & 1);
+                ay += lanes_before(b);
+                same += (uint32_t)__popcll(b);
+            }
         }
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            if (x[i] || (y[i] && ay < need)) kept[ax + min(ay, need)] = j + i;
-            ax += x[i];
-            ay += y[i];
+            const uint32_t xi = x >> i & 1, yi = y >> i & 1;
+            if (xi | (yi & (uint32_t)(ay < need))) kept[ax + min(ay, need)] = j + i;
+            ax += xi;
+            ay += yi;
         }
     });
 }

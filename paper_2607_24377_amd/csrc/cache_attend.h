@@ -504,10 +504,12 @@ struct Sight {
 };
 
 // One block for the wave's rows at `base`; `scores_at`: where the row's scores are kept
-// (kWeigh; null: nowhere).
-template <AttendKind kKind, class Q>
+// (kWeigh; null: nowhere).  `prefetch` loads the next one: first of all, but after stores
+// (loads that stores under a condition follow, the compiler has to wait for with those).
+template <AttendKind kKind, class Q, class Prefetch>
 __device__ __forceinline__ void attend_block(State& st, Block& x, const Q& q, int base, const Sight<kKind>& sight,
-                                             float* scores_at, int h) {
+                                             float* scores_at, int h, const Prefetch& prefetch) {
+    if constexpr (kKind != kWeigh) prefetch();
     const bool any = sight.partial(base);
     const auto sees = sight.mask_of(base, any);
     if (any || x.lost) clean_values(st, x.v, x.ve, sees, sight.keys - base, x.lost, h);
@@ -524,6 +526,7 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const Q& q, in
                 *reinterpret_cast<float4*>(scores_at + base + 16 * h + i) =
                     make_float4(s[i] * q.c, s[i + 1] * q.c, s[i + 2] * q.c, s[i + 3] * q.c);
         }
+        prefetch();
     }
     consume(st, s, x.v, x.ve, q.c, sees, any, h);
 }

@@ -88,11 +88,14 @@ __device__ __forceinline__ void attend_run(State& st, const CacheArgs& c, int s,
     load_block(x, c, block_at(c, page_of(c, s, sight.block(v0)), head, sight.block(v0)), q, h);
     int page = page_of(c, s, sight.block(min(v0 + step, last)));
     for (int v = v0;; v += step) {
-        if (v + step < v1) {
-            load_block(y, c, block_at(c, page, head, sight.block(v + step)), q, h);
+        // (behind the last block that one again: loads under a condition, the compiler waits
+        // for the next block before this one)
+        auto prefetch = [&] {
+            const int next = sight.block(min(v + step, last));
+            load_block(y, c, block_at(c, page, head, next), q, h);
             page = page_of(c, s, sight.block(min(v + 2 * step, last)));
-        }
-        attend_block<kKind>(st, x, qo, sight.block(v) * kBlockTokens, sight, scores_at, h);
+        };
+        attend_block<kKind>(st, x, qo, sight.block(v) * kBlockTokens, sight, scores_at, h, prefetch);
         if (v + step >= v1) break;
         x = y;
     }

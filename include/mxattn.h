@@ -471,10 +471,16 @@ size_t mxattn_cache_attend_weights_workspace(int64_t page_tokens, int64_t seqs, 
  *   kept     device int32 [seqs, Hkv, budget]: their positions, ascending, then -1
  *   counts   device int32 [seqs]: min(kv_len, budget); 0 for an impossible length
  *   budget   1 .. 2^24, sinks >= 0, recent >= 0, sinks + recent <= budget
- *            (MXATTN_ERR_VALUE otherwise); seqs * Hkv < 2^22 */
+ *            (MXATTN_ERR_VALUE otherwise); seqs * Hkv < 2^22
+ *   workspace  as mxattn_cache_attend's, of mxattn_cache_select_workspace() bytes: none
+ *            where max_pages * page_tokens <= 16384, else at most 1.2 MB for each sequence
+ *            and KV head.  It shares no byte with the other arguments.  NULL: from the
+ *            library's pool, not under graph capture. */
 int mxattn_cache_select(const float* weights, int64_t pages, int64_t page_tokens, const int32_t* page_table,
                         const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t Hkv, int64_t budget,
-                        int64_t sinks, int64_t recent, int32_t* kept, int32_t* counts, void* stream);
+                        int64_t sinks, int64_t recent, int32_t* kept, int32_t* counts, void* workspace,
+                        size_t workspace_bytes, void* stream);
+size_t mxattn_cache_select_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t Hkv);
 
 /* Move kept tokens together: position base + i of a sequence (i < counts) becomes what was
  * at position kept[i], K, V and weights; the sequence's length is then base + counts.

@@ -72,7 +72,7 @@ const char* mxattn_status_string(int s) {
         case MXATTN_ERR_UNSUPPORTED: return "unsupported head dimension (d must be 128)";
         case MXATTN_ERR_OOM: return "workspace allocation failed";
         case MXATTN_ERR_HIP: return "HIP runtime error";
-        case MXATTN_ERR_SCRATCH: return "more scratch needed than there is (the no-allocation entry point: B*H*ceil(Nkv/128) <= 32768; cache attention: a workspace of mxattn_cache_attend_workspace() or mxattn_cache_attend_weights_workspace() bytes from the caller, always on a stream under graph capture)";
+        case MXATTN_ERR_SCRATCH: return "more scratch needed than there is (the no-allocation entry point: B*H*ceil(Nkv/128) <= 32768; cache attention: a workspace of mxattn_cache_attend_workspace() or mxattn_cache_attend_weights_workspace() bytes, selection: of mxattn_cache_select_workspace(), from the caller, always on a stream under graph capture)";
         case MXATTN_ERR_BOUNDARY: return "invalid scale boundary (need 4 <= q <= 8 and 1 <= nq <= 64) or pre-scale (need 0 < gamma < 3e38)";
         case MXATTN_ERR_VALUE: return "invalid value (rot 0 or a multiple of 16 up to 128, pairs 0 or 1, eps finite and >= 0, page_tokens a power of two from 32 to 4096, Hq a multiple of Hkv, at most 256 of it, window >= 1, sinks and recent >= 0 and together at most a budget of 1 to 2^24)";
         default: return "unknown status";
@@ -799,48 +799,58 @@ static int check_attend(AttendCall& x, mxattn::CacheAttendArgs& a) {
     return MXATTN_OK;
 }
 
-extern "C++" {  // (a template)
-// Runs `launch(workspace)` with `bytes` of workspace: the caller's, or the library's where it gives none.
-template <class Launch>
-static int run_attend(const AttendCall& x, const mxattn::CacheArgs& c, size_t bytes, Launch launch) {
+extern "C++" {  // (templates)
+// Runs `launch(workspace)` of the call `name` with `bytes` of workspace: the caller's, which must be as large and clash
+// with nothing (`clash(from, bytes)`), or the library's where it gives none.
+template <class Clash, class Launch>
+static int run_with(const char* name, void* workspace, size_t workspace_bytes, size_t bytes, hipStream_t stream,
+                    const char* what, Clash clash, Launch launch) {
     uint8_t* memory = nullptr;
     Workspace ws;
-    if (bytes && x.workspace) {
-        if (x.workspace_bytes < bytes) {
-            std::snprintf(g_last_error, sizeof g_last_error, "%s: %zu bytes of workspace needed, the caller's has %zu", x.name,
-                          bytes, x.workspace_bytes);
+    if (bytes && workspace) {
+        if (workspace_bytes < bytes) {
+            std::snprintf(g_last_error, sizeof g_last_error, "%s: %zu bytes of workspace needed, the caller's has %zu", name,
+                          bytes, workspace_bytes);
             return MXATTN_ERR_SCRATCH;
         }
-        if (!aligned(x.workspace, 16)) return MXATTN_ERR_ALIGN;
-        if (overlaps(x.workspace, bytes, x.q, x.q_bytes) || overlaps(x.workspace, bytes, x.out, x.out_bytes) ||
-            in_cache(x.workspace, bytes, c))
-            return MXATTN_ERR_SHAPE;
-        memory = static_cast<uint8_t*>(x.workspace);
+        if (!aligned(workspace, 16)) return MXATTN_ERR_ALIGN;
+        if (clash(workspace, bytes)) return MXATTN_ERR_SHAPE;
+        memory = static_cast<uint8_t*>(workspace);
         bytes = 0;
     } else if (bytes) {
         // an allocation of the pool is not recorded into a graph: its replays need memory that lasts
         hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-        if (x.stream) {
-            if (hipError_t e = hipStreamIsCapturing(x.stream, &capture)) {
+        if (stream) {
+            if (hipError_t e = hipStreamIsCapturing(stream, &capture)) {
                 set_error("hipStreamIsCapturing", e);
                 return MXATTN_ERR_HIP;
             }
         }
         if (capture != hipStreamCaptureStatusNone) {
             std::snprintf(g_last_error, sizeof g_last_error,
-                          "%s: %zu bytes of workspace needed from the caller, as the stream is being captured", x.name, bytes);
+                          "%s: %zu bytes of workspace needed from the caller, as the stream is being captured", name, bytes);
             return MXATTN_ERR_SCRATCH;
         }
-        if (int st = ws.take(bytes, x.stream)) return st;
+        if (int st = ws.take(bytes, stream)) return st;
         memory = ws.get();
     }
     int st = MXATTN_OK;
     hipError_t e = launch(memory);
     if (e != hipSuccess) {
-        set_error("cache attention launch", e);
+        set_error(what, e);
         st = MXATTN_ERR_HIP;
     }
     return bytes ? ws.give_back(st) : st;
+}
+
+template <class Launch>
+static int run_attend(const AttendCall& x, const mxattn::CacheArgs& c, size_t bytes, Launch launch) {
+    return run_with(
+        x.name, x.workspace, x.workspace_bytes, bytes, x.stream, "cache attention launch",
+        [&](const void* p, size_t n) {
+            return overlaps(p, n, x.q, x.q_bytes) || overlaps(p, n, x.out, x.out_bytes) || in_cache(p, n, c);
+        },
+        launch);
 }
 }  // extern "C++"
 
@@ -943,7 +953,8 @@ static int check_items(int64_t seqs, int64_t Hkv) { return seqs * Hkv >> 22 ? MX
 
 int mxattn_cache_select(const float* weights, int64_t pages, int64_t page_tokens, const int32_t* page_table,
                         const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t Hkv, int64_t budget, int64_t sinks,
-                        int64_t recent, int32_t* kept, int32_t* counts, void* stream) {
+                        int64_t recent, int32_t* kept, int32_t* counts, void* workspace, size_t workspace_bytes,
+                        void* stream) {
     if (!weights || !page_table || !kv_len || !kept || !counts) return MXATTN_ERR_NULL;
     mxattn::SelectArgs a{};
     if (int st = check_pages(a.c, pages, page_tokens, page_table, seqs, max_pages, 1, Hkv)) return st;
@@ -964,12 +975,25 @@ int mxattn_cache_select(const float* weights, int64_t pages, int64_t page_tokens
     a.recent = (int)recent;
     a.kept = kept;
     a.counts = counts;
-    hipError_t e = mxattn::launch_cache_select(a, reinterpret_cast<hipStream_t>(stream));
-    if (e != hipSuccess) {
-        set_error("cache selection launch", e);
-        return MXATTN_ERR_HIP;
-    }
-    return MXATTN_OK;
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    return run_with(
+        "mxattn_cache_select", workspace, workspace_bytes, mxattn::cache_select_workspace(seqs * Hkv, max_pages * page_tokens),
+        st, "cache selection launch",
+        [&](const void* p, size_t n) {
+            return overlaps(p, n, weights, wb) || overlaps(p, n, kept, kb) || overlaps(p, n, counts, cb) ||
+                   overlaps(p, n, kv_len, cb) || overlaps(p, n, page_table, tb);
+        },
+        [&](uint8_t* memory) {
+            a.workspace = memory;
+            return mxattn::launch_cache_select(a, st);
+        });
+}
+
+size_t mxattn_cache_select_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t Hkv) {
+    if (page_tokens < 32 || page_tokens > 4096 || (page_tokens & (page_tokens - 1)) != 0 ||
+        check_batch(seqs, max_pages, page_tokens, 1, Hkv) || check_items(seqs, Hkv))
+        return 0;
+    return mxattn::cache_select_workspace(seqs * Hkv, max_pages * page_tokens);
 }
 
 int mxattn_cache_compact(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int64_t pages,

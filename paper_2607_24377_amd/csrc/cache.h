@@ -111,7 +111,12 @@ struct SelectArgs {
     int budget, sinks, recent;
     int32_t* kept;         // [seqs, heads, budget]
     int32_t* counts;       // [seqs]
+    uint8_t* workspace;    // cache_select_workspace bytes, 16-byte aligned
+    int chunk_keys, chunks;  // set by the launcher, as what follows
+    size_t item_bytes;
 };
+// items: sequences times heads; reach: the most keys of a sequence that its table holds.
+size_t cache_select_workspace(int64_t items, int64_t reach);
 hipError_t launch_cache_select(const SelectArgs& a, hipStream_t stream);
 
 struct CompactArgs {

@@ -1,12 +1,10 @@
 // cache_evict.hip -- which tokens of a cache stay, and moving those that stay together.
 //
 // Selection: of a sequence's L keys of one KV head the first `sinks`, the last `recent`
-// and, of those between, the heaviest, `budget` in all.  A workgroup finds the weight of
-// the last one that stays digit by digit (11, 11 and 10 bits of the number in an order of
-// unsigned integers, a histogram in LDS for each), then writes the kept positions in
-// order: each wave starts where the stretches before its own end.  What shares the digits
-// found so far is put aside in LDS as soon as it fits, so that the weights are read three
-// times (histogram, putting aside, writing).
+// and, of those between, the heaviest, `budget` in all.  The weight of the last one that
+// stays is found digit by digit (11, 11 and 10 bits of the number in an order of unsigned
+// integers, histograms in LDS); then the kept positions are written in order, each wave
+// from where the stretches before its own end.
 //
 // Compaction: position base + i becomes what was at kept[i].  A block of 32 kept tokens
 // takes the largest scale byte of the blocks that they come from, so that no code grows
@@ -21,11 +19,7 @@
 namespace mxattn {
 namespace {
 
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kDigits = 2048;
-constexpr int kCopies = 8;      // of the histogram: weights share few of the first digits
-constexpr int kAside = 8192;
 
 // Weights in the order of unsigned integers; NaN below every number, -0 with +0.
 __device__ __forceinline__ uint32_t ordered(float w) {
@@ -45,19 +39,23 @@ __device__ __forceinline__ uint32_t lanes_before(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// The weights of a head's stretch j0 .. j1 - 1, j0 a multiple of 256, four a lane, 1024 at a
-// time: f gets the lane's first position, its four weights (of no page: NaN), and which of
-// them are of the stretch and between m0 and m1 (as bits), or are of it and not between.
-// (One at a time: two loads after each other for every 64.)
-template <class F>
-__device__ __forceinline__ void for_weights(const SelectArgs& a, int s, int head, int j0, int j1, int m0, int m1, const F& f) {
-    const CacheArgs& c = a.c;
-    const int lane = threadIdx.x & 63, log2 = c.bpp_log2 + 5;
-    const int32_t* table = c.page_table + (int64_t)s * c.max_pages;
-    constexpr int kTurns = 4;
-    for (int j = j0; j < j1; j += 256 * kTurns) {
+// A wave's stretch j0 .. j1 - 1 of a head's weights, j0 a multiple of 256; those from m0 to
+// m1 - 1 may go.  each(f): f gets the lane's first position of four, their weights (of no
+// page: NaN), and which of them are of the stretch and may go (as bits), or may not.
+struct Stretch {
+    static constexpr int kTurns = 4;  // 1024 positions in flight, and kept if there are no more
+    const SelectArgs& a;
+    int s, head, j0, j1, m0, m1;
+    f32x4u w[kTurns];
+    __device__ __forceinline__ Stretch(const SelectArgs& a_, int s_, int head_, int j0_, int j1_, int m0_, int m1_)
+        : a(a_), s(s_), head(head_), j0(j0_), j1(j1_), m0(m0_), m1(m1_) {
+        if (j0 < j1) load(j0);
+    }
+    __device__ __forceinline__ void load(int j) {
+        const CacheArgs& c = a.c;
+        const int lane = threadIdx.x & 63, log2 = c.bpp_log2 + 5;
+        const int32_t* table = c.page_table + (int64_t)s * c.max_pages;
         int page[kTurns];
-        f32x4u w[kTurns];
 #pragma unroll
         for (int i = 0; i < kTurns; i++) page[i] = table[min(j + 256 * i + 4 * lane, j1 - 1) >> log2];
 #pragma unroll
@@ -68,27 +66,33 @@ __device__ __forceinline__ void for_weights(const SelectArgs& a, int s, int head
                 a.weights + (((int64_t)(there ? page[i] : 0) * c.heads + head) << log2) + (at & ((1 << log2) - 1)));
             if (!there) w[i] = f32x4u{0.f, 0.f, 0.f, 0.f} * __builtin_nanf("");
         }
+    }
+    template <class F>
+    __device__ __forceinline__ void each(const F& f) {
+        for (int j = j0; j < j1; j += 256 * kTurns) {
+            if (j1 - j0 > 256 * kTurns) load(j);
 #pragma unroll
-        for (int i = 0; i < kTurns; i++) {
-            const int at = j + 256 * i, p = at + 4 * lane;
-            if (at >= j1) break;
-            if (at >= m0 && at + 256 <= min(m1, j1)) {
-                f(p, w[i], 15u, 0u);
-            } else {
-                uint32_t free = 0, forced = 0;
+            for (int i = 0; i < kTurns; i++) {
+                const int at = j + 256 * i, p = at + 4 * (threadIdx.x & 63);
+                if (at >= j1) break;
+                if (at >= m0 && at + 256 <= min(m1, j1)) {
+                    f(p, w[i], 15u, 0u);
+                } else {
+                    uint32_t free = 0, forced = 0;
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    if (p + k >= j1) continue;
-                    if (p + k >= m0 && p + k < m1)
-                        free |= 1u << k;
-                    else
-                        forced |= 1u << k;
+                    for (int k = 0; k < 4; k++) {
+                        if (p + k >= j1) continue;
+                        if (p + k >= m0 && p + k < m1)
+                            free |= 1u << k;
+                        else
+                            forced |= 1u << k;
+                    }
+                    f(p, w[i], free, forced);
                 }
-                f(p, w[i], free, forced);
             }
         }
     }
-}
+};
 
 __device__ __forceinline__ uint32_t sum64(uint32_t x) {
 #pragma unroll
@@ -96,194 +100,456 @@ __device__ __forceinline__ uint32_t sum64(uint32_t x) {
     return x;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(SelectArgs a) {
-    __shared__ __align__(16) uint32_t s_hist[kDigits * kCopies];
-    __shared__ uint32_t s_aside[kAside];
-    __shared__ uint8_t s_whose[kAside];
-    __shared__ uint32_t s_wave[kSelectWaves];
-    __shared__ uint32_t s_found[3];  // the digit of the last one that stays, how many of it do, how many there are
-    __shared__ uint32_t s_above[kSelectWaves], s_equal[kSelectWaves], s_count;
-    const CacheArgs& c = a.c;
-    // (head by head: the XCDs take workgroups in turn, and the heads of a sequence spread over them)
-    const int s = (int)(blockIdx.x / (unsigned)c.heads), head = (int)blockIdx.x - s * c.heads, tid = threadIdx.x;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int len = c.kv_len[s], L = (unsigned)len > (unsigned)(c.max_pages << (c.bpp_log2 + 5)) ? 0 : len;
-    const int count = min(L, a.budget);
-    int32_t* kept = a.kept + ((int64_t)s * c.heads + head) * a.budget;
-    if (head == 0 && tid == 0) a.counts[s] = count;
-    for (int i = count + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
-    if (L <= a.budget) {
-        for (int i = tid; i < L; i += kSelectThreads) kept[i] = i;
-        return;
+// The search: `prefix` in the bits of `known` is what the weight of the last one that stays
+// begins with, and `need` of those that begin so stay.
+struct Search {
+    uint32_t prefix, known, need;
+    // The digits of the three passes.
+    static __device__ __forceinline__ int shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+    static __device__ __forceinline__ uint32_t mask(int pass) { return pass == 2 ? 1023 : 2047; }
+};
+
+// Histograms of a workgroup of kThreads threads, kCopies of each (weights share few of the first digits).
+template <int kThreads, int kCopies>
+struct Histogram {
+    uint32_t bins[kDigits * kCopies];
+    uint32_t wave[kThreads / 64], found[3];
+    __device__ __forceinline__ void clear() {
+        for (int i = threadIdx.x; i < kDigits * kCopies / 4; i += kThreads)
+            reinterpret_cast<uint4*>(bins)[i] = make_uint4(0, 0, 0, 0);
     }
-    const int m0 = a.sinks, m1 = L - a.recent;  // what lies between may go
-    // a stretch of all positions for each wave
-    const int per = (L + 256 * kSelectWaves - 1) / (256 * kSelectWaves) * 256;
-    const int j0 = min(wave * per, L), j1 = min(j0 + per, L);
-    if (tid < kSelectWaves) s_above[tid] = s_equal[tid] = 0;
-    if (tid == 0) s_count = 0;
-    // the weight of the last one that stays, `prefix` in the bits of `known`, and how many
-    // of exactly that weight do
-    uint32_t prefix = 0, known = 0;
-    uint32_t need = (uint32_t)(a.budget - a.sinks - a.recent);  // below the number of those between
-    const bool any = need > 0;
-    bool aside = false;  // what shares the known digits is in s_aside, what is above them counted
-    for (int pass = 0; any && pass < 3; pass++) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-        const uint32_t mask = pass == 2 ? 1023 : 2047;
-        const bool fits = pass > 0 && !aside && s_found[2] <= kAside;
-        for (int i = tid; i < kDigits * kCopies / 4; i += kSelectThreads)
-            reinterpret_cast<uint4*>(s_hist)[i] = make_uint4(0, 0, 0, 0);
-        __syncthreads();
-        auto add = [&](uint32_t u) { atomicAdd(&s_hist[((u >> shift) & mask) * kCopies + (lane & (kCopies - 1))], 1u); };
-        if (aside) {
-            const int n = (int)s_count;
-            for (int i = tid; i < n; i += kSelectThreads)
-                if ((s_aside[i] & known) == prefix) add(s_aside[i]);
-        } else {
-            uint32_t above = 0;
-            for_weights(a, s, head, j0, j1, m0, m1, [&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
-                uint32_t u[4], mine = 0, more = forced;
+    __device__ __forceinline__ void add(uint32_t u, int pass) {
+        atomicAdd(&bins[((u >> Search::shift(pass)) & Search::mask(pass)) * kCopies + (threadIdx.x & (kCopies - 1))], 1u);
+    }
+    __device__ __forceinline__ uint32_t total(int digit) const {
+        uint32_t n = 0;
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    u[i] = ordered(w[i]);
-                    const uint32_t d = u[i] & known;
-                    if (!(free >> i & 1)) continue;
-                    if (d == prefix) {
-                        add(u[i]);
-                        mine |= 1u << i;
-                    }
-                    if (d > prefix) more |= 1u << i;
-                }
-                if (!fits) return;
-                above += (uint32_t)__popc(more);
-                if (__any(mine != 0)) {  // room for the wave's at once
-                    uint32_t before = 0, total = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const uint64_t b = __ballot(mine >> i & 1);
-                        before += lanes_before(b);
-                        total += (uint32_t)__popcll(b);
-                    }
-                    uint32_t at = 0;
-                    if (lane == 0) at = atomicAdd(&s_count, total);
-                    at = __builtin_amdgcn_readfirstlane((int)at) + before;
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        if (!(mine >> i & 1)) continue;
-                        s_aside[at] = u[i];
-                        s_whose[at++] = (uint8_t)wave;
-                    }
-                }
-            });
-            above = sum64(above);
-            if (fits && lane == 0) s_above[wave] = above;
+        for (int k = 0; k < kCopies; k += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(bins + digit * kCopies + k);
+            n += v.x + v.y + v.z + v.w;
         }
-        aside = aside || fits;
-        __syncthreads();
-        // thread t has digits 2 t and 2 t + 1 from the largest down
-        uint32_t x = 0, y = 0;
-        const uint4* pair = reinterpret_cast<const uint4*>(s_hist + (kDigits - 2 - 2 * tid) * kCopies);
+        return n;
+    }
+    // The digit of the last one that stays; n[i]: the number of digit kDigits - 1 - kEach tid - i.
+    // Returns how many have it.  Barriers before and after.
+    static constexpr int kEach = kDigits / kThreads;
+    __device__ __forceinline__ uint32_t find(Search& x, int pass, const uint32_t (&n)[kEach]) {
+        const int tid = threadIdx.x, lane = tid & 63;
+        uint32_t sum = 0;
 #pragma unroll
-        for (int k = 0; k < kCopies / 4; k++) {
-            const uint4 v = pair[k], w = pair[kCopies / 4 + k];
-            y += v.x + v.y + v.z + v.w;
-            x += w.x + w.y + w.z + w.w;
-        }
-        uint32_t incl = x + y;
+        for (int i = 0; i < kEach; i++) sum += n[i];
+        uint32_t incl = sum;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const uint32_t v = (uint32_t)__shfl_up((int)incl, d);
             if (lane >= d) incl += v;
         }
-        if (lane == 63) s_wave[wave] = incl;
+        if (lane == 63) wave[tid >> 6] = incl;
         __syncthreads();
-        uint32_t before = incl - x - y;
-        for (int k = 0; k < wave; k++) before += s_wave[k];
-        if (before < need && need <= before + x) {
-            s_found[0] = (uint32_t)(kDigits - 1 - 2 * tid);
-            s_found[1] = need - before;
-            s_found[2] = x;
-        } else if (before + x < need && need <= before + x + y) {
-            s_found[0] = (uint32_t)(kDigits - 2 - 2 * tid);
-            s_found[1] = need - before - x;
-            s_found[2] = y;
-        }
-        __syncthreads();
-        prefix |= s_found[0] << shift;
-        need = s_found[1];
-        known |= mask << shift;
-    }
-    // which of a lane's four stay for their weight or place, and which have the last one's weight
-    const float border = number_of(prefix);
-    auto look = [&](const f32x4u& w, uint32_t free, uint32_t forced, uint32_t& x, uint32_t& y) {
-        x = y = 0;
-        if (any) {
+        uint32_t before = incl - sum;
+        for (int k = 0; k < (tid >> 6); k++) before += wave[k];
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                // (0 is NaN's place: every number is above it)
-                x |= (uint32_t)(prefix ? w[i] > border : w[i] == w[i]) << i;
-                y |= (uint32_t)(prefix ? w[i] == border : w[i] != w[i]) << i;
+        for (int i = 0; i < kEach; i++) {
+            if (before < x.need && x.need <= before + n[i]) {
+                found[0] = (uint32_t)(kDigits - 1 - kEach * tid - i);
+                found[1] = x.need - before;
+                found[2] = n[i];
             }
+            before += n[i];
         }
-        x = (x & free) | forced;
-        y &= free;
-    };
-    // how many of each wave's stretch do
-    if (aside) {
-        const int n = (int)s_count;
-        for (int i = tid; i < n; i += kSelectThreads) {
-            if (s_aside[i] > prefix) atomicAdd(&s_above[s_whose[i]], 1u);
-            if (s_aside[i] == prefix) atomicAdd(&s_equal[s_whose[i]], 1u);
-        }
-    } else {
-        uint32_t above = 0, equal = 0;
-        for_weights(a, s, head, j0, j1, m0, m1, [&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
-            uint32_t x, y;
-            look(w, free, forced, x, y);
-            above += (uint32_t)__popc(x);
-            equal += (uint32_t)__popc(y);
-        });
-        above = sum64(above);
-        equal = sum64(equal);
-        if (lane == 0) {
-            s_above[wave] = above;
-            s_equal[wave] = equal;
+        __syncthreads();
+        x.prefix |= found[0] << Search::shift(pass);
+        x.known |= Search::mask(pass) << Search::shift(pass);
+        x.need = found[1];
+        return found[2];
+    }
+    __device__ __forceinline__ uint32_t find(Search& x, int pass) {
+        uint32_t n[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; i++) n[i] = total(kDigits - 1 - kEach * (int)threadIdx.x - i);
+        return find(x, pass, n);
+    }
+};
+
+// What a wave puts aside: the weights (ordered) among a lane's four that begin with the
+// prefix, from place `at` of all on; room for the wave's is taken at once.
+template <class Store>
+__device__ __forceinline__ void put_aside(uint32_t mine, const uint32_t (&u)[4], uint32_t* count, const Store& store) {
+    if (!__any(mine != 0)) return;
+    uint32_t before = 0, total = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint64_t b = __ballot(mine >> i & 1);
+        before += lanes_before(b);
+        total += (uint32_t)__popcll(b);
+    }
+    uint32_t at = 0;
+    if ((threadIdx.x & 63) == 0) at = atomicAdd(count, total);
+    at = __builtin_amdgcn_readfirstlane((int)at) + before;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        if (mine >> i & 1) store(at++, u[i]);
+}
+
+// Of a lane's four, which begin with x's prefix, and which are above all that do.
+__device__ __forceinline__ void sort_out(const Search& x, const f32x4u& w, uint32_t free, uint32_t (&u)[4], uint32_t& mine,
+                                         uint32_t& more) {
+    mine = more = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        u[i] = ordered(w[i]);
+        mine |= (uint32_t)((u[i] & x.known) == x.prefix) << i;
+        more |= (uint32_t)((u[i] & x.known) > x.prefix) << i;
+    }
+    mine &= free;
+    more &= free;
+}
+
+// Of a lane's four, which stay for their weight or place, and which have the last one's
+// weight, when the search has ended (`any`: there was one).
+__device__ __forceinline__ void look(const Search& x, bool any, const f32x4u& w, uint32_t free, uint32_t forced, uint32_t& above,
+                                     uint32_t& equal) {
+    above = equal = 0;
+    if (any) {
+        const float border = number_of(x.prefix);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            // (0 is NaN's place: every number is above it)
+            above |= (uint32_t)(x.prefix ? w[i] > border : w[i] == w[i]) << i;
+            equal |= (uint32_t)(x.prefix ? w[i] == border : w[i] != w[i]) << i;
         }
     }
-    __syncthreads();
-    uint32_t at = 0, same = 0;  // those above and those equal before this place
-    for (int k = 0; k < wave; k++) {
-        at += s_above[k];
-        same += s_equal[k];
-    }
-    for_weights(a, s, head, j0, j1, m0, m1, [&](int j, const f32x4u& w, uint32_t free, uint32_t forced) {
-        uint32_t x, y;
-        look(w, free, forced, x, y);
+    above = (above & free) | forced;
+    equal &= free;
+}
+
+// Writes what of a stretch stays; at, same: those above and those equal before it.
+__device__ __forceinline__ void write_kept(Stretch& st, const Search& x, bool any, uint32_t at, uint32_t same, int32_t* kept) {
+    st.each([&](int j, const f32x4u& w, uint32_t free, uint32_t forced) {
+        uint32_t above, equal;
+        look(x, any, w, free, forced, above, equal);
         uint32_t ax = at;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const uint64_t b = __ballot(x >> i & 1);
+            const uint64_t b = __ballot(above >> i & 1);
             ax += lanes_before(b);
             at += (uint32_t)__popcll(b);
         }
         uint32_t ay = same;
-        if (__any(y != 0)) {
+        if (__any(equal != 0)) {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                const uint64_t b = __ballot(y >> i & 1);
+                const uint64_t b = __ballot(equal >> i & 1);
                 ay += lanes_before(b);
                 same += (uint32_t)__popcll(b);
             }
         }
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const uint32_t xi = x >> i & 1, yi = y >> i & 1;
-            if (xi | (yi & (uint32_t)(ay < need))) kept[ax + min(ay, need)] = j + i;
+            const uint32_t xi = above >> i & 1, yi = equal >> i & 1;
+            if (xi | (yi & (uint32_t)(ay < x.need))) kept[ax + min(ay, x.need)] = j + i;
             ax += xi;
             ay += yi;
         }
     });
+}
+
+// A sequence's head as the kernels see it.
+struct Cutting {
+    int s, head, L, count, m0, m1;  // keys, those that stay; those from m0 to m1 - 1 may go
+    uint32_t need;                  // of them stay
+    int32_t* kept;
+    __device__ __forceinline__ Cutting(const SelectArgs& a, int s_, int head_) : s(s_), head(head_) {
+        const int len = a.c.kv_len[s];
+        L = (unsigned)len > (unsigned)(a.c.max_pages << (a.c.bpp_log2 + 5)) ? 0 : len;
+        count = min(L, a.budget);
+        m0 = a.sinks;
+        m1 = L - a.recent;
+        need = (uint32_t)(a.budget - a.sinks - a.recent);
+        kept = a.kept + ((int64_t)s * a.c.heads + head) * a.budget;
+    }
+    __device__ __forceinline__ bool whole() const { return L == count; }
+};
+
+// A workgroup for a head: as many keys as its registers hold in one reading.
+constexpr int kOneThreads = 1024;
+constexpr int kOneMost = 16 * kOneThreads;
+
+__global__ __launch_bounds__(kOneThreads) void cache_select_kernel(SelectArgs a) {
+    constexpr int kWavesHere = kOneThreads / 64;
+    __shared__ __align__(16) Histogram<kOneThreads, 4> hist;
+    __shared__ uint32_t s_above[kWavesHere], s_equal[kWavesHere];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const Cutting x(a, (int)(blockIdx.x / (unsigned)a.c.heads), (int)(blockIdx.x % (unsigned)a.c.heads));
+    if (x.head == 0 && tid == 0) a.counts[x.s] = x.count;
+    for (int i = x.count + tid; i < a.budget; i += kOneThreads) x.kept[i] = -1;
+    if (x.whole()) {
+        for (int i = tid; i < x.L; i += kOneThreads) x.kept[i] = i;
+        return;
+    }
+    const int per = (x.L + 256 * kWavesHere - 1) / (256 * kWavesHere) * 256;
+    const int j0 = min(wave * per, x.L), j1 = min(j0 + per, x.L);
+    Stretch st(a, x.s, x.head, j0, j1, x.m0, x.m1);
+    Search search{0, 0, x.need};
+    const bool any = x.need > 0;
+    for (int pass = 0; any && pass < 3; pass++) {
+        hist.clear();
+        __syncthreads();
+        st.each([&](int, const f32x4u& w, uint32_t free, uint32_t) {
+            uint32_t u[4], mine, more;
+            sort_out(search, w, free, u, mine, more);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (mine >> i & 1) hist.add(u[i], pass);
+        });
+        __syncthreads();
+        hist.find(search, pass);
+    }
+    uint32_t above = 0, equal = 0;
+    st.each([&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
+        uint32_t p, q;
+        look(search, any, w, free, forced, p, q);
+        above += (uint32_t)__popc(p);
+        equal += (uint32_t)__popc(q);
+    });
+    above = sum64(above);
+    equal = sum64(equal);
+    if (lane == 0) {
+        s_above[wave] = above;
+        s_equal[wave] = equal;
+    }
+    __syncthreads();
+    uint32_t at = 0, same = 0;
+    for (int k = 0; k < wave; k++) {
+        at += s_above[k];
+        same += s_equal[k];
+    }
+    write_kept(st, search, any, at, same, x.kept);
+}
+
+// More keys: a workgroup for every chunk of a head's, in three launches.  The first digit
+// of all (a histogram of each chunk, added up by everyone who needs it); what begins with
+// it put aside, in one list for a head in any order; the rest of the search, by every
+// workgroup for itself over that list, which also says what the chunks before keep.
+constexpr int kManyThreads = 256;
+constexpr int kListMost = 16384;
+constexpr int kListHere = 4096;  // of a workgroup, which takes its room in the head's list at once
+
+// A head's part of the workspace.
+struct Lists {
+    uint16_t* digits;  // [chunks, kDigits]
+    uint2* list;       // [kListMost]: weight (ordered), chunk
+    uint32_t* above;   // [chunks]: those above all that begin so, or kept for their place
+    uint32_t* header;  // entries of the list, the first digit, how many of it stay, how many have it
+    static size_t bytes(int chunks) {
+        return ((size_t)chunks * (kDigits * 2 + 4) + kListMost * 8 + 16 + 15) & ~(size_t)15;
+    }
+    __device__ __forceinline__ Lists(const SelectArgs& a, int64_t item) {
+        uint8_t* p = a.workspace + item * a.item_bytes;
+        header = reinterpret_cast<uint32_t*>(p);
+        list = reinterpret_cast<uint2*>(p + 16);
+        digits = reinterpret_cast<uint16_t*>(p + 16 + kListMost * 8);
+        above = reinterpret_cast<uint32_t*>(p + 16 + kListMost * 8 + (size_t)a.chunks * kDigits * 2);
+    }
+};
+
+// The chunk of a workgroup, and the stretch of one of its four waves.
+struct Chunk {
+    int j0, j1, all;  // all: chunks that the head's keys fill
+    __device__ __forceinline__ Chunk(const SelectArgs& a, const Cutting& x, int chunk) {
+        const int wave = threadIdx.x >> 6, each = a.chunk_keys / (kManyThreads / 64);
+        j0 = __builtin_amdgcn_readfirstlane(min(chunk * a.chunk_keys + wave * each, x.L));
+        j1 = min(j0 + each, x.L);
+        all = (x.L + a.chunk_keys - 1) / a.chunk_keys;
+    }
+};
+
+__global__ __launch_bounds__(kManyThreads) void cache_select_digits_kernel(SelectArgs a) {
+    __shared__ __align__(16) Histogram<kManyThreads, 4> hist;
+    const Placed place(a.c, a.chunks);
+    if (place.s < 0) return;
+    const Cutting x(a, place.s, place.head);
+    const Chunk chunk(a, x, place.chunk);
+    if (x.whole() || x.need == 0 || place.chunk >= chunk.all) return;
+    const Lists lists(a, (int64_t)x.s * a.c.heads + x.head);
+    if (place.chunk == 0 && threadIdx.x == 0) lists.header[0] = 0;
+    hist.clear();
+    __syncthreads();
+    Stretch st(a, x.s, x.head, chunk.j0, chunk.j1, x.m0, x.m1);
+    st.each([&](int, const f32x4u& w, uint32_t free, uint32_t) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (free >> i & 1) hist.add(ordered(w[i]), 0);
+    });
+    __syncthreads();
+    uint4 out;
+    uint32_t n[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) n[i] = hist.total(8 * (int)threadIdx.x + i);
+    out = make_uint4(n[0] | n[1] << 16, n[2] | n[3] << 16, n[4] | n[5] << 16, n[6] | n[7] << 16);
+    reinterpret_cast<uint4*>(lists.digits + (size_t)place.chunk * kDigits)[threadIdx.x] = out;
+}
+
+__global__ __launch_bounds__(kManyThreads) void cache_select_aside_kernel(SelectArgs a) {
+    __shared__ __align__(16) Histogram<kManyThreads, 4> hist;
+    __shared__ uint32_t s_above, s_count, s_first, s_list[kListHere];
+    const Placed place(a.c, a.chunks);
+    if (place.s < 0) return;
+    const Cutting x(a, place.s, place.head);
+    const Chunk chunk(a, x, place.chunk);
+    if (x.whole() || place.chunk >= chunk.all) return;
+    const Lists lists(a, (int64_t)x.s * a.c.heads + x.head);
+    const bool any = x.need > 0;
+    Stretch st(a, x.s, x.head, chunk.j0, chunk.j1, x.m0, x.m1);
+    Search search{0, 0, x.need};
+    if (threadIdx.x == 0) s_above = s_count = 0;
+    if (any) {
+        uint32_t n[8] = {0, 0, 0, 0, 0, 0, 0, 0};  // of digits from the largest down
+        const uint4* from = reinterpret_cast<const uint4*>(lists.digits) + (kDigits / 8 - 1 - threadIdx.x);
+#pragma unroll 8
+        for (int k = 0; k < chunk.all; k++) {
+            const uint4 v = from[(size_t)k * (kDigits / 8)];
+            const uint32_t d[4] = {v.w, v.z, v.y, v.x};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                n[2 * i] += d[i] >> 16;
+                n[2 * i + 1] += d[i] & 0xFFFFu;
+            }
+        }
+        const uint32_t having = hist.find(search, 0, n);
+        if (place.chunk == 0 && threadIdx.x == 0) {
+            lists.header[1] = search.prefix;
+            lists.header[2] = search.need;
+            lists.header[3] = having;
+        }
+    } else {
+        __syncthreads();
+    }
+    uint32_t above = 0;
+    st.each([&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
+        uint32_t u[4], mine = 0, more = 0;
+        if (any) {
+            sort_out(search, w, free, u, mine, more);
+            put_aside(mine, u, &s_count, [&](uint32_t at, uint32_t v) {
+                if (at >= kListHere) at = atomicAdd(lists.header, 1u) + kListHere;
+                if (at < kListHere)
+                    s_list[at] = v;
+                else if (at - kListHere < kListMost)
+                    lists.list[at - kListHere] = make_uint2(v, (uint32_t)place.chunk);
+            });
+        }
+        above += (uint32_t)__popc(more | forced);
+    });
+    above = sum64(above);
+    if ((threadIdx.x & 63) == 0) atomicAdd(&s_above, above);
+    __syncthreads();
+    const uint32_t n = min(s_count, (uint32_t)kListHere);
+    if (threadIdx.x == 0) {
+        lists.above[place.chunk] = s_above;
+        s_first = n ? atomicAdd(lists.header, n) : 0;
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n; i += kManyThreads)
+        if (s_first + i < kListMost) lists.list[s_first + i] = make_uint2(s_list[i], (uint32_t)place.chunk);
+}
+
+__global__ __launch_bounds__(kManyThreads) void cache_select_write_kernel(SelectArgs a) {
+    __shared__ __align__(16) Histogram<kManyThreads, 4> hist;
+    __shared__ uint32_t s_before[2], s_above[kManyThreads / 64], s_equal[kManyThreads / 64];
+    const Placed place(a.c, a.chunks);
+    if (place.s < 0) return;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Cutting x(a, place.s, place.head);
+    const Chunk chunk(a, x, place.chunk);
+    if (x.head == 0 && place.chunk == 0 && tid == 0) a.counts[x.s] = x.count;
+    const int64_t stride = (int64_t)a.chunks * kManyThreads, here = (int64_t)place.chunk * kManyThreads + tid;
+    for (int64_t i = x.count + here; i < a.budget; i += stride) x.kept[i] = -1;
+    if (x.whole()) {
+        for (int64_t i = here; i < x.L; i += stride) x.kept[i] = (int)i;
+        return;
+    }
+    if (place.chunk >= chunk.all) return;
+    const Lists lists(a, (int64_t)x.s * a.c.heads + x.head);
+    const bool any = x.need > 0;
+    Stretch st(a, x.s, x.head, chunk.j0, chunk.j1, x.m0, x.m1);
+    Search search{0, 0, x.need};
+    if (tid < 2) s_before[tid] = 0;
+    uint32_t at = 0, same = 0;
+    if (any) {
+        search = {lists.header[1], Search::mask(0) << Search::shift(0), lists.header[2]};
+        const uint32_t having = lists.header[3];
+        // f of every weight that begins with the prefix and its chunk; a list that is too long: from the weights
+        auto each = [&](const auto& f) {
+            if (having <= kListMost) {
+                for (uint32_t i = tid; i < having; i += kManyThreads) {
+                    const uint2 e = lists.list[i];
+                    f(e.x, (int)e.y);
+                }
+            } else {
+                const int per = (x.L + 4 * 256 - 1) / (4 * 256) * 256;
+                const int j0 = min(wave * per, x.L), j1 = min(j0 + per, x.L);
+                const uint32_t first = search.prefix & (Search::mask(0) << Search::shift(0));
+                Stretch all(a, x.s, x.head, j0, j1, x.m0, x.m1);
+                all.each([&](int j, const f32x4u& w, uint32_t free, uint32_t) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const uint32_t u = ordered(w[i]);
+                        if ((free >> i & 1) && (u & (Search::mask(0) << Search::shift(0))) == first)
+                            f(u, (j + i) / a.chunk_keys);
+                    }
+                });
+            }
+        };
+        for (int pass = 1; pass < 3; pass++) {
+            hist.clear();
+            __syncthreads();
+            each([&](uint32_t u, int) {
+                if ((u & search.known) == search.prefix) hist.add(u, pass);
+            });
+            __syncthreads();
+            hist.find(search, pass);
+        }
+        each([&](uint32_t u, int k) {
+            at += k < place.chunk && u > search.prefix;
+            same += k < place.chunk && u == search.prefix;
+        });
+    }
+    for (int k = tid; k < place.chunk; k += kManyThreads) at += lists.above[k];
+    uint32_t above = 0, equal = 0;
+    st.each([&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
+        uint32_t p, q;
+        look(search, any, w, free, forced, p, q);
+        above += (uint32_t)__popc(p);
+        equal += (uint32_t)__popc(q);
+    });
+    at = sum64(at);
+    same = sum64(same);
+    above = sum64(above);
+    equal = sum64(equal);
+    __syncthreads();
+    if ((tid & 63) == 0) {
+        s_above[wave] = above;
+        s_equal[wave] = equal;
+        atomicAdd(&s_before[0], at);
+        atomicAdd(&s_before[1], same);
+    }
+    __syncthreads();
+    at = s_before[0];
+    same = s_before[1];
+    for (int k = 0; k < wave; k++) {
+        at += s_above[k];
+        same += s_equal[k];
+    }
+    write_kept(st, search, any, at, same, x.kept);
+}
+
+// Keys of a chunk: 4096, or more where a head would have more than 64 of them; no more than
+// 16 bits count.  0: a workgroup for a head (few keys, or items that pass a launch's 2^32
+// threads).
+int chunk_keys(int64_t items, int64_t reach) {
+    if (reach <= kOneMost) return 0;
+    const int64_t n = std::min<int64_t>((reach + 64 * 4096 - 1) / (64 * 4096) * 4096, 61440);
+    return (items + 7) * ((reach + n - 1) / n) < (int64_t)1 << 23 ? (int)n : 0;
 }
 
 // ---------------------------------------------------------------------------
@@ -459,8 +725,27 @@ __global__ __launch_bounds__(kThreads) void cache_compact_kernel(CompactArgs a, 
 
 }  // namespace
 
-hipError_t launch_cache_select(const SelectArgs& a, hipStream_t stream) {
-    cache_select_kernel<<<(unsigned)a.c.seqs * (unsigned)a.c.heads, kSelectThreads, 0, stream>>>(a);
+size_t cache_select_workspace(int64_t items, int64_t reach) {
+    const int keys = chunk_keys(items, reach);
+    return keys ? (size_t)items * Lists::bytes((int)((reach + keys - 1) / keys)) : 0;
+}
+
+hipError_t launch_cache_select(const SelectArgs& args, hipStream_t stream) {
+    SelectArgs a = args;
+    const int64_t reach = ((int64_t)a.c.max_pages << a.c.bpp_log2) * kBlockTokens;
+    a.chunk_keys = chunk_keys((int64_t)a.c.seqs * a.c.heads, reach);
+    if (!a.chunk_keys) {
+        cache_select_kernel<<<(unsigned)a.c.seqs * (unsigned)a.c.heads, kOneThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    a.chunks = (int)((reach + a.chunk_keys - 1) / a.chunk_keys);
+    a.item_bytes = Lists::bytes(a.chunks);
+    const unsigned grid = placed_grid(a.c, a.chunks);
+    cache_select_digits_kernel<<<grid, kManyThreads, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    cache_select_aside_kernel<<<grid, kManyThreads, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    cache_select_write_kernel<<<grid, kManyThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 

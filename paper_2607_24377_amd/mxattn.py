@@ -90,7 +90,9 @@ def lib() -> ctypes.CDLL:
             L.mxattn_cache_attend_weights.restype = I
             L.mxattn_cache_attend_weights_workspace.argtypes = [I64] * 8
             L.mxattn_cache_attend_weights_workspace.restype = SZ
-            L.mxattn_cache_select.argtypes = [P, I64, I64, P, P] + [I64] * 6 + [P, P, P]
+            L.mxattn_cache_select.argtypes = [P, I64, I64, P, P] + [I64] * 6 + [P, P, P, SZ, P]
+            L.mxattn_cache_select_workspace.argtypes = [I64] * 4
+            L.mxattn_cache_select_workspace.restype = SZ
             L.mxattn_cache_select.restype = I
             L.mxattn_cache_compact.argtypes = [P, P, P, P, I64, I64, P, I64, I64, P, I64, I64, I64, P, I64, I64, P, P, P, P]
             L.mxattn_cache_compact.restype = I
@@ -575,11 +577,16 @@ def cache_select(weights: torch.Tensor, page_table, kv_len, budget: int, sinks: 
         raise ValueError("kept must be [seqs, heads, budget]")
     if counts is None:
         counts = torch.empty((seqs,), dtype=i32, device=weights.device)
-    _run((_lib or lib()).mxattn_cache_select, "mxattn_cache_select", dev, stream,
+    L, work, size = _lib or lib(), None, 0
+    if stream is None:  # (as for attention)
+        size = L.mxattn_cache_select_workspace(page, seqs, max_pages, heads)
+        if size:
+            work = torch.empty(size, dtype=torch.uint8, device=weights.device)
+    _run(L.mxattn_cache_select, "mxattn_cache_select", dev, stream,
          (_address(weights, "weights", torch.float32, dev, weights.numel()), pages, page,
           _address(page_table, "page_table", i32, dev, seqs * max_pages), _address(kv_len, "kv_len", i32, dev, seqs), seqs,
           max_pages, heads, budget, sinks, recent, _address(kept, "kept", i32, dev, kept.numel()),
-          _address(counts, "counts", i32, dev, seqs)))
+          _address(counts, "counts", i32, dev, seqs), work.data_ptr() if size else None, size))
     return kept, counts
 
 

@@ -36,7 +36,7 @@ CALLS = [("mxattn_cache_attend_window", WINDOW, c) for c in WINDOW_BAD] + [("mxa
 CALLS += [("mxattn_cache_attend_weights", WEIGHTS, c) for c in WEIGHTS_BAD]
 
 BATCH = dict(pages=10, page=64, table=far(11), lens=far(13), seqs=3, max_pages=4)
-SELECT = dict(w=far(41), **BATCH, H=2, budget=100, sinks=4, recent=50, kept=far(43), counts=far(44), stream=None)
+SELECT = dict(w=far(41), **BATCH, H=2, budget=100, sinks=4, recent=50, kept=far(43), counts=far(44), ws=None, ws_bytes=0, stream=None)
 SELECT_BAD = [(dict([(n, None)]), NULL) for n in ("w", "table", "lens", "kept", "counts")] + [
     (dict(pages=0), SHAPE), (dict(page=48), VALUE), (dict(seqs=0), SHAPE), (dict(max_pages=0), SHAPE), (dict(H=0), SHAPE),
     (dict(seqs=1 << 20, H=4), SHAPE), (dict(budget=0), VALUE), (dict(budget=(1 << 24) + 1), VALUE), (dict(sinks=-1), VALUE),
@@ -54,6 +54,13 @@ COMPACT_BAD = [(dict([(n, None)]), NULL) for n in ("kc", "ks", "vc", "vs", "tabl
     (dict(kc=far(20) + 8), ALIGN), (dict(kept=far(43) + 2), ALIGN), (dict(base=far(46) + 1), ALIGN), (dict(w=far(41) + 2), ALIGN),
     (dict(out=far(45) + 2), ALIGN), (dict(counts=far(44) + 2), ALIGN), (dict(w=far(23)), SHAPE), (dict(w=far(20) - WB + 4), SHAPE),
 ]
+LONG_SELECT = dict(SELECT, page=4096, max_pages=5)
+LONG_SELECT_BAD = [
+    (dict(ws=far(30), ws_bytes=1000), 10), (dict(ws=far(30) + 8, ws_bytes=1 << 30), ALIGN), (dict(ws=far(41), ws_bytes=1 << 30), SHAPE),
+    (dict(ws=far(43) + 2384, ws_bytes=1 << 30), SHAPE), (dict(ws=far(44), ws_bytes=1 << 30), SHAPE),
+    (dict(ws=far(13), ws_bytes=1 << 30), SHAPE), (dict(ws=far(11) + 48, ws_bytes=1 << 30), SHAPE),
+]
+CALLS += [("mxattn_cache_select", LONG_SELECT, c) for c in LONG_SELECT_BAD]
 CALLS += [("mxattn_cache_select", SELECT, c) for c in SELECT_BAD] + [("mxattn_cache_compact", COMPACT, c) for c in COMPACT_BAD]
 
 
@@ -85,6 +92,17 @@ def test_weights_workspace_sizes(L):  # noqa: F811
     assert size(*long) == (plain(*long) + 15) // 16 * 16 + 64 * 32 * 8
     for i, bad in ((0, 48), (1, 0), (2, 0), (3, 0), (4, 7), (5, 0), (6, -1), (7, -1)):
         assert size(*ok[:i], bad, *ok[i + 1:]) == 0, (i, bad)
+
+
+def test_select_workspace_sizes(L):  # noqa: F811
+    size = L.mxattn_cache_select_workspace
+    assert size(64, 3, 256, 2) == 0 and size(4096, 3, 4, 2) == 0  # a workgroup holds the keys
+    assert size(4096, 1 << 18, 4096, 1) == 0  # more chunks than a launch holds
+    one = size(64, 1, 257, 1)
+    assert 0 < one <= 1.2 * 2 ** 20 and one % 16 == 0 and size(64, 3, 257, 2) == 6 * one
+    assert size(4096, 1, 4096, 1) <= 1.3e6
+    for bad in ((48, 1, 257, 1), (64, 0, 257, 1), (64, 1, 0, 1), (64, 1, 257, 0), (64, 1 << 20, 257, 4)):
+        assert size(*bad) == 0
 
 
 def test_binding_refuses_tensors_that_do_not_fit():

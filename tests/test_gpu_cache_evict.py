@@ -40,6 +40,15 @@ SELECTS = [
     ([40000], 2, 256, 5000, 4, 1000, "some"),
     ([40000], 1, 4096, 39000, 0, 0, "ties"),
     ([90 * i % 1000 for i in range(200)], 2, 32, 128, 2, 30, "some"),
+    # a table for more keys than a workgroup holds: several for each head, some of them without keys, whole
+    # stretches that must stay, chunks of more than 4096 keys, more of a digit than the list takes
+    ([17000, 40, 16384, 0, 8193], 3, 64, 3000, 5, 2000, "odd"),
+    ([120000, 4097], 2, 256, 10000, 64, 1000, "some"),
+    ([70000], 1, 32, 50000, 30000, 20000, "some"),
+    ([70000], 1, 32, 50000, 30000, 19999, "some"),
+    ([70000], 2, 64, 30000, 10, 20, "equal"),
+    ([300000], 1, 1024, 100001, 0, 0, "ties"),
+    ([300000], 1, 4096, 2, 0, 1, "odd"),
 ]
 
 

@@ -88,9 +88,9 @@ __global__ __launch_bounds__(kThreads) void cache_weigh_scores_kernel(CacheWeigh
     }
 }
 
-// From K and Q.  A workgroup takes 4 kBlocks blocks of keys, held as operands by its waves,
-// and walks the rows that see some of them, 64 a step: waves w and w + 4 have the same keys
-// and a half of the rows each.  Q comes through LDS, two steps ahead: 16 lanes copy a row,
+// From K and Q.  A workgroup takes 128 keys, held as operands by its waves, and walks the
+// rows that see some of them, 64 a step: waves w and w + 4 have the same block and a half of
+// the rows each.  Q comes through LDS, two steps ahead: 16 lanes copy a row,
 // its 16-byte chunks in an order of its own, so that lanes that read a chunk of all rows
 // read all banks.
 constexpr int kWaves = 8;
@@ -110,6 +110,8 @@ struct Walk {
     const uint8_t* p;
     int row, g;  // (and its head in the group)
 };
+// kWhole: a step is whole tokens (the group divides it).
+template <bool kWhole>
 struct Stride {
     int64_t token, row, step, carry;  // bytes from token to token and head to head, of a step, and where a step passes a token
     int group, g;
@@ -127,8 +129,9 @@ struct Stride {
     }
     __device__ __forceinline__ void advance(Walk& w) const {
         w.row += kStepRows;
-        w.g += g;
         w.p += step;
+        if constexpr (kWhole) return;
+        w.g += g;
         if (w.g >= group) {
             w.g -= group;
             w.p += carry;
@@ -136,12 +139,12 @@ struct Stride {
     }
 };
 
-template <int kBlocks>
-__global__ __launch_bounds__(64 * kWaves, kBlocks == 1 ? 4 : 2) void cache_weigh_rows_kernel(CacheWeighArgs w, int chunks) {
+template <bool kWhole>
+__global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheWeighArgs w, int chunks) {
     __shared__ __align__(16) uint8_t st0[kStageBytes];
     __shared__ __align__(16) uint8_t st1[kStageBytes];
     __shared__ __align__(16) uint8_t st2[kStageBytes];
-    __shared__ float s_sum[kKeyWaves * kBlocks * kBlockTokens];
+    __shared__ float s_sum[kKeyWaves * kBlockTokens];
     const CacheAttendArgs& a = w.a;
     const CacheArgs& c = a.c;
     const Placed place(a.c, chunks);
@@ -151,92 +154,96 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks == 1 ? 4 : 2) void cache_weigh
     if (k.n == 0) return;
     const int past = k.keys - k.n, rows = k.n * a.group;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane & 31, h = lane >> 5;
-    constexpr int kGroupKeys = kKeyWaves * kBlocks * kBlockTokens;
+    constexpr int kGroupKeys = kKeyWaves * kBlockTokens;
     const int last = (k.keys + kBlockTokens - 1) / kBlockTokens - 1;
-    const int mine = (wave & 3) * kBlocks * kBlockTokens, half = wave >> 2;
-    const Stride by_q(a, a.q_stride * 2, kHeadDim * 2), by_stats(a, (int64_t)c.heads * a.group * 8, 8);
+    const int half = wave >> 2;
+    const Stride<kWhole> by_q(a, a.q_stride * 2, kHeadDim * 2), by_stats(a, (int64_t)c.heads * a.group * 8, 8);
     const uint16_t* q0 = a.q + row_offset(a, k.first, 0, head, a.q_stride);
     const float2* stats0 = a.stats + row_number(a, k.first, 0, head);
     const uint8_t* last_q = by_q.at(a, q0, rows - 1).p;
     const uint8_t* last_stats = by_stats.at(a, stats0, rows - 1).p;
     for (int64_t j64 = (int64_t)place.chunk * kGroupKeys; j64 < k.keys; j64 += (int64_t)chunks * kGroupKeys) {
-        const int base = (int)j64 + mine;
-        KExact keys[kBlocks];
-        float sum[kBlocks][16];
-#pragma unroll
-        for (int b = 0; b < kBlocks; b++) {
-            const int i = min(base / kBlockTokens + b, last);
+        const int base = (int)j64 + (wave & 3) * kBlockTokens;
+        KExact keys;
+        float sum[16];
+        {
+            const int i = min(base / kBlockTokens, last);
             const BlockAt p = block_at(c, page_of(c, s, i), head, i);
             const uint8_t* kb = c.kc + p.at * kBlockBytes + 2 * h * 512 + operand_key(q) * 16;
             uint4 codes[4];
 #pragma unroll
             for (int e = 0; e < 4; e++) codes[e] = *reinterpret_cast<const uint4*>(kb + (4 * (e >> 1) + (e & 1)) * 512);
-            keys[b] = exact_keys(codes, c.ks[p.at]);
-#pragma unroll
-            for (int e = 0; e < 16; e++) sum[b][e] = 0.f;
+            keys = exact_keys(codes, c.ks[p.at]);
         }
+#pragma unroll
+        for (int e = 0; e < 16; e++) sum[e] = 0.f;
         // the first rows whose tokens see the group's first key
         const int from = (a.causal ? max(0, (int)j64 - past) * a.group : 0) & ~(kStepRows - 1);
         const int steps = (rows - from + kStepRows - 1) / kStepRows;
-        Walk r0 = by_q.at(a, q0, from + 8 * wave + (lane >> 4)), r1 = by_q.at(a, q0, from + 8 * wave + 4 + (lane >> 4));
+        // (a row's chunks keep their order from step to step, as 16 divides it)
+        const int lane_row = 8 * wave + (lane >> 4), ch0 = 16 * ((lane ^ lane_row) & 15), ch1 = 16 * ((lane ^ lane_row ^ 4) & 15);
+        Walk r0 = by_q.at(a, q0, from + lane_row), r1 = by_q.at(a, q0, from + lane_row + 4);
         Walk rs = by_stats.at(a, stats0, from + 32 * half + q);
-        // the next rows into a stage, 16 lanes a row (behind the last row: that one)
-        auto copy = [&](uint8_t* stage) {
-            const uint8_t* p0 = (r0.row < rows ? r0.p : last_q) + 16 * ((lane ^ r0.row) & 15);
-            const uint8_t* p1 = (r1.row < rows ? r1.p : last_q) + 16 * ((lane ^ r1.row) & 15);
+        r0.p += ch0;
+        r1.p += ch1;
+        // the rows of step `step` into a stage, 16 lanes a row (behind the last row: that one)
+        auto copy = [&](int step, uint8_t* stage) {
+            const uint8_t *p0 = r0.p, *p1 = r1.p;
+            if (from + (step + 1) * kStepRows > rows) {
+                if (r0.row >= rows) p0 = last_q + ch0;
+                if (r1.row >= rows) p1 = last_q + ch1;
+            }
             __builtin_amdgcn_global_load_lds((global_ptr_t)p0, (lds_ptr_t)(stage + 8 * wave * 256), 16, 0, 0);
             __builtin_amdgcn_global_load_lds((global_ptr_t)p1, (lds_ptr_t)(stage + (8 * wave + 4) * 256), 16, 0, 0);
             by_q.advance(r0);
             by_q.advance(r1);
         };
-        auto stats = [&] {
-            const float2 x = *reinterpret_cast<const float2*>(rs.row < rows ? rs.p : last_stats);
+        auto stats = [&](int step) {
+            const uint8_t* p = rs.p;
+            if (from + (step + 1) * kStepRows > rows && rs.row >= rows) p = last_stats;
             by_stats.advance(rs);
-            return x;
+            return *reinterpret_cast<const float2*>(p);
         };
+        int off[8];  // of a lane's operands in a stage
+#pragma unroll
+        for (int i = 0; i < 8; i++) off[i] = (32 * half + q) * 256 + ((8 * (i >> 2) + 4 * h + (i & 3)) ^ (q & 15)) * 16;
         __syncthreads();  // the stages are free
-        copy(st0);
-        if (steps > 1) copy(st1);
-        float2 next = stats();
+        copy(0, st0);
+        if (steps > 1) copy(1, st1);
+        float2 next = stats(0);
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         auto one = [&](int step, const uint8_t* cur, uint8_t* far) {
             const float2 ml = next;
-            if (step + 1 < steps) next = stats();
-            if (step + 2 < steps) copy(far);
+            if (step + 1 < steps) next = stats(step + 1);
+            if (step + 2 < steps) copy(step + 2, far);
             const int row0 = from + step * kStepRows + 32 * half;
             // keys that the first and the last row see
             const int min_end = a.causal ? past + token_of(a, min(row0, rows - 1)) + 1 : k.keys;
             const int max_end = a.causal ? past + token_of(a, min(row0 + 31, rows - 1)) + 1 : k.keys;
             if (row0 < rows && max_end > base) {
-                const uint8_t* stage = cur + (32 * half + q) * 256;
                 uint4 qr[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    qr[i] = *reinterpret_cast<const uint4*>(stage + ((8 * (i >> 2) + 4 * h + (i & 3)) ^ (q & 15)) * 16);
+                for (int i = 0; i < 8; i++) qr[i] = *reinterpret_cast<const uint4*>(cur + off[i]);
+                v16f x = scores(keys, qr);
+                float2 mb = ml;
+                if (row0 + 32 > rows || base + kBlockTokens > min_end) {
+                    const int end = row0 + q >= rows ? 0 : a.causal ? past + token_of(a, row0 + q) + 1 : k.keys;
+                    const int seen = end - base - 16 * h;
 #pragma unroll
-                for (int b = 0; b < kBlocks; b++) {
-                    const int at = base + b * kBlockTokens;
-                    v16f x = scores(keys[b], qr);
-                    float2 mb = ml;
-                    if (row0 + 32 > rows || at + kBlockTokens > min_end) {
-                        const int end = row0 + q >= rows ? 0 : a.causal ? past + token_of(a, row0 + q) + 1 : k.keys;
-                        const int seen = end - at - 16 * h;
+                    for (int e = 0; e < 16; e++) x[e] = e < seen ? x[e] : -__builtin_inff();
+                    if (__any(ml.y != ml.y)) {  // a masked key's p is 0, and 0 * NaN would reach it
+                        if (ml.y != ml.y) {
 #pragma unroll
-                        for (int e = 0; e < 16; e++) x[e] = e < seen ? x[e] : -__builtin_inff();
-                        if (__any(ml.y != ml.y)) {  // a masked key's p is 0, and 0 * NaN would reach it
-                            if (ml.y != ml.y) {
-#pragma unroll
-                                for (int e = 0; e < 16; e++) sum[b][e] = e < seen ? __builtin_nanf("") : sum[b][e];
-                                mb = make_float2(0.f, 0.f);
-                            }
+                            for (int e = 0; e < 16; e++) sum[e] = e < seen ? __builtin_nanf("") : sum[e];
+                            mb = make_float2(0.f, 0.f);
                         }
                     }
+                }
 #pragma unroll
-                    for (int e = 0; e < 16; e++) {
-                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.scale, -mb.x));
-                        sum[b][e] = __builtin_fmaf(p, mb.y, sum[b][e]);
-                    }
+                for (int e = 0; e < 16; e++) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.scale, -mb.x));
+                    sum[e] = __builtin_fmaf(p, mb.y, sum[e]);
                 }
             }
             // the next step's rows landed: what this step copies may still be on its way
@@ -255,27 +262,20 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks == 1 ? 4 : 2) void cache_weigh
             if (step + 2 < steps) one(step + 2, st2, st1);
         }
         // the sums of the 32 rows' lanes; lane e of each half gets that of key 16 h + e
-        float total[kBlocks];
+        float total = 0.f;
 #pragma unroll
-        for (int b = 0; b < kBlocks; b++) {
-            total[b] = 0.f;
+        for (int e = 0; e < 16; e++) {
+            float x = sum[e];
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                float x = sum[b][e];
-#pragma unroll
-                for (int d = 1; d < 32; d *= 2) x += __shfl_xor(x, d);
-                total[b] = q == e ? x : total[b];
-            }
-            if (half && q < 16) s_sum[mine + b * kBlockTokens + 16 * h + q] = total[b];
+            for (int d = 1; d < 32; d *= 2) x += __shfl_xor(x, d);
+            total = q == e ? x : total;
         }
+        const int mine = (wave & 3) * kBlockTokens + 16 * h + q, j = base + 16 * h + q;
+        if (half && q < 16) s_sum[mine] = total;
         __syncthreads();
-#pragma unroll
-        for (int b = 0; b < kBlocks; b++) {
-            const int j = base + b * kBlockTokens + 16 * h + q;
-            if (half || q >= 16 || j >= k.keys) continue;
-            const int64_t at = weights_at(c, s, head, j);
-            if (at >= 0) w.after[at] = sum_with(w, at, j < past, total[b] + s_sum[mine + b * kBlockTokens + 16 * h + q]);
-        }
+        if (half || q >= 16 || j >= k.keys) continue;
+        const int64_t at = weights_at(c, s, head, j);
+        if (at >= 0) w.after[at] = sum_with(w, at, j < past, total + s_sum[mine]);
     }
 }
 
@@ -315,9 +315,11 @@ hipError_t launch_cache_weigh(CacheWeighArgs w, int64_t max_q, int64_t max_kv, h
         const int chunks = chunks_of(a, max_kv, 4 * kThreads);
         cache_weigh_scores_kernel<<<placed_grid(a.c, chunks), kThreads, 0, stream>>>(w, chunks);
     } else {
-        constexpr int kBlocks = 1;
-        const int chunks = chunks_of(a, max_kv, kKeyWaves * kBlocks * kBlockTokens);
-        cache_weigh_rows_kernel<kBlocks><<<placed_grid(a.c, chunks), 64 * kWaves, 0, stream>>>(w, chunks);
+        const int chunks = chunks_of(a, max_kv, kKeyWaves * kBlockTokens);
+        if (kStepRows % a.group == 0)
+            cache_weigh_rows_kernel<true><<<placed_grid(a.c, chunks), 64 * kWaves, 0, stream>>>(w, chunks);
+        else
+            cache_weigh_rows_kernel<false><<<placed_grid(a.c, chunks), 64 * kWaves, 0, stream>>>(w, chunks);
     }
     return hipGetLastError();
 }

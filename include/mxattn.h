@@ -497,8 +497,9 @@ size_t mxattn_cache_select_workspace(int64_t page_tokens, int64_t seqs, int64_t 
  *   base       device int32 [seqs], or NULL: 0
  *   out_table  device int32 [seqs, out_pages]: where the tokens go, on pages that hold
  *              none of the call's sources; nothing is written to a page that does not
- *              exist.  NULL or page_table: in place, where kept ascends and kept[i] >= base + i
- *              (anything else gives undefined contents there; nothing out of range).
+ *              exist.  NULL or page_table (then of as many pages, MXATTN_ERR_SHAPE): in
+ *              place, where kept ascends and kept[i] >= base + i (anything else gives
+ *              undefined contents there; nothing out of range).
  *   weights    device fp32 [pages, Hkv, page_tokens], or NULL
  * In place a head's blocks are moved one turn after another; to other pages all at once.
  * Sequences of a call must not share pages that are written.  seqs * Hkv < 2^22. */

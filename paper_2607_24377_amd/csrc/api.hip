@@ -1007,6 +1007,7 @@ int mxattn_cache_compact(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, 
     if (int st = check_pages(a.c, pages, page_tokens, page_table, seqs, max_pages, 1, Hkv)) return st;
     if (int st = check_items(seqs, Hkv)) return st;
     if (out_table && (out_pages < 1 || out_pages > mxattn::kMaxKeys / page_tokens)) return MXATTN_ERR_SHAPE;
+    if (out_table == page_table && out_pages != max_pages) return MXATTN_ERR_SHAPE;
     if ((kept_heads != 1 && kept_heads != Hkv) || width < 1 || width > mxattn::kMaxKeys) return MXATTN_ERR_SHAPE;
     if (int st = check_codes(a.c, k_codes, k_scales, v_codes, v_scales)) return st;
     if (!aligned(out_table, 4) || !aligned(kept, 4) || !aligned(counts, 4) || !aligned(base, 4) || !aligned(weights, 4))

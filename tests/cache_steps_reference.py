@@ -42,13 +42,15 @@ def tree(mask):
 
 
 def attend(cache, q, table, q_start, kv_len, sees):
-    """[tokens, Hq, d] fp64, a bound on the error of the kernel's result, and {(s, head): (weights [L], bound)}.
+    """[tokens, Hq, d] fp64, a bound on the error of the kernel's result, and {(s, head): (weights [L], bound, bound
+    where l is a sum of the scores that become weights too)}.
 
     The bound of the output is that of cache_reference.attend.  A weight is the sum over rows of p = 2^(s c - m) / l:
     each p is off by its score's error and exp2's (rel below), by l's (at most the largest error of the row's p, whose
     scores may be of the FP8 matrix cores: 2^-15 of sum |q k|, and 2^-18 from the chain of its additions) and by one
     more rounding each of 1 / l and of the product (2^-23); the fp32 sum of up to 2^14 positive terms, 32 at a time in
-    parallel, adds at most 2^-15 of itself in a chain of 2^9 additions."""
+    parallel, adds at most 2^-15 of itself in a chain of 2^9 additions.  Where up to 32 rows' scores are kept, l is
+    their sum, and a weight that of at most 2^6 terms."""
     out, tol = torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64)
     weights = {}
     Hq, Hkv = q.shape[1], cache.k.shape[1]
@@ -58,7 +60,7 @@ def attend(cache, q, table, q_start, kv_len, sees):
         for h in range(Hkv if n else 0):
             k, v = cache.rows(table[s], L, h)
             hidden = ~sees(n, L, tokens)
-            total, bound = torch.zeros(L, dtype=torch.float64), torch.zeros(L, dtype=torch.float64)
+            total, bound, near = (torch.zeros(L, dtype=torch.float64) for _ in range(3))
             for g in range(Hq // Hkv):
                 i = h * (Hq // Hkv) + g
                 x = q[tokens, i].double()
@@ -82,7 +84,8 @@ def attend(cache, q, table, q_start, kv_len, sees):
                 tol[tokens, i] = 2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -17 + 2 * drift) * (p @ vv.abs())
                 total += p.sum(0)
                 bound += (p * (rel + sums + 2.0 ** -18 + 2.0 ** -22)).sum(0)
-            weights[s, h] = total, bound + 2.0 ** -15 * total
+                near += (p * (rel + drift + 2.0 ** -18 + 2.0 ** -22)).sum(0)
+            weights[s, h] = total, bound + 2.0 ** -15 * total, near + 2.0 ** -18 * total
     return out, tol, weights
 
 

@@ -52,7 +52,7 @@ COMPACT_BAD = [(dict([(n, None)]), NULL) for n in ("kc", "ks", "vc", "vs", "tabl
     (dict(seqs=1 << 20, H=4), SHAPE), (dict(d=64), UNSUPPORTED), (dict(out_pages=0), SHAPE), (dict(out_pages=1 << 20), SHAPE),
     (dict(kept_heads=3), SHAPE), (dict(kept_heads=0), SHAPE), (dict(width=0), SHAPE), (dict(width=(1 << 24) + 1), SHAPE),
     (dict(kc=far(20) + 8), ALIGN), (dict(kept=far(43) + 2), ALIGN), (dict(base=far(46) + 1), ALIGN), (dict(w=far(41) + 2), ALIGN),
-    (dict(out=far(45) + 2), ALIGN), (dict(counts=far(44) + 2), ALIGN), (dict(w=far(23)), SHAPE), (dict(w=far(20) - WB + 4), SHAPE),
+    (dict(out=far(45) + 2), ALIGN), (dict(out=far(11), out_pages=3), SHAPE), (dict(counts=far(44) + 2), ALIGN), (dict(w=far(23)), SHAPE), (dict(w=far(20) - WB + 4), SHAPE),
 ]
 LONG_SELECT = dict(SELECT, page=4096, max_pages=5)
 LONG_SELECT_BAD = [

@@ -183,6 +183,31 @@ def test_in_place_with_any_contents_stays_inside(mx):  # noqa: F811
         assert torch.equal(a[free], b[free])
 
 
+def test_starts_and_lengths_that_belong_to_no_batch_stay_inside(mx):  # noqa: F811
+    """q_start that does not ascend, lengths, counts and bases of any value: some answer, nothing out of range."""
+    H, page, S = 2, 32, 4
+    table = torch.arange(8, dtype=torch.int32).view(S, 2).cuda()
+    cache = filled(mx, 10, H, page, 7)
+    before = [c.clone() for c in cache]
+    q = rows(50, 4, 1)
+    tree = torch.full((50, 1), -1, dtype=torch.int32, device="cuda")
+    w = torch.ones((10, H, page), device="cuda")
+    for st in ([0, 90, 50, 20, 50], [-7, -3, 1 << 30, 0, 5], [50, 20, 0, 0, 0], [5, 5, 5, 5, 5]):
+        for L in ([64, 64, 64, 64], [-1, 1 << 30, 65, 0], [3, 64, 1, 33]):
+            batch_ = (q, *cache, table, ints(st), ints(L))
+            for b in ((0, 0), (1, 64), (1, 5000), (50, 5000)):
+                mx.cache_attend_window(*batch_, 20, 3, True, *b)
+                mx.cache_attend_window(*batch_, 20, 3, False, *b)
+                mx.cache_attend_tree(*batch_, tree, *b)
+                mx.cache_attend_weights(*batch_, w, True, *b)
+            kept, counts = mx.cache_select(w, table, ints(L), 30, 2, 5)
+            mx.cache_compact(*cache, table, kept, ints(L), ints(st[:4]), weights=w)
+            torch.cuda.synchronize()
+    for c, b in zip(cache, before):  # pages of no sequence
+        assert torch.equal(c[8:], b[8:])
+    assert bool((w[8:] == 1).all())
+
+
 def test_eviction_in_a_graph(mx):  # noqa: F811
     """Selection and compaction captured together and replayed with other weights."""
     lens, H, page, budget = [700, 90, 1200], 2, 64, 256

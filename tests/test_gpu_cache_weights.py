@@ -31,10 +31,11 @@ WEIGHTS = [
 ]
 
 
-def check(w, want, before, table, start, lens, tol_of=None):
-    """Weights w of every sequence with tokens against the sums `want` and what was there before."""
+def check(w, want, before, table, start, lens, near=False):
+    """Weights w of every sequence with tokens against the sums `want` and what was there before; near: few rows."""
     used = torch.zeros(w.shape, dtype=torch.bool)
-    for (s, h), (total, bound) in want.items():
+    for (s, h), (total, *bounds) in want.items():
+        bound = bounds[near]
         L, n = lens[s], start[s + 1] - start[s]
         old = steps.weights_of(before, table[s], L, h).double() if before is not None else torch.zeros(L, dtype=torch.float64)
         old[max(L - n, 0):] = 0
@@ -64,11 +65,12 @@ def test_weights_against_64_bits(mx, case):  # noqa: F811
     for bounds in ((0, 0), (max(new), max(lens)), (1, max(lens)), (33, max(lens)), (1, 6000), (129, 30000)):
         if bounds[1] and bounds[1] < max(lens):
             continue
+        near = bounds[1] > 0 and min(bounds[0], start[-1] + 2) * Hq // Hkv <= 32 and max(new) * Hq // Hkv <= 64
         o, w = mx.cache_attend_weights(*args, before.cuda(), causal, *bounds,
                                        weights_out=torch.full_like(before, -7.0, device="cuda"))
         err = (o.cpu().double() - want)[:n].abs()
         assert bool((err <= tol[:n] + 1e-30).all())
-        used = check(w.cpu(), sums, before, table, start, lens)
+        used = check(w.cpu(), sums, before, table, start, lens, near)
         assert bool((w.cpu()[~used] == -7).all())  # nothing else is written
     # in place and from nothing
     o, w = mx.cache_attend_weights(*args, None, causal)
@@ -94,6 +96,35 @@ def test_every_row_gives_one_and_repeats(mx):  # noqa: F811
                 assert abs(total - 4 * n) <= float(sums[s, h][1].sum())
         o2, w2 = mx.cache_attend_weights(*args, None, True, *bounds)
         assert torch.equal(w, w2) and torch.equal(o, o2)
+
+
+def test_scores_too_many_to_keep(mx):  # noqa: F811
+    """More than 1 GiB of scores are not kept but computed again: the same weights, of one long table and of many short
+    sequences."""
+    table, start, lens, pages = batch([1], [900], 4096)
+    cache = filled(mx, pages, 2, 4096, 7)
+    q = rows(1, 64, 5)
+    wide = torch.cat((table, torch.full((1, 4094), 1 << 30, dtype=torch.int32)), 1).cuda()
+    sums = steps.attend(ref.Cache(*cache), q.cpu(), table, start, lens, steps.causal)[2]
+    for max_kv in (901, 0):  # 0: up to 2^24 keys, 4 GiB of scores
+        w = mx.cache_attend_weights(q, *cache, wide, ints(start), ints(lens), None, True, 1, max_kv)[1]
+        check(w.cpu(), sums, None, table, start, lens)
+    S = 20000
+    t = torch.arange(S, dtype=torch.int32).view(S, 1)
+    cache = filled(mx, S, 1, 32, 3)
+    lens = [1 + 7 * i % 32 for i in range(S)]
+    q = rows(S, 16, 6)
+    args = (q, *cache, t.cuda(), ints(list(range(S + 1))), ints(lens))
+    (a, v), (b, w) = (mx.cache_attend_weights(*args, None, True, 1, m) for m in (32, 0))
+    t32 = torch.cat((t, torch.full((S, 31), -1, dtype=torch.int32)), 1).cuda()
+    c, x = mx.cache_attend_weights(q, *cache, t32, *args[-2:], None, True, 1, 1024)
+    assert torch.equal(v, w)  # (a table of 32 keys)
+    # the same scores, but l of the FP8 ones: 2^-15 of sum |q k| and two roundings in 2^-20
+    k = ref.Cache(*cache)
+    size = float(q.float().norm(dim=-1).max()) * float((k.k * torch.exp2(k.ke.double())[..., None, None].amax()).norm(dim=-1).max())
+    rel = 2.0 ** -15 * size / math.sqrt(ref.D) + 2.0 ** -18
+    assert bool(((x - w).abs() <= rel * w).all()) and bool((x != 0).any())
+    assert bool(((c.float() - b.float()).abs() <= 2.0 ** -6 * 448).all())
 
 
 @pytest.mark.parametrize("bounds", [(1, 6000), (40, 6000), (1, 300)])

@@ -164,19 +164,6 @@ __global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheW
     const uint8_t* last_stats = by_stats.at(a, stats0, rows - 1).p;
     for (int64_t j64 = (int64_t)place.chunk * kGroupKeys; j64 < k.keys; j64 += (int64_t)chunks * kGroupKeys) {
         const int base = (int)j64 + (wave & 3) * kBlockTokens;
-        KExact keys;
-        float sum[16];
-        {
-            const int i = min(base / kBlockTokens, last);
-            const BlockAt p = block_at(c, page_of(c, s, i), head, i);
-            const uint8_t* kb = c.kc + p.at * kBlockBytes + 2 * h * 512 + operand_key(q) * 16;
-            uint4 codes[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++) codes[e] = *reinterpret_cast<const uint4*>(kb + (4 * (e >> 1) + (e & 1)) * 512);
-            keys = exact_keys(codes, c.ks[p.at]);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; e++) sum[e] = 0.f;
         // the first rows whose tokens see the group's first key
         const int from = (a.causal ? max(0, (int)j64 - past) * a.group : 0) & ~(kStepRows - 1);
         const int steps = (rows - from + kStepRows - 1) / kStepRows;
@@ -211,6 +198,19 @@ __global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheW
         copy(0, st0);
         if (steps > 1) copy(1, st1);
         float2 next = stats(0);
+        KExact keys;
+        float sum[16];
+        {
+            const int i = min(base / kBlockTokens, last);
+            const BlockAt p = block_at(c, page_of(c, s, i), head, i);
+            const uint8_t* kb = c.kc + p.at * kBlockBytes + 2 * h * 512 + operand_key(q) * 16;
+            uint4 codes[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) codes[e] = *reinterpret_cast<const uint4*>(kb + (4 * (e >> 1) + (e & 1)) * 512);
+            keys = exact_keys(codes, c.ks[p.at]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e++) sum[e] = 0.f;
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         auto one = [&](int step, const uint8_t* cur, uint8_t* far) {
@@ -261,19 +261,22 @@ __global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheW
             if (step + 1 < steps) one(step + 1, st1, st0);
             if (step + 2 < steps) one(step + 2, st2, st1);
         }
-        // the sums of the 32 rows' lanes; lane e of each half gets that of key 16 h + e
-        float total = 0.f;
+        // the sums of the 32 rows' lanes: each exchange leaves a lane half of its keys, in the
+        // end key 16 h + q / 2
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-            float x = sum[e];
+        for (int n = 8; n > 0; n /= 2) {
+            const bool up = q & (2 * n);
 #pragma unroll
-            for (int d = 1; d < 32; d *= 2) x += __shfl_xor(x, d);
-            total = q == e ? x : total;
+            for (int e = 0; e < n; e++) {
+                const float away = up ? sum[e] : sum[e + n], mine = up ? sum[e + n] : sum[e];
+                sum[e] = mine + __shfl_xor(away, 2 * n);
+            }
         }
-        const int mine = (wave & 3) * kBlockTokens + 16 * h + q, j = base + 16 * h + q;
-        if (half && q < 16) s_sum[mine] = total;
+        float total = sum[0] + __shfl_xor(sum[0], 1);
+        const int mine = (wave & 3) * kBlockTokens + 16 * h + (q >> 1), j = base + 16 * h + (q >> 1);
+        if (half) s_sum[mine] = total;
         __syncthreads();
-        if (half || q >= 16 || j >= k.keys) continue;
+        if (half || (q & 1) || j >= k.keys) continue;
         const int64_t at = weights_at(c, s, head, j);
         if (at >= 0) w.after[at] = sum_with(w, at, j < past, total + s_sum[mine]);
     }

@@ -1,6 +1,7 @@
 // cache.h -- argument structures and launchers of the operators around the
 // 8-bit paged cache: per-head norm and rotation (rope.hip), appending
-// (cache_append.hip) and attention over it (cache_attend.hip).
+// (cache_append.hip), attention over it (cache_attend.hip), the weights of its keys
+// (cache_weigh.hip), and cutting and moving what it holds (cache_evict.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -181,7 +182,7 @@ __device__ __forceinline__ int owner_of(const CacheArgs& c, int64_t w, int64_t g
 // to the 8 XCDs in turn and there to its shader engines in turn, so an item's chunks follow
 // one another on one XCD, whose L2 holds what they share, and spread over all its engines.
 // (In the order of sequences, one of four that was the longest lay on two XCDs, or on an
-// engine of each: the weights of 4 prompts took 400 and 272 us for what takes 130.)
+// engine of each: the sums of 4 prompts' weights took 358 and 272 us, and 169 so.)
 struct Placed {
     int s, head, chunk;  // s < 0: none
     __device__ __forceinline__ Placed(const CacheArgs& c, int chunks) {

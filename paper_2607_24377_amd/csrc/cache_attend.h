@@ -1,5 +1,6 @@
-// cache_attend.h -- the arithmetic of attention over the 8-bit paged cache, and
-// how its work is divided over workgroups (device code of cache_attend.hip).
+// cache_attend.h -- the arithmetic of attention over the 8-bit paged cache, what its
+// rows see, and how its work is divided over workgroups (device code of
+// cache_attend.hip, cache_attend_tiles.hip and cache_weigh.hip).
 // A row is one query token and head.  A wave holds 32 rows of a sequence that
 // share a KV head and walks cached blocks of 32 keys:
 //
@@ -329,24 +330,32 @@ struct State {
 // Bytes of v that are NaN codes, as 0x80 in each.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t v) { return ((v & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
-// The keys of a block that the lane's row sees: its first ones, or those of a mask.
+// The lane's 16 keys of a block that its row sees: its first ones, or those of a mask.
 struct Below {
     int n;
-    __device__ __forceinline__ bool operator()(int key) const { return key < n; }
+    __device__ __forceinline__ bool any() const { return n > 0; }
+    __device__ __forceinline__ bool operator()(int i) const { return i < n; }
+    // x of a key that the row sees, else -inf.
+    __device__ __forceinline__ float masked(float x, int i) const { return i < n ? x : -__builtin_inff(); }
 };
 struct Bits {
     uint32_t b;
-    __device__ __forceinline__ bool operator()(int key) const { return (b >> key) & 1u; }
+    __device__ __forceinline__ bool any() const { return b != 0; }
+    __device__ __forceinline__ bool operator()(int i) const { return (b >> i) & 1u; }
+    __device__ __forceinline__ float masked(float x, int i) const {  // (a bit field and a bit select)
+        const uint32_t m = (uint32_t)((int32_t)(b << (31 - i)) >> 31);
+        return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & m) | (0xFF800000u & ~m));
+    }
 };
 
 // A block that only some rows see and that holds NaN codes of V: a masked key
 // has p = 0, and 0 * NaN would reach every row.  The codes are taken out, and
 // the rows that see one get NaN: its count, from a product of ones.
 template <class Mask>
-__device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], const Mask& sees, int h) {
+__device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], const Mask& sees) {
     f16x8 seen[2];
 #pragma unroll
-    for (int i = 0; i < 16; i++) seen[i >> 3][i & 7] = sees(16 * h + i) ? (_Float16)1.f : (_Float16)0.f;
+    for (int i = 0; i < 16; i++) seen[i >> 3][i & 7] = sees(i) ? (_Float16)1.f : (_Float16)0.f;
 #pragma unroll
     for (int n = 0; n < 4; n++) {
         uint32_t* x = reinterpret_cast<uint32_t*>(&v[n]);
@@ -370,8 +379,10 @@ __device__ __forceinline__ void spread_nan(State& st, uint4 (&v)[4], const Mask&
 __device__ __forceinline__ bool has_nan(const uint4 (&v)[4]) {
     uint32_t m = 0;
 #pragma unroll
-    for (int n = 0; n < 4; n++) m |= nan_bytes(v[n].x) | nan_bytes(v[n].y) | nan_bytes(v[n].z) | nan_bytes(v[n].w);
-    return m != 0;
+    for (int n = 0; n < 4; n++)
+        m |= ((v[n].x & 0x7F7F7F7Fu) + 0x01010101u) | ((v[n].y & 0x7F7F7F7Fu) + 0x01010101u) |
+             ((v[n].z & 0x7F7F7F7Fu) + 0x01010101u) | ((v[n].w & 0x7F7F7F7Fu) + 0x01010101u);
+    return (m & 0x80808080u) != 0;
 }
 
 // V's codes and scale byte of a block whose keys not every row sees, or of no page; the
@@ -380,27 +391,29 @@ template <class Mask>
 __device__ __forceinline__ void clean_values(State& st, uint4 (&v)[4], int& e, const Mask& sees, int held, bool lost, int h) {
     const bool none = !lost && e == 255;  // a scale that is no number: nor is any value
     if (lost || none) e = 127;            // (a zero code times that scale is NaN too)
+    if (lost || held < kBlockTokens || __builtin_amdgcn_readfirstlane(none)) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
+        for (int i = 0; i < 4; i++) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            if (none) w[j] = 0x7F7F7F7Fu;
-            // what lies behind the last key may be anything: zero
-            const int left = lost ? 0 : held - 16 * h - 4 * j;
-            w[j] &= left <= 0 ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1;
+            for (int j = 0; j < 4; j++) {
+                if (none) w[j] = 0x7F7F7F7Fu;
+                // what lies behind the last key may be anything: zero
+                const int left = lost ? 0 : held - 16 * h - 4 * j;
+                w[j] &= left <= 0 ? 0u : left >= 4 ? ~0u : (1u << (8 * left)) - 1;
+            }
         }
     }
-    if (__any(has_nan(v))) spread_nan(st, v, sees, h);
+    if (__any(has_nan(v))) spread_nan(st, v, sees);
 }
 
 // Softmax of a block's scores and their product with V of scale byte `e`; `sees`: the
 // keys of the block that the lane's row sees, `any`: some row does not see all.
 template <class Mask>
-__device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], int e, float c, const Mask& sees, bool any, int h) {
+__device__ __forceinline__ void consume(State& st, v16f s, uint4 (&v)[4], int e, float c, const Mask& sees, bool any) {
     if (any) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) s[i] = sees(16 * h + i) ? s[i] : -__builtin_inff();
+        for (int i = 0; i < 16; i++) s[i] = sees.masked(s[i], i);
     }
     float mx = max2(max2(s[0], s[1]), s[2]);
 #pragma unroll
@@ -494,12 +507,12 @@ struct Sight {
         return held;
     }
     static __device__ __forceinline__ uint32_t ones(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
-    // The mask of the block at `base`.
-    __device__ __forceinline__ auto mask_of(int base, bool any) const {
+    // The mask of lane half h's keys of the block at `base`.
+    __device__ __forceinline__ auto mask_of(int base, bool any, int h) const {
         if constexpr (kKind == kWindow || kKind == kTree)
-            return Bits{any ? bits(base) : ~0u};
+            return Bits{any ? (bits(base) >> (16 * h)) & 0xFFFFu : 0xFFFFu};
         else
-            return Below{end - base};
+            return Below{end - base - 16 * h};
     }
 };
 
@@ -511,13 +524,9 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const Q& q, in
                                              float* scores_at, int h, const Prefetch& prefetch) {
     if constexpr (kKind != kWeigh) prefetch();
     const bool any = sight.partial(base);
-    const auto sees = sight.mask_of(base, any);
+    const auto sees = sight.mask_of(base, any, h);
     if (any || x.lost) clean_values(st, x.v, x.ve, sees, sight.keys - base, x.lost, h);
-    if constexpr (kKind == kWindow || kKind == kTree) {
-        if (x.lost && sees.b) st.l = __builtin_nanf("");
-    } else {
-        if (x.lost && sight.end > base) st.l = __builtin_nanf("");  // no such page: NaN for the rows that would see it
-    }
+    if (x.lost && sees.any()) st.l = __builtin_nanf("");  // no such page: NaN for the rows that would see it
     const v16f s = scores(x.k, x.ke, q);
     if constexpr (kKind == kWeigh) {
         if (scores_at) {
@@ -528,7 +537,7 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const Q& q, in
         }
         prefetch();
     }
-    consume(st, s, x.v, x.ve, q.c, sees, any, h);
+    consume(st, s, x.v, x.ve, q.c, sees, any);
 }
 
 // ---------------------------------------------------------------------------

@@ -12,7 +12,11 @@
 // 5 for the join, 5.0 TB/s; one over 118801 keys, 24 heads: 730 MB, 134 and 6, 5.4 TB/s
 // (reading alone reaches 6.4 TB/s on this card); 16 x 4 tokens over 6000 keys, 40 heads
 // on 8: 113 MB, 28 and 7; one over 512 keys, 2 heads: 8.0, a chain of loads (lengths,
-// pages, codes).
+// pages, codes).  With a window of 4096 keys and 4 sinks: 64 tokens far behind it 538 MB,
+// 100 and 5, 5.4 TB/s; a row of 2 heads over 132 keys 6.6.  With scores kept for weights:
+// 64 over 8200 keys 142 and 6, of which the 38 MB of scores are 22 (kept in one place
+// instead they cost nothing; as whole 64-byte pieces, past the caches, or by strides of
+// other channels the same).
 #include "cache_attend.h"
 
 #include <algorithm>

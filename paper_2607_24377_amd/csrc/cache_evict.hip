@@ -4,7 +4,9 @@
 // and, of those between, the heaviest, `budget` in all.  The weight of the last one that
 // stays is found digit by digit (11, 11 and 10 bits of the number in an order of unsigned
 // integers, histograms in LDS); then the kept positions are written in order, each wave
-// from where the stretches before its own end.
+// from where the stretches before its own end.  16 sequences of up to 4500 keys, 8 heads:
+// 12.4 us, a chain of loads and barriers; one of 118800: 5, 10 and 14 us (by one workgroup
+// for a head 88, with one key a lane and load 254).
 //
 // Compaction: position base + i becomes what was at kept[i].  A block of 32 kept tokens
 // takes the largest scale byte of the blocks that they come from, so that no code grows
@@ -12,6 +14,11 @@
 // which is exact unless it falls below 2^-6.  A wave per block of K or V; in place, the
 // workgroup that has a head's keys (or values) walks its blocks in order, all loads of a
 // turn before its stores: what later blocks need lies behind what was written.
+//
+// Bound by HBM, and by the layout: V's 32 tokens of a channel are a sector, so that a kept
+// token brings its whole block.  118800 keys cut to 14850 at random, 8 heads: 213 MB
+// fetched (15 MB kept of each of K and V) and 31 written, 39 us, 6.1 TB/s; 16 sequences of up to
+// 4500 cut to 2048: 29 us.
 #include "heads.h"
 
 #include <algorithm>

@@ -9,7 +9,14 @@
 // bytes of a key's codes, and a second pass over them sums.  Many rows: the scores are
 // computed once more, keys outside, rows inside, so that every sum stays in a wave's
 // registers and no order of additions depends on the schedule.  Either way the scores that
-// become weights are fp32 sums of exact products (QExact).
+// become weights are fp32 sums of exact products (QExact): a weight is then off by 1e-7 of
+// itself, by those of the FP8 matrix cores by 1e-5.
+//
+// Bound by what attention leaves and by the exponentials: 64 tokens over 8200 keys, 32 heads
+// on 8, 57 MB, 15 us; 4 prompts of up to 2048 tokens 135 to 139 us, beside 250 to 270 for their
+// attention (86 vector instructions for 32 x 32 scores, 16 of them exponentials; vector issue
+// busy 44 %, matrix cores 28 %; the longest prompt's 128 steps follow one another); 1560 rows
+// x 32760 keys x 40 heads 730.
 #include "cache_attend.h"
 
 #include <algorithm>

@@ -452,7 +452,8 @@ int mxattn_cache_attend_tree(const void* q, int64_t q_stride, const uint8_t* k_c
  * (which one's weights are stored there is undefined).
  *   workspace    mxattn_cache_attend_weights_workspace() bytes: mxattn_cache_attend's, 8 for
  *                each token and head, and with few tokens the scores, 4 for each token,
- *                head and key of max_kv, at most 1 GiB. */
+ *                head and key of max_kv, at most 1 GiB (with many over few keys, up to
+ *                256 KiB for partial sums). */
 int mxattn_cache_attend_weights(const void* q, int64_t q_stride, const uint8_t* k_codes, const uint8_t* k_scales,
                                 const uint8_t* v_codes, const uint8_t* v_scales, int64_t pages,
                                 int64_t page_tokens, const int32_t* page_table, const int32_t* q_start,

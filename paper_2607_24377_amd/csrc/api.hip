@@ -752,9 +752,9 @@ size_t mxattn_cache_attend_workspace(int64_t page_tokens, int64_t seqs, int64_t 
 
 size_t mxattn_cache_attend_weights_workspace(int64_t page_tokens, int64_t seqs, int64_t max_pages, int64_t tokens,
                                              int64_t Hq, int64_t Hkv, int64_t max_q, int64_t max_kv) {
-    mxattn::CacheAttendArgs a{};
-    if (!sized_attend(a, page_tokens, seqs, max_pages, tokens, Hq, Hkv, max_q, max_kv)) return 0;
-    return mxattn::cache_weigh_workspace(a, max_q, max_kv);
+    mxattn::CacheWeighArgs w{};
+    if (!sized_attend(w.a, page_tokens, seqs, max_pages, tokens, Hq, Hkv, max_q, max_kv)) return 0;
+    return mxattn::cache_weigh_workspace(w, max_q, max_kv);
 }
 
 // The arguments that the calls of attention over the cache share.
@@ -937,7 +937,7 @@ int mxattn_cache_attend_weights(const void* q, int64_t q_stride, const uint8_t* 
         in_cache(weights_out, wb, w.a.c) || (weights && overlaps(weights, wb, out, x.out_bytes)) ||
         (weights && weights != weights_out && overlaps(weights_out, wb, weights, wb)))
         return MXATTN_ERR_SHAPE;
-    const size_t bytes = mxattn::cache_weigh_workspace(w.a, x.max_q, x.max_kv);
+    const size_t bytes = mxattn::cache_weigh_workspace(w, x.max_q, x.max_kv);
     if (workspace && (overlaps(workspace, bytes, weights_out, wb) || (weights && overlaps(workspace, bytes, weights, wb))))
         return MXATTN_ERR_SHAPE;
     w.before = weights;

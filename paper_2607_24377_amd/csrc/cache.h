@@ -101,8 +101,11 @@ struct CacheWeighArgs {
     CacheAttendArgs a;
     const float* before;  // [pages, heads, page_tokens]; null: zeros
     float* after;
+    float* partial;          // set by the call, as what follows: [runs, seqs * heads, partial_stride]
+    int64_t partial_stride;
+    int runs;
 };
-size_t cache_weigh_workspace(CacheAttendArgs a, int64_t max_q, int64_t max_kv);
+size_t cache_weigh_workspace(CacheWeighArgs w, int64_t max_q, int64_t max_kv);
 hipError_t launch_cache_weigh(CacheWeighArgs w, int64_t max_q, int64_t max_kv, hipStream_t stream);
 
 // Which tokens stay, and moving them together (cache_evict.hip).

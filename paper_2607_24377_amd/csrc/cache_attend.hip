@@ -298,14 +298,22 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_items_kernel(CacheAt
 // keys that a row sees (us, kernels with their joins; 8 KV heads):
 //   few keys: an item is one workgroup's.  16 sequences x 5 rows x 1000 keys 13.6, in
 //   shares 18.2; one sequence's row over 2000 keys 16.7 and 14.3.  Up to 128 rows: 90
-//   rows x 290 keys 8.5, in shares 18.8, in tiles of 128 rows 33.
+//   rows x 290 keys 8.5, in shares 18.8, in tiles of 128 rows 33.  More rows, where 32 x 32
+//   scores are not many (plain attention, whose callers know its bits, stays as it was):
+//   4 sequences x 290 rows x 294 keys 12, in tiles 41; 35 x 445 rows of one head x 485 keys
+//   21 and 37; 4 x 2048 rows x 512 keys (32 K of them) 46 and 63, 15 x 1704 of 3 heads x 569
+//   (44 K) 67 and 71, 8 x 2048 x 768 (98 K) 108 and 97.
 //   else up to 32 rows: shares; more: tiles of 128 rows, whose four waves read the keys
 //   once.  16 sequences x 40 rows x 4000 keys, in shares 57, in tiles 50; 125 rows 83
 //   and 61.
+constexpr int64_t kFewBlocks = 40960;
+int64_t score_blocks(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    return a.c.seqs * ((max_q * a.group + kRows - 1) / kRows) * a.c.heads * ((max_kv + kBlockTokens - 1) / kBlockTokens);
+}
 enum Way { kItems, kShares, kTiles };
 Way way(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
     const int64_t rows = max_q * a.group;
-    if (max_kv <= 1024 && rows <= 128) return kItems;
+    if (max_kv <= 1024 && (rows <= 128 || (a.kind != kPlain && score_blocks(a, max_q, max_kv) <= kFewBlocks))) return kItems;
     return rows <= kRows ? kShares : kTiles;
 }
 
@@ -356,7 +364,7 @@ size_t cache_attend_workspace(const CacheAttendArgs& a, int64_t max_q, int64_t m
 }
 
 bool cache_attend_keeps_scores(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
-    return way(a, max_q, max_kv) != kTiles;
+    return way(a, max_q, max_kv) != kTiles && max_q * a.group <= 128;
 }
 
 hipError_t launch_cache_attend(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv, hipStream_t stream) {

@@ -147,14 +147,14 @@ struct Stride {
 };
 
 template <bool kWhole>
-__global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheWeighArgs w, int chunks) {
+__global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheWeighArgs w, int chunks, int runs) {
     __shared__ __align__(16) uint8_t st0[kStageBytes];
     __shared__ __align__(16) uint8_t st1[kStageBytes];
     __shared__ __align__(16) uint8_t st2[kStageBytes];
     __shared__ float s_sum[kKeyWaves * kBlockTokens];
     const CacheAttendArgs& a = w.a;
     const CacheArgs& c = a.c;
-    const Placed place(a.c, chunks);
+    const Placed place(a.c, chunks * runs);
     const int s = place.s, head = place.head;
     if (s < 0) return;
     const Keys k(a, s);
@@ -163,17 +163,18 @@ __global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheW
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane & 31, h = lane >> 5;
     constexpr int kGroupKeys = kKeyWaves * kBlockTokens;
     const int last = (k.keys + kBlockTokens - 1) / kBlockTokens - 1;
-    const int half = wave >> 2;
+    const int half = wave >> 2, chunk = place.chunk / runs, run = place.chunk - chunk * runs;
     const Stride<kWhole> by_q(a, a.q_stride * 2, kHeadDim * 2), by_stats(a, (int64_t)c.heads * a.group * 8, 8);
     const uint16_t* q0 = a.q + row_offset(a, k.first, 0, head, a.q_stride);
     const float2* stats0 = a.stats + row_number(a, k.first, 0, head);
     const uint8_t* last_q = by_q.at(a, q0, rows - 1).p;
     const uint8_t* last_stats = by_stats.at(a, stats0, rows - 1).p;
-    for (int64_t j64 = (int64_t)place.chunk * kGroupKeys; j64 < k.keys; j64 += (int64_t)chunks * kGroupKeys) {
+    for (int64_t j64 = (int64_t)chunk * kGroupKeys; j64 < k.keys; j64 += (int64_t)chunks * kGroupKeys) {
         const int base = (int)j64 + (wave & 3) * kBlockTokens;
         // the first rows whose tokens see the group's first key
-        const int from = (a.causal ? max(0, (int)j64 - past) * a.group : 0) & ~(kStepRows - 1);
-        const int steps = (rows - from + kStepRows - 1) / kStepRows;
+        const int all_from = (a.causal ? max(0, (int)j64 - past) * a.group : 0) & ~(kStepRows - 1);
+        const int all_steps = (rows - all_from + kStepRows - 1) / kStepRows, before = all_steps * run / runs;
+        const int from = all_from + before * kStepRows, steps = all_steps * (run + 1) / runs - before;
         // (a row's chunks keep their order from step to step, as 16 divides it)
         const int lane_row = 8 * wave + (lane >> 4), ch0 = 16 * ((lane ^ lane_row) & 15), ch1 = 16 * ((lane ^ lane_row ^ 4) & 15);
         Walk r0 = by_q.at(a, q0, from + lane_row), r1 = by_q.at(a, q0, from + lane_row + 4);
@@ -284,9 +285,31 @@ __global__ __launch_bounds__(64 * kWaves, 4) void cache_weigh_rows_kernel(CacheW
         if (half) s_sum[mine] = total;
         __syncthreads();
         if (half || (q & 1) || j >= k.keys) continue;
+        total += s_sum[mine];
+        if (runs > 1) {
+            w.partial[((int64_t)run * c.seqs * c.heads + (int64_t)s * c.heads + head) * w.partial_stride + j] = total;
+            continue;
+        }
         const int64_t at = weights_at(c, s, head, j);
-        if (at >= 0) w.after[at] = sum_with(w, at, j < past, total + s_sum[mine]);
+        if (at >= 0) w.after[at] = sum_with(w, at, j < past, total);
     }
+}
+
+// The runs' sums of a key, one after another.
+__global__ __launch_bounds__(kThreads) void cache_weigh_runs_kernel(CacheWeighArgs w, int chunks, int runs) {
+    const CacheAttendArgs& a = w.a;
+    const Placed place(a.c, chunks);
+    if (place.s < 0) return;
+    const Keys k(a, place.s);
+    const int j = place.chunk * kThreads + threadIdx.x;
+    if (k.n == 0 || j >= k.keys) return;
+    const int64_t items = (int64_t)a.c.seqs * a.c.heads;
+    const float* p = w.partial + ((int64_t)place.s * a.c.heads + place.head) * w.partial_stride + j;
+    float sum = 0.f;
+#pragma unroll 8
+    for (int r = 0; r < runs; r++) sum += p[r * items * w.partial_stride];
+    const int64_t at = weights_at(a.c, place.s, place.head, j);
+    if (at >= 0) w.after[at] = sum_with(w, at, j < k.keys - k.n, sum);
 }
 
 // Scores are kept up to this many bytes; beyond, they are computed twice.
@@ -300,36 +323,56 @@ int chunks_of(const CacheAttendArgs& a, int64_t max_kv, int keys) {
     return (int)std::min<int64_t>(most, (max_kv + keys - 1) / keys);
 }
 
+// Into how many runs the rows are cut, where few keys and heads leave the chip idle: two
+// workgroups a CU, as far as the caller's bounds say, each of two steps or more.  (8000 rows x
+// 1000 keys of one head: 99 us by 8 workgroups, 14 in runs, 6 of them for their sums.)
+int runs_of(const CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+    const int64_t groups = (int64_t)a.c.seqs * a.c.heads * ((max_kv + kKeyWaves * kBlockTokens - 1) / (kKeyWaves * kBlockTokens));
+    const int64_t steps = (max_q * a.group + kStepRows - 1) / kStepRows;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / groups, steps / 2), 64));
+}
+
 // Chooses the kind, and where what the kernels leave for the sums lies; returns the bytes.
-size_t lay_out(CacheAttendArgs& a, int64_t max_q, int64_t max_kv) {
+size_t lay_out(CacheWeighArgs& w, int64_t max_q, int64_t max_kv) {
+    CacheAttendArgs& a = w.a;
     const int64_t rows = (int64_t)a.c.tokens * a.c.heads * a.group;
     a.score_stride = (max_kv + 31) / 32 * 32;
-    a.kind = cache_attend_keeps_scores(a, max_q, max_kv) && rows <= kMostScores / 4 / a.score_stride ? kWeigh : kWeighStats;
+    a.kind = kWeighStats;
+    if (cache_attend_keeps_scores(a, max_q, max_kv) && rows <= kMostScores / 4 / a.score_stride) a.kind = kWeigh;
     const size_t parts = up16(cache_attend_workspace(a, max_q, max_kv));
     const size_t stats = up16((size_t)rows * sizeof(float2));
     a.stats = reinterpret_cast<float2*>(a.workspace + parts);
-    a.scores = reinterpret_cast<float*>(a.workspace + parts + stats);
-    return parts + stats + (a.kind == kWeigh ? (size_t)rows * (size_t)a.score_stride * 4 : 0);
+    a.scores = w.partial = reinterpret_cast<float*>(a.workspace + parts + stats);
+    w.partial_stride = a.score_stride;
+    w.runs = a.kind == kWeigh ? 1 : runs_of(a, max_q, max_kv);
+    const int64_t more = a.kind == kWeigh ? rows : w.runs > 1 ? (int64_t)w.runs * a.c.seqs * a.c.heads : 0;
+    return parts + stats + (size_t)more * (size_t)a.score_stride * 4;
 }
 
 }  // namespace
 
-size_t cache_weigh_workspace(CacheAttendArgs a, int64_t max_q, int64_t max_kv) { return lay_out(a, max_q, max_kv); }
+size_t cache_weigh_workspace(CacheWeighArgs w, int64_t max_q, int64_t max_kv) { return lay_out(w, max_q, max_kv); }
 
 hipError_t launch_cache_weigh(CacheWeighArgs w, int64_t max_q, int64_t max_kv, hipStream_t stream) {
     CacheAttendArgs& a = w.a;
     a.most_keys = (int)max_kv;
-    lay_out(a, max_q, max_kv);
+    lay_out(w, max_q, max_kv);
     if (hipError_t e = launch_cache_attend(a, max_q, max_kv, stream)) return e;
     if (a.kind == kWeigh) {
         const int chunks = chunks_of(a, max_kv, 4 * kThreads);
         cache_weigh_scores_kernel<<<placed_grid(a.c, chunks), kThreads, 0, stream>>>(w, chunks);
-    } else {
-        const int chunks = chunks_of(a, max_kv, kKeyWaves * kBlockTokens);
-        if (kStepRows % a.group == 0)
-            cache_weigh_rows_kernel<true><<<placed_grid(a.c, chunks), 64 * kWaves, 0, stream>>>(w, chunks);
-        else
-            cache_weigh_rows_kernel<false><<<placed_grid(a.c, chunks), 64 * kWaves, 0, stream>>>(w, chunks);
+        return hipGetLastError();
+    }
+    const int chunks = chunks_of(a, max_kv, kKeyWaves * kBlockTokens);
+    const unsigned grid = placed_grid(a.c, (int64_t)chunks * w.runs);
+    if (kStepRows % a.group == 0)
+        cache_weigh_rows_kernel<true><<<grid, 64 * kWaves, 0, stream>>>(w, chunks, w.runs);
+    else
+        cache_weigh_rows_kernel<false><<<grid, 64 * kWaves, 0, stream>>>(w, chunks, w.runs);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (w.runs > 1) {
+        const int sums = (int)((max_kv + kThreads - 1) / kThreads);
+        cache_weigh_runs_kernel<<<placed_grid(a.c, sums), kThreads, 0, stream>>>(w, sums, w.runs);
     }
     return hipGetLastError();
 }

@@ -278,10 +278,10 @@ struct Cutting {
     __device__ __forceinline__ bool whole() const { return L == count; }
 };
 
-// A workgroup for a head: as many keys as its registers hold in one reading.
-constexpr int kOneThreads = 1024;
-constexpr int kOneMost = 16 * kOneThreads;
+// A workgroup for a head, which reads its keys once if its registers hold them (16 a thread).
+constexpr int kOneMost = 16 * 1024;
 
+template <int kOneThreads>
 __global__ __launch_bounds__(kOneThreads) void cache_select_kernel(SelectArgs a) {
     constexpr int kWavesHere = kOneThreads / 64;
     __shared__ __align__(16) Histogram<kOneThreads, 4> hist;
@@ -742,7 +742,11 @@ hipError_t launch_cache_select(const SelectArgs& args, hipStream_t stream) {
     const int64_t reach = ((int64_t)a.c.max_pages << a.c.bpp_log2) * kBlockTokens;
     a.chunk_keys = chunk_keys((int64_t)a.c.seqs * a.c.heads, reach);
     if (!a.chunk_keys) {
-        cache_select_kernel<<<(unsigned)a.c.seqs * (unsigned)a.c.heads, kOneThreads, 0, stream>>>(a);
+        const unsigned items = (unsigned)a.c.seqs * (unsigned)a.c.heads;
+        if (reach <= 1024)  // (1080 heads of 102 keys 21 us, by 1024 threads each 27; 512 of 4000 17 and 13)
+            cache_select_kernel<256><<<items, 256, 0, stream>>>(a);
+        else
+            cache_select_kernel<1024><<<items, 1024, 0, stream>>>(a);
         return hipGetLastError();
     }
     a.chunks = (int)((reach + a.chunk_keys - 1) / a.chunk_keys);

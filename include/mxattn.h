@@ -364,8 +364,9 @@ int mxattn_cache_append(const void* k, const void* v, int64_t k_stride, int64_t 
 
 /* Attention of the call's tokens over their sequences' cached keys (their own
  * among them, appended before): O = softmax(Q K^T / sqrt(d)) V with fp32 scores,
- * softmax and sums.  Query head i reads KV head i / (Hq / Hkv).  Three choices hold
- * less than fp32: P is rounded to f16 before its product with V (by 2^-11 of each p,
+ * softmax and sums.  Query head i reads KV head i / (Hq / Hkv).  Four choices hold
+ * less than fp32: scores are sums of the FP8 matrix cores (off by up to 2^-15 of
+ * sum |q k|, as measured); P is rounded to f16 before its product with V (by 2^-11 of each p,
  * or 2^-36 of the row's largest below 2^-25 of that); Q is held to 2^-21 of its row's
  * largest magnitude; and blocks of V whose scale is below 2^-55 of the largest one of
  * their sequence lose digits.  Scores of 2^26 and more in magnitude, and keys of 2^112

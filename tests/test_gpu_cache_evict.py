@@ -233,6 +233,70 @@ def test_eviction_in_a_graph(mx):  # noqa: F811
         check_cache(cache, c)
 
 
+def test_steps_past_32_bit_offsets(mx):  # noqa: F811
+    """Blocks past 4 GiB of codes: the same as at the cache's start."""
+    pages, H, page = 36000, 8, 128  # 4.7 GB of K codes, and of V
+    new, past = [1, 40], [300, 1500]
+    table, start, lens, _ = batch(new, past, page, spare=0)
+    table = torch.where(table < pages, table, -1)
+    used = int(table.max()) + 1
+    out = torch.arange(2 * 4, dtype=torch.int32).view(2, 4) + used  # 400 tokens each
+    used += 8
+    k, v, q = rows(sum(lens), H, 1), rows(sum(lens), H, 2), rows(start[-1], 2 * H, 3)
+    cache = tuple(torch.zeros(s, dtype=torch.uint8, device="cuda") for s in mx.cache_shapes(pages, H, page))
+    w = torch.zeros((pages, H, page), device="cuda")
+    first = [0, lens[0], sum(lens)]
+    tree = torch.full((start[-1], 2), -1, dtype=torch.int32, device="cuda")
+    got = []
+    for shift in (0, pages - used):
+        t, o = torch.where(table >= 0, table + shift, table).cuda(), (out + shift).cuda()
+        mx.cache_append(k, v, *cache, t, ints(first), ints(lens))
+        args = (q, *cache, t, ints(start), ints(lens))
+        res = [mx.cache_attend_window(*args, 700, 40, True, *b) for b in ((1, 100), (1, 5000), (40, 5000))]
+        res += [mx.cache_attend_tree(*args, tree, *b) for b in ((1, 5000), (40, 5000))]
+        res += [mx.cache_attend_weights(*args, w, True, *b)[0] for b in ((1, 1600), (40, 1600))]
+        kept, counts = mx.cache_select(w, t, ints(lens), 400, 4, 20)
+        mx.cache_compact(*cache, t, kept, counts, None, o, w)
+        mx.cache_compact(*cache, t, kept, counts)
+        got.append(res + [kept, counts] + [x[shift:shift + used].clone() for x in (*cache, w)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b) and bool((a != 0).any())
+
+
+def test_two_graphs_one_after_another(mx):  # noqa: F811
+    """Calls with workspace captured twice, on other inputs, and replayed in turn: neither uses the other's."""
+    lens, H, page = [700, 2100], 2, 256
+    table, _, lens, pages = batch([0] * 2, lens, page)
+    table = torch.cat((torch.where(table < pages, table, -1), torch.full((2, 80), -1, dtype=torch.int32)), 1)  # > 16384 keys
+    cache = filled(mx, pages, H, page, 7)
+    t, L, st = table.cuda(), ints(lens), ints([0, 1, 2])
+    calls, graphs, outs, want = [], [], [], []
+    for i in range(2):
+        q, w = rows(2, 8, 10 + i), heavy(pages, H, page, i).cuda()
+
+        def call(q=q, w=w):
+            o, v = mx.cache_attend_weights(q, *cache, t, st, L, w, True, 1, 2100, weights_out=torch.zeros_like(w))
+            return [o, v, *mx.cache_select(v, t, L, 300, 2, 9),
+                    mx.cache_attend_window(q, *cache, t, st, L, 1500, 3, True, 1, 2100)]
+        want.append(call())
+        calls.append(call)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call())
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 0, 1):
+        for x in outs[i]:
+            x.zero_()
+        graphs[i].replay()
+        calls[1 - i]()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
+    graphs[0].replay()
+    graphs[1].replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for o, w in zip(outs, want) for a, b in zip(o, w))
+
+
 def test_a_generation_with_drafts_and_eviction(mx):  # noqa: F811
     """Prompts are appended and weighed, cut to a budget in place, generation goes on with a window, a tree of drafts is
     verified and its accepted path stays: every attention agrees with 64 bits over what the cache holds."""

@@ -907,10 +907,13 @@ int mxattn_cache_attend_tree(const void* q, int64_t q_stride, const uint8_t* k_c
     if (int st = check_attend(x, a)) return st;
     if (tree_words < 1 || tree_words > mxattn::kMaxKeys / 32) return MXATTN_ERR_SHAPE;
     if (!aligned(tree, 4)) return MXATTN_ERR_ALIGN;
-    if (overlaps(out, x.out_bytes, tree, (size_t)tokens * tree_words * 4)) return MXATTN_ERR_SHAPE;
+    const size_t tb = (size_t)tokens * (size_t)tree_words * 4;
+    if (overlaps(out, x.out_bytes, tree, tb)) return MXATTN_ERR_SHAPE;
     a.kind = mxattn::kTree;
     a.tree = tree;
     a.tree_words = (int)tree_words;
+    const size_t bytes = mxattn::cache_attend_workspace(a, x.max_q, x.max_kv);
+    if (workspace && bytes && overlaps(workspace, bytes, tree, tb)) return MXATTN_ERR_SHAPE;
     return run_plain_attend(x, a);
 }
 

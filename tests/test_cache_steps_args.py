@@ -60,6 +60,8 @@ LONG_SELECT_BAD = [
     (dict(ws=far(43) + 2384, ws_bytes=1 << 30), SHAPE), (dict(ws=far(44), ws_bytes=1 << 30), SHAPE),
     (dict(ws=far(13), ws_bytes=1 << 30), SHAPE), (dict(ws=far(11) + 48, ws_bytes=1 << 30), SHAPE),
 ]
+LONG_TREE = dict(TREE, page=4096, max_pages=50, max_q=1)
+CALLS += [("mxattn_cache_attend_tree", LONG_TREE, (dict(ws=ws, ws_bytes=1 << 30), SHAPE)) for ws in (far(40), far(40) + 64, far(40) - 16)]
 CALLS += [("mxattn_cache_select", LONG_SELECT, c) for c in LONG_SELECT_BAD]
 CALLS += [("mxattn_cache_select", SELECT, c) for c in SELECT_BAD] + [("mxattn_cache_compact", COMPACT, c) for c in COMPACT_BAD]
 

@@ -5,8 +5,8 @@
 // stays is found digit by digit (11, 11 and 10 bits of the number in an order of unsigned
 // integers, histograms in LDS); then the kept positions are written in order, each wave
 // from where the stretches before its own end.  16 sequences of up to 4500 keys, 8 heads:
-// 12.4 us, a chain of loads and barriers; one of 118800: 5, 10 and 13 us (by one workgroup
-// for a head 88, with one key a lane and load 254).
+// 12.4 us, a chain of loads and barriers; one of 118800: 5, 10, 4 and 13 us (by one workgroup
+// for a head 88, with one key a lane and load 254); of 1000000 even weights 78 in all.
 //
 // Compaction: position base + i becomes what was at kept[i].  A block of 32 kept tokens
 // takes the largest scale byte of the blocks that they come from, so that no code grows
@@ -136,6 +136,15 @@ struct Histogram {
             n += v.x + v.y + v.z + v.w;
         }
         return n;
+    }
+    // Writes the counts (of no more than 16 bits) to a row of kDigits.
+    __device__ __forceinline__ void store(uint16_t* row) const {
+        static_assert(kThreads * 8 == kDigits, "eight digits a thread");
+        uint32_t n[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) n[i] = total(8 * (int)threadIdx.x + i);
+        reinterpret_cast<uint4*>(row)[threadIdx.x] =
+            make_uint4(n[0] | n[1] << 16, n[2] | n[3] << 16, n[4] | n[5] << 16, n[6] | n[7] << 16);
     }
     // The digit of the last one that stays; n[i]: the number of digit kDigits - 1 - kEach tid - i.
     // Returns how many have it.  Barriers before and after.
@@ -334,31 +343,57 @@ __global__ __launch_bounds__(kOneThreads) void cache_select_kernel(SelectArgs a)
     write_kept(st, search, any, at, same, x.kept);
 }
 
-// More keys: a workgroup for every chunk of a head's, in three launches.  The first digit
+// More keys: a workgroup for every chunk of a head's, in four launches.  The first digit
 // of all (a histogram of each chunk, added up by everyone who needs it); what begins with
 // it put aside, in one list for a head in any order; the rest of the search, by every
 // workgroup for itself over that list, which also says what the chunks before keep.
+// Where too many begin with it to be listed, the other digits go the first one's way: the
+// second in the list's place, the third in the launch that has nothing to do otherwise.
 constexpr int kManyThreads = 256;
-constexpr int kListMost = 16384;
-constexpr int kListHere = 4096;  // of a workgroup, which takes its room in the head's list at once
+constexpr int kListMost = 4096;  // (118800 keys, 2000 on the list: 28 us for 32 without; 14000: 38 and 32)
 
 // A head's part of the workspace.
 struct Lists {
-    uint16_t* digits;  // [chunks, kDigits]
+    uint16_t* digits;  // [chunks, kDigits]: the first, or the third
     uint2* list;       // [kListMost]: weight (ordered), chunk
+    uint16_t* second;  // [chunks, kDigits], in the list's place
     uint32_t* above;   // [chunks]: those above all that begin so, or kept for their place
-    uint32_t* header;  // entries of the list, the first digit, how many of it stay, how many have it
+    // entries of the list, the first digit, how many of it stay, how many have it; the first two digits, how many of them stay
+    uint32_t* header;
+    static constexpr int kHeader = 32;
+    static __host__ __device__ size_t list_bytes(int chunks) {
+        const size_t second = (size_t)chunks * kDigits * 2;
+        return second > kListMost * 8 ? second : kListMost * 8;
+    }
     static size_t bytes(int chunks) {
-        return ((size_t)chunks * (kDigits * 2 + 4) + kListMost * 8 + 16 + 15) & ~(size_t)15;
+        return ((size_t)chunks * (kDigits * 2 + 4) + list_bytes(chunks) + kHeader + 15) & ~(size_t)15;
     }
     __device__ __forceinline__ Lists(const SelectArgs& a, int64_t item) {
         uint8_t* p = a.workspace + item * a.item_bytes;
         header = reinterpret_cast<uint32_t*>(p);
-        list = reinterpret_cast<uint2*>(p + 16);
-        digits = reinterpret_cast<uint16_t*>(p + 16 + kListMost * 8);
-        above = reinterpret_cast<uint32_t*>(p + 16 + kListMost * 8 + (size_t)a.chunks * kDigits * 2);
+        list = reinterpret_cast<uint2*>(p + kHeader);
+        second = reinterpret_cast<uint16_t*>(p + kHeader);
+        digits = reinterpret_cast<uint16_t*>(p + kHeader + list_bytes(a.chunks));
+        above = reinterpret_cast<uint32_t*>(p + kHeader + list_bytes(a.chunks) + (size_t)a.chunks * kDigits * 2);
     }
+    __device__ __forceinline__ Search first() const { return {header[1], Search::mask(0) << Search::shift(0), header[2]}; }
+    __device__ __forceinline__ bool listed() const { return header[3] <= kListMost; }
 };
+
+// A thread's eight digits, from the largest of all down, of `chunks` rows together.
+__device__ __forceinline__ void add_digits(const uint16_t* rows, int chunks, uint32_t (&n)[8]) {
+    const uint4* from = reinterpret_cast<const uint4*>(rows) + (kDigits / 8 - 1 - threadIdx.x);
+#pragma unroll 8
+    for (int k = 0; k < chunks; k++) {
+        const uint4 v = from[(size_t)k * (kDigits / 8)];
+        const uint32_t d[4] = {v.w, v.z, v.y, v.x};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            n[2 * i] += d[i] >> 16;
+            n[2 * i + 1] += d[i] & 0xFFFFu;
+        }
+    }
+}
 
 // The chunk of a workgroup, and the stretch of one of its four waves.
 struct Chunk {
@@ -389,17 +424,12 @@ __global__ __launch_bounds__(kManyThreads) void cache_select_digits_kernel(Selec
             if (free >> i & 1) hist.add(ordered(w[i]), 0);
     });
     __syncthreads();
-    uint4 out;
-    uint32_t n[8];
-#pragma unroll
-    for (int i = 0; i < 8; i++) n[i] = hist.total(8 * (int)threadIdx.x + i);
-    out = make_uint4(n[0] | n[1] << 16, n[2] | n[3] << 16, n[4] | n[5] << 16, n[6] | n[7] << 16);
-    reinterpret_cast<uint4*>(lists.digits + (size_t)place.chunk * kDigits)[threadIdx.x] = out;
+    hist.store(lists.digits + (size_t)place.chunk * kDigits);
 }
 
 __global__ __launch_bounds__(kManyThreads) void cache_select_aside_kernel(SelectArgs a) {
     __shared__ __align__(16) Histogram<kManyThreads, 4> hist;
-    __shared__ uint32_t s_above, s_count, s_first, s_list[kListHere];
+    __shared__ uint32_t s_above, s_count, s_first, s_list[kListMost];
     const Placed place(a.c, a.chunks);
     if (place.s < 0) return;
     const Cutting x(a, place.s, place.head);
@@ -410,39 +440,39 @@ __global__ __launch_bounds__(kManyThreads) void cache_select_aside_kernel(Select
     Stretch st(a, x.s, x.head, chunk.j0, chunk.j1, x.m0, x.m1);
     Search search{0, 0, x.need};
     if (threadIdx.x == 0) s_above = s_count = 0;
+    uint32_t having = 0;
     if (any) {
         uint32_t n[8] = {0, 0, 0, 0, 0, 0, 0, 0};  // of digits from the largest down
-        const uint4* from = reinterpret_cast<const uint4*>(lists.digits) + (kDigits / 8 - 1 - threadIdx.x);
-#pragma unroll 8
-        for (int k = 0; k < chunk.all; k++) {
-            const uint4 v = from[(size_t)k * (kDigits / 8)];
-            const uint32_t d[4] = {v.w, v.z, v.y, v.x};
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                n[2 * i] += d[i] >> 16;
-                n[2 * i + 1] += d[i] & 0xFFFFu;
-            }
-        }
-        const uint32_t having = hist.find(search, 0, n);
+        add_digits(lists.digits, chunk.all, n);
+        having = hist.find(search, 0, n);
         if (place.chunk == 0 && threadIdx.x == 0) {
             lists.header[1] = search.prefix;
             lists.header[2] = search.need;
             lists.header[3] = having;
         }
-    } else {
-        __syncthreads();
     }
+    if (having > kListMost) {
+        hist.clear();
+        __syncthreads();
+        st.each([&](int, const f32x4u& w, uint32_t free, uint32_t) {
+            uint32_t u[4], mine, more;
+            sort_out(search, w, free, u, mine, more);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (mine >> i & 1) hist.add(u[i], 1);
+        });
+        __syncthreads();
+        hist.store(lists.second + (size_t)place.chunk * kDigits);
+        return;
+    }
+    __syncthreads();
     uint32_t above = 0;
     st.each([&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
         uint32_t u[4], mine = 0, more = 0;
         if (any) {
             sort_out(search, w, free, u, mine, more);
             put_aside(mine, u, &s_count, [&](uint32_t at, uint32_t v) {
-                if (at >= kListHere) at = atomicAdd(lists.header, 1u) + kListHere;
-                if (at < kListHere)
-                    s_list[at] = v;
-                else if (at - kListHere < kListMost)
-                    lists.list[at - kListHere] = make_uint2(v, (uint32_t)place.chunk);
+                if (at < kListMost) s_list[at] = v;  // (never more, as they are counted)
             });
         }
         above += (uint32_t)__popc(more | forced);
@@ -450,14 +480,52 @@ __global__ __launch_bounds__(kManyThreads) void cache_select_aside_kernel(Select
     above = sum64(above);
     if ((threadIdx.x & 63) == 0) atomicAdd(&s_above, above);
     __syncthreads();
-    const uint32_t n = min(s_count, (uint32_t)kListHere);
+    const uint32_t n = min(s_count, (uint32_t)kListMost);
     if (threadIdx.x == 0) {
         lists.above[place.chunk] = s_above;
-        s_first = n ? atomicAdd(lists.header, n) : 0;
+        s_first = n ? atomicAdd(lists.header, n) : 0;  // (a chunk's room in the head's list at once)
     }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < n; i += kManyThreads)
         if (s_first + i < kListMost) lists.list[s_first + i] = make_uint2(s_list[i], (uint32_t)place.chunk);
+}
+
+// The third digit, where there is no list.
+__global__ __launch_bounds__(kManyThreads) void cache_select_third_kernel(SelectArgs a) {
+    __shared__ __align__(16) Histogram<kManyThreads, 4> hist;
+    __shared__ uint32_t s_above;
+    const Placed place(a.c, a.chunks);
+    if (place.s < 0) return;
+    const Cutting x(a, place.s, place.head);
+    const Chunk chunk(a, x, place.chunk);
+    if (x.whole() || x.need == 0 || place.chunk >= chunk.all) return;
+    const Lists lists(a, (int64_t)x.s * a.c.heads + x.head);
+    if (lists.listed()) return;
+    Stretch st(a, x.s, x.head, chunk.j0, chunk.j1, x.m0, x.m1);
+    Search search = lists.first();
+    uint32_t n[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    add_digits(lists.second, chunk.all, n);
+    if (threadIdx.x == 0) s_above = 0;
+    hist.clear();
+    hist.find(search, 1, n);
+    if (place.chunk == 0 && threadIdx.x == 0) {
+        lists.header[4] = search.prefix;
+        lists.header[5] = search.need;
+    }
+    uint32_t above = 0;
+    st.each([&](int, const f32x4u& w, uint32_t free, uint32_t forced) {
+        uint32_t u[4], mine, more;
+        sort_out(search, w, free, u, mine, more);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (mine >> i & 1) hist.add(u[i], 2);
+        above += (uint32_t)__popc(more | forced);
+    });
+    above = sum64(above);
+    if ((threadIdx.x & 63) == 0) atomicAdd(&s_above, above);
+    __syncthreads();
+    hist.store(lists.digits + (size_t)place.chunk * kDigits);
+    if (threadIdx.x == 0) lists.above[place.chunk] = s_above;
 }
 
 __global__ __launch_bounds__(kManyThreads) void cache_select_write_kernel(SelectArgs a) {
@@ -482,33 +550,33 @@ __global__ __launch_bounds__(kManyThreads) void cache_select_write_kernel(Select
     Search search{0, 0, x.need};
     if (tid < 2) s_before[tid] = 0;
     uint32_t at = 0, same = 0;
-    if (any) {
-        search = {lists.header[1], Search::mask(0) << Search::shift(0), lists.header[2]};
+    if (any && !lists.listed()) {
+        search = {lists.header[4], ~Search::mask(2), lists.header[5]};
+        uint32_t n[8] = {0, 0, 0, 0, 0, 0, 0, 0}, before[8];
+        add_digits(lists.digits, place.chunk, n);
+#pragma unroll
+        for (int i = 0; i < 8; i++) before[i] = n[i];
+        add_digits(lists.digits + (size_t)place.chunk * kDigits, chunk.all - place.chunk, n);
+        hist.find(search, 2, n);
+        const uint32_t found = search.prefix & Search::mask(2);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint32_t digit = (uint32_t)(kDigits - 1 - 8 * tid - i);
+            at += digit > found ? before[i] : 0;
+            same += digit == found ? before[i] : 0;
+        }
+    } else if (any) {
+        search = lists.first();
         const uint32_t having = lists.header[3];
-        // f of every weight that begins with the prefix and its chunk; a list that is too long: from the weights
+        // f of every weight that begins with the prefix and its chunk
         auto each = [&](const auto& f) {
-            if (having <= kListMost) {
-                for (uint32_t i = tid; i < having; i += 8 * kManyThreads) {  // eight in flight (14 K of them: 37 us all in all for 50)
-                    uint2 e[8];
+            for (uint32_t i = tid; i < having; i += 8 * kManyThreads) {  // eight in flight
+                uint2 e[8];
 #pragma unroll
-                    for (int k = 0; k < 8; k++) e[k] = lists.list[min(i + k * kManyThreads, having - 1)];
+                for (int k = 0; k < 8; k++) e[k] = lists.list[min(i + k * kManyThreads, having - 1)];
 #pragma unroll
-                    for (int k = 0; k < 8; k++)
-                        if (i + k * kManyThreads < having) f(e[k].x, (int)e[k].y);
-                }
-            } else {
-                const int per = (x.L + 4 * 256 - 1) / (4 * 256) * 256;
-                const int j0 = min(wave * per, x.L), j1 = min(j0 + per, x.L);
-                const uint32_t first = search.prefix & (Search::mask(0) << Search::shift(0));
-                Stretch all(a, x.s, x.head, j0, j1, x.m0, x.m1);
-                all.each([&](int j, const f32x4u& w, uint32_t free, uint32_t) {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const uint32_t u = ordered(w[i]);
-                        if ((free >> i & 1) && (u & (Search::mask(0) << Search::shift(0))) == first)
-                            f(u, (j + i) / a.chunk_keys);
-                    }
-                });
+                for (int k = 0; k < 8; k++)
+                    if (i + k * kManyThreads < having) f(e[k].x, (int)e[k].y);
             }
         };
         for (int pass = 1; pass < 3; pass++) {
@@ -759,6 +827,8 @@ hipError_t launch_cache_select(const SelectArgs& args, hipStream_t stream) {
     cache_select_digits_kernel<<<grid, kManyThreads, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     cache_select_aside_kernel<<<grid, kManyThreads, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    cache_select_third_kernel<<<grid, kManyThreads, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     cache_select_write_kernel<<<grid, kManyThreads, 0, stream>>>(a);
     return hipGetLastError();

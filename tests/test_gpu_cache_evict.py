@@ -19,6 +19,10 @@ def heavy(pages, heads, page, seed, kind="some"):
         w = torch.randint(0, 3, w.shape, generator=g).float()
     if kind == "equal":
         w = torch.full_like(w, 0.25)
+    if kind == "even":
+        w = torch.rand(w.shape, generator=g)
+    if kind == "narrow":  # numbers next to one another
+        w = 1 + torch.randint(0, 3000, w.shape, generator=g).float() * 2 ** -23
     if kind == "odd":  # zeros of both signs, negatives, infinities, NaN, subnormals
         pick = torch.randint(0, 8, w.shape, generator=g)
         for i, x in enumerate((0.0, -0.0, -1.5, math.inf, -math.inf, math.nan, 1e-40)):
@@ -49,6 +53,8 @@ SELECTS = [
     ([70000], 2, 64, 30000, 10, 20, "equal"),
     ([300000], 1, 1024, 100001, 0, 0, "ties"),
     ([300000], 1, 4096, 2, 0, 1, "odd"),
+    ([300000, 65000, 9000], 2, 256, 90001, 4, 500, "even"),
+    ([200000, 16385], 2, 128, 15000, 0, 0, "narrow"),
 ]
 
 

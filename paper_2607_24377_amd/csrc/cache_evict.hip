@@ -287,7 +287,8 @@ struct Cutting {
     __device__ __forceinline__ bool whole() const { return L == count; }
 };
 
-// A workgroup for a head, which reads its keys once if its registers hold them (16 a thread).
+// A workgroup for a head, which reads its keys once if its registers hold them (16 a thread),
+// else in every pass.
 constexpr int kOneMost = 16 * 1024;
 
 template <int kOneThreads>
@@ -623,10 +624,12 @@ __global__ __launch_bounds__(kManyThreads) void cache_select_write_kernel(Select
 }
 
 // Keys of a chunk: 4096, or more where a head would have more than 64 of them; no more than
-// 16 bits count.  0: a workgroup for a head (few keys, or items that pass a launch's 2^32
-// threads).
+// 16 bits count.  0: a workgroup for a head: few keys, or items that pass a launch's 2^32
+// threads, or enough of them to fill the chip, where a longest one of 65536 keys takes 58 us
+// (256 of 32768 keys 38 us, in chunks 71 to 85; 512 of 65536 120 and 240 to 264; 128 of 32768
+// 34 and 40 to 50, of 65536 64 and 72 to 80; but 32 of 65536 58 and 28).
 int chunk_keys(int64_t items, int64_t reach) {
-    if (reach <= kOneMost) return 0;
+    if (reach <= (items >= 128 ? 65536 : kOneMost)) return 0;
     const int64_t n = std::min<int64_t>((reach + 64 * 4096 - 1) / (64 * 4096) * 4096, 61440);
     return (items + 7) * ((reach + n - 1) / n) < (int64_t)1 << 23 ? (int)n : 0;
 }

@@ -100,6 +100,7 @@ def test_select_workspace_sizes(L):  # noqa: F811
     size = L.mxattn_cache_select_workspace
     assert size(64, 3, 256, 2) == 0 and size(4096, 3, 4, 2) == 0  # a workgroup holds the keys
     assert size(4096, 1 << 18, 4096, 1) == 0  # more chunks than a launch holds
+    assert size(4096, 16, 16, 8) == 0 < size(4096, 16, 17, 8) and 0 < size(4096, 15, 16, 8)  # many heads: of longer ones too
     one = size(64, 1, 257, 1)
     assert 0 < one <= 1.2 * 2 ** 20 and one % 16 == 0 and size(64, 3, 257, 2) == 6 * one
     assert size(4096, 1, 4096, 1) <= 2.3e6

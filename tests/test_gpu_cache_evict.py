@@ -55,6 +55,9 @@ SELECTS = [
     ([300000], 1, 4096, 2, 0, 1, "odd"),
     ([300000, 65000, 9000], 2, 256, 90001, 4, 500, "even"),
     ([200000, 16385], 2, 128, 15000, 0, 0, "narrow"),
+    # so many heads that each is one workgroup's, which reads its keys again in every pass
+    ([20000, 16385, 30001] + [33 * i for i in range(127)], 2, 64, 3000, 4, 100, "odd"),
+    ([20000, 16384, 65535] + [9 * i for i in range(61)], 4, 32, 20, 0, 0, "narrow"),
 ]
 
 

@@ -476,8 +476,8 @@ size_t mxattn_cache_attend_weights_workspace(int64_t page_tokens, int64_t seqs, 
  *            (MXATTN_ERR_VALUE otherwise); seqs * Hkv < 2^22
  *   workspace  as mxattn_cache_attend's, of mxattn_cache_select_workspace() bytes: none
  *            where max_pages * page_tokens <= 16384 (65536 from seqs * Hkv = 128 on), else at
- *            most 2.3 MB for each sequence and KV head.  It shares no byte with the other arguments.  NULL: from the
- *            library's pool, not under graph capture. */
+ *            most 2.3 MB for each sequence and KV head.  It shares no byte with the other
+ *            arguments.  NULL: from the library's pool, not under graph capture. */
 int mxattn_cache_select(const float* weights, int64_t pages, int64_t page_tokens, const int32_t* page_table,
                         const int32_t* kv_len, int64_t seqs, int64_t max_pages, int64_t Hkv, int64_t budget,
                         int64_t sinks, int64_t recent, int32_t* kept, int32_t* counts, void* workspace,

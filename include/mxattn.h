@@ -442,7 +442,9 @@ int mxattn_cache_attend_tree(const void* q, int64_t q_stride, const uint8_t* k_c
  * that owns tokens of the call, and every KV head,
  *   weights_out[j] = (j < kv_len - n ? weights[j] : 0) + sum of p over the n tokens and the
  *                    Hq / Hkv heads
- * in fp32, p the probabilities that O is made of.  Weights lie beside the cache, fp32
+ * in fp32, p the probabilities that O is made of (before they are rounded to f16).  Scores
+ * are fp32 sums of exact products in this call, whatever its bounds: off by 2^-20 of
+ * sum |q k| and less, and the p of a row add up to 1 within 2^-16.  Weights lie beside the cache, fp32
  * [pages, Hkv, page_tokens]; those of other positions and sequences are not written.
  *   weights      NULL: zeros
  *   weights_out  may be `weights`; must not overlap it otherwise

@@ -85,7 +85,7 @@ struct CacheAttendArgs {
     int tree_words;
     int most_keys;               // kWeigh, kWeighStats: a longer sequence is none
     float2* stats;               // [tokens * Hq]: m and 1 / l of every row, p = exp2(s c - m) / l
-    float* scores;               // kWeigh: [tokens * Hq, score_stride], s c of the keys that a tile of rows sees
+    float* scores;               // kWeigh: [tokens * Hq, score_stride], s (without c) of the keys that a tile of rows sees
     int64_t score_stride;        // a multiple of 32
 };
 // max_q, max_kv: most new tokens and keys of a sequence, as far as the caller knows

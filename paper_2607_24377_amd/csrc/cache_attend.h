@@ -129,12 +129,12 @@ __device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QOperan
     return s;
 }
 
-// Q as it is, for scores that are kept or computed again as weights: the FP8 matrix cores
-// keep too few digits of the products that they add up (their sums are off by up to 2^-15
-// of sum |q k|, measured, so probabilities by 1e-5; beside the rounding of P and O that does
-// not count).  K's codes are exact in bf16 and bf16 products are added in fp32 (2^-24), in
-// the time of the two FP8 products and 32 conversions a block, for which attention of a
-// few rows has room.  The operands' channels in the order of the FP8 ones.
+// Q as it is, for attention that weighs the keys: the FP8 matrix cores keep too few digits
+// of the products that they add up (their sums are off by up to 2^-15 of sum |q k|,
+// measured, so probabilities by 1e-5; beside the rounding of P and O that does not count).
+// K's codes are exact in bf16 and bf16 products are added in fp32 (2^-24), in the time of
+// the four FP8 products and 32 conversions a block.  The operands' channels in the order
+// of the FP8 ones.
 struct QExact {
     uint4 r[8];
     float c;  // as QOperand's
@@ -194,7 +194,7 @@ __device__ __forceinline__ v16f scores(const uint4 (&k)[4], int e, const QExact&
 // Q as the kernels of a kind take it.
 template <AttendKind kKind>
 __device__ __forceinline__ auto load_q_of(const uint16_t* row, int h, float scale, bool live) {
-    if constexpr (kKind == kWeigh)
+    if constexpr (kKind == kWeigh || kKind == kWeighStats)
         return load_q_exact(row, h, scale, live);
     else
         return load_q(row, h, scale, live);
@@ -532,8 +532,7 @@ __device__ __forceinline__ void attend_block(State& st, Block& x, const Q& q, in
         if (scores_at) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<float4*>(scores_at + base + 16 * h + i) =
-                    make_float4(s[i] * q.c, s[i + 1] * q.c, s[i + 2] * q.c, s[i + 3] * q.c);
+                *reinterpret_cast<float4*>(scores_at + base + 16 * h + i) = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
         }
         prefetch();
     }

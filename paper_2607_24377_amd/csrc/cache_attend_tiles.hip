@@ -275,7 +275,8 @@ __device__ __forceinline__ uint4 part(const uint8_t* block, int p, int lane) {
     return *reinterpret_cast<const uint4*>(block + p * 1024 + lane * 16);
 }
 
-__device__ __forceinline__ v16f block_scores(const uint8_t* block, int e, const QOperand& q, int lane) {
+template <class Q>
+__device__ __forceinline__ v16f block_scores(const uint8_t* block, int e, const Q& q, int lane) {
     uint4 k[4];
 #pragma unroll
     for (int p = 0; p < 4; p++) k[p] = part(block, p, lane);
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_tiles_kernel(CacheAt
             StepLoader::pages(page, c, it.s, 2 * j0 + 4, all);
         };
         if (kKind == kWindow) load_first();
-        const QOperand qo = load_q(a.q + row_offset(a, it.first, row, it.head, a.q_stride), h, a.scale, live && sight.some());
+        const auto qo = load_q_of<kKind>(a.q + row_offset(a, it.first, row, it.head, a.q_stride), h, a.scale, live && sight.some());
         st.clear();
         if (kKind != kWindow) load_first();
         if (j0 < j1) {

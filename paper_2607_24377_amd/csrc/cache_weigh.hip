@@ -8,9 +8,13 @@
 // output).  Few rows: they leave the scores too, 4 bytes per row and key beside the 256
 // bytes of a key's codes, and a second pass over them sums.  Many rows: the scores are
 // computed once more, keys outside, rows inside, so that every sum stays in a wave's
-// registers and no order of additions depends on the schedule.  Either way the scores that
-// become weights are fp32 sums of exact products (QExact): a weight is then off by 1e-7 of
-// itself, by those of the FP8 matrix cores by 1e-5.
+// registers and no order of additions depends on the schedule.  Either way p's score is
+// the very number that l is a sum over: both come from one product of the same operands in
+// the same order, an fp32 sum of exact products (QExact), and s c - m is rounded once in
+// both.  A row's p then add up to 1 within the roundings of l's additions whatever the
+// scores' size, and each is off by its score's error, 2^-20 of sum |q k| / sqrt(d) and less
+// (m and l from FP8 products, as attention alone takes them, are off by up to 2^-15 of that:
+// 160 rows of scores of some hundreds added up to 159.97).
 //
 // Bound by what attention leaves and by the exponentials: 64 tokens over 8200 keys, 32 heads
 // on 8, 57 MB, 15 us; 4 prompts of up to 2048 tokens 135 to 139 us, beside 250 to 270 for their
@@ -66,6 +70,10 @@ __global__ __launch_bounds__(kThreads) void cache_weigh_scores_kernel(CacheWeigh
         // the rows that see key j, four in flight (a token's heads lie in a row)
         const int64_t row0 = ((int64_t)k.first * a.c.heads + head) * a.group, token = (int64_t)a.c.heads * a.group;
         const int rows = k.n * a.group;
+        // (s c - m in one rounding, as in l)
+        auto weight = [&a](float score, float2 ml) {
+            return __builtin_amdgcn_exp2f(__builtin_fmaf(score, a.scale, -ml.x)) * ml.y;
+        };
         for (int r = a.causal ? max(0, j - past) * a.group : 0; r < rows; r += 4) {
             float2 ml[4];
             float4 x[4];
@@ -80,10 +88,10 @@ __global__ __launch_bounds__(kThreads) void cache_weigh_scores_kernel(CacheWeigh
             }
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                if (j < end[i]) sum.x += __builtin_amdgcn_exp2f(x[i].x - ml[i].x) * ml[i].y;
-                if (j + 1 < end[i]) sum.y += __builtin_amdgcn_exp2f(x[i].y - ml[i].x) * ml[i].y;
-                if (j + 2 < end[i]) sum.z += __builtin_amdgcn_exp2f(x[i].z - ml[i].x) * ml[i].y;
-                if (j + 3 < end[i]) sum.w += __builtin_amdgcn_exp2f(x[i].w - ml[i].x) * ml[i].y;
+                if (j < end[i]) sum.x += weight(x[i].x, ml[i]);
+                if (j + 1 < end[i]) sum.y += weight(x[i].y, ml[i]);
+                if (j + 2 < end[i]) sum.z += weight(x[i].z, ml[i]);
+                if (j + 3 < end[i]) sum.w += weight(x[i].w, ml[i]);
             }
         }
         const int64_t at = weights_at(a.c, s, head, j);

@@ -48,3 +48,21 @@ def test_many_short_sequences_and_their_scores_twice(mx):  # noqa: F811
         check.weights(w, sums, None, t[some], list(range(len(some) + 1)), few)
         held = torch.arange(32) < torch.tensor(lens)[:, None]
         assert bool((w[:, 0][held] > 0).all()) and bool((w[:, 0][~held] == 0).all())
+
+
+def test_outputs_of_many_short_sequences(mx):  # noqa: F811
+    """The outputs beside those weights, of either way, within the bound of single outputs (a sample of sequences)."""
+    S = 20000
+    t = torch.arange(S, dtype=torch.int32).view(S, 1)
+    cache = filled(mx, S, 1, 32, 3)
+    lens = [1 + 7 * i % 32 for i in range(S)]
+    q = rows(S, 16, 6)
+    some = list(range(0, S, 97)) + [S - 1]
+    want, tol, _ = steps.attend(ref.Cache(*cache), q.cpu()[some], t[some], list(range(len(some) + 1)), [lens[i] for i in some],
+                                steps.causal)
+    assert float(tol.max()) < 0.05 * float(want.abs().max())  # (a bound that could fail)
+    wide = torch.cat((t, torch.full((S, 31), -1, dtype=torch.int32)), 1)
+    for table, m in ((t, 32), (wide, 1024)):
+        o = mx.cache_attend_weights(q, *cache, table.cuda(), ints(list(range(S + 1))), ints(lens), None, True, 1, m)[0].cpu()
+        assert bool(o.isfinite().all())
+        assert bool(((o[some].double() - want).abs() <= tol).all())

@@ -189,16 +189,20 @@ __device__ __forceinline__ int owner_of(const CacheArgs& c, int64_t w, int64_t g
 struct Placed {
     int s, head, chunk;  // s < 0: none
     __device__ __forceinline__ Placed(const CacheArgs& c, int chunks) {
-        const unsigned items = (unsigned)c.seqs * (unsigned)c.heads, id = blockIdx.x, n = (unsigned)chunks;
+        const unsigned items = (unsigned)c.seqs * (unsigned)c.heads, n = (unsigned)chunks;
+        const unsigned id = blockIdx.x + gridDim.x * blockIdx.y;
         const unsigned t = items < 8 ? id : id >> 3, k = t / n, item = items < 8 ? k : (id & 7) + 8 * k;
         chunk = (int)(t - k * n);
         s = item < items ? (int)(item / (unsigned)c.heads) : -1;
         head = (int)item - s * c.heads;
     }
 };
-inline unsigned placed_grid(const CacheArgs& c, int64_t chunks) {
-    const int64_t items = (int64_t)c.seqs * c.heads;
-    return (unsigned)((items < 8 ? items : (items + 7) / 8 * 8) * chunks);
+// Its grid, of so many threads each: two dimensions where one would pass a launch's 2^32.
+inline dim3 placed_grid(const CacheArgs& c, int64_t chunks, int threads) {
+    const int64_t items = (int64_t)c.seqs * c.heads, n = (items < 8 ? items : (items + 7) / 8 * 8) * chunks;
+    int64_t rows = 1;  // (n is a multiple of 8 where there are so many)
+    while (n / rows * threads >> 32) rows *= 2;
+    return dim3((unsigned)(n / rows), (unsigned)rows);
 }
 
 }  // namespace mxattn

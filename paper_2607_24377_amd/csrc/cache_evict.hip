@@ -826,7 +826,7 @@ hipError_t launch_cache_select(const SelectArgs& args, hipStream_t stream) {
     }
     a.chunks = (int)((reach + a.chunk_keys - 1) / a.chunk_keys);
     a.item_bytes = Lists::bytes(a.chunks);
-    const unsigned grid = placed_grid(a.c, a.chunks);
+    const dim3 grid = placed_grid(a.c, a.chunks, kManyThreads);
     cache_select_digits_kernel<<<grid, kManyThreads, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     cache_select_aside_kernel<<<grid, kManyThreads, 0, stream>>>(a);
@@ -842,7 +842,7 @@ hipError_t launch_cache_compact(const CompactArgs& a, hipStream_t stream) {
     const int64_t turns = (a.width / kBlockTokens + 2 + kWaves - 1) / kWaves;
     const int64_t most = ((int64_t)1 << 22) / ((int64_t)a.c.seqs * a.c.heads);
     const int64_t runs = a.in_place ? 1 : std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(turns, most), 32767));
-    cache_compact_kernel<<<placed_grid(a.c, 2 * runs), kThreads, 0, stream>>>(a, (int)runs);
+    cache_compact_kernel<<<placed_grid(a.c, 2 * runs, kThreads), kThreads, 0, stream>>>(a, (int)runs);
     return hipGetLastError();
 }
 

@@ -325,7 +325,8 @@ constexpr int64_t kMostScores = (int64_t)1 << 30;
 
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
-// Workgroups of an item: one for each `keys` keys, but no launch past 2^32 threads.
+// Workgroups of an item: one for each `keys` keys, but no more than 2^22 of all items where
+// those are fewer, and one of each otherwise (they are below 2^24).
 int chunks_of(const CacheAttendArgs& a, int64_t max_kv, int keys) {
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 22) / ((int64_t)a.c.seqs * a.c.heads));
     return (int)std::min<int64_t>(most, (max_kv + keys - 1) / keys);
@@ -368,11 +369,11 @@ hipError_t launch_cache_weigh(CacheWeighArgs w, int64_t max_q, int64_t max_kv, h
     if (hipError_t e = launch_cache_attend(a, max_q, max_kv, stream)) return e;
     if (a.kind == kWeigh) {
         const int chunks = chunks_of(a, max_kv, 4 * kThreads);
-        cache_weigh_scores_kernel<<<placed_grid(a.c, chunks), kThreads, 0, stream>>>(w, chunks);
+        cache_weigh_scores_kernel<<<placed_grid(a.c, chunks, kThreads), kThreads, 0, stream>>>(w, chunks);
         return hipGetLastError();
     }
     const int chunks = chunks_of(a, max_kv, kKeyWaves * kBlockTokens);
-    const unsigned grid = placed_grid(a.c, (int64_t)chunks * w.runs);
+    const dim3 grid = placed_grid(a.c, (int64_t)chunks * w.runs, 64 * kWaves);
     if (kStepRows % a.group == 0)
         cache_weigh_rows_kernel<true><<<grid, 64 * kWaves, 0, stream>>>(w, chunks, w.runs);
     else
@@ -380,7 +381,7 @@ hipError_t launch_cache_weigh(CacheWeighArgs w, int64_t max_q, int64_t max_kv, h
     if (hipError_t e = hipGetLastError()) return e;
     if (w.runs > 1) {
         const int sums = (int)((max_kv + kThreads - 1) / kThreads);
-        cache_weigh_runs_kernel<<<placed_grid(a.c, sums), kThreads, 0, stream>>>(w, sums, w.runs);
+        cache_weigh_runs_kernel<<<placed_grid(a.c, sums, kThreads), kThreads, 0, stream>>>(w, sums, w.runs);
     }
     return hipGetLastError();
 }

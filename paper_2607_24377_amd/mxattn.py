@@ -126,6 +126,20 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory for what a call writes.  On a stream that is given it is that stream's: what the current stream's
+    allocator has free may still be in use by work enqueued there.  It is not reused before the current stream, where
+    the caller has the tensor, is done with it either."""
+    if stream is not None:
+        here, there = torch.cuda.current_stream(device), _stream(stream)
+        if there != here.cuda_stream:
+            with torch.cuda.stream(torch.cuda.ExternalStream(there, device)):
+                t = torch.empty(shape, dtype=dtype, device=device)
+            t.record_stream(here)
+            return t
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _check(st: int, where: str):
     if st != OK:
         raise MxattnError(st, where)
@@ -160,9 +174,9 @@ def quantize(x: torch.Tensor, block_axis: int, mode, stream=None, codes=None, sc
     B, H, N, d = _bhnd(x)
     cs, ss = code_shapes(block_axis, B, H, N, d)
     if codes is None:
-        codes = torch.empty(cs, dtype=torch.uint8, device=x.device)
+        codes = _empty(cs, torch.uint8, x.device, stream)
     if scales is None:
-        scales = torch.empty(ss, dtype=torch.uint8, device=x.device)
+        scales = _empty(ss, torch.uint8, x.device, stream)
     st = lib().mxattn_quantize(x.data_ptr(), codes.data_ptr(), scales.data_ptr(), block_axis,
                                _mode(mode), B, H, N, d, _stream(stream))
     _check(st, "mxattn_quantize")
@@ -174,9 +188,9 @@ def quantize_qmax(x: torch.Tensor, block_axis: int, qmax: float, stream=None, co
     B, H, N, d = _bhnd(x)
     cs, ss = code_shapes(block_axis, B, H, N, d)
     if codes is None:
-        codes = torch.empty(cs, dtype=torch.uint8, device=x.device)
+        codes = _empty(cs, torch.uint8, x.device, stream)
     if scales is None:
-        scales = torch.empty(ss, dtype=torch.uint8, device=x.device)
+        scales = _empty(ss, torch.uint8, x.device, stream)
     st = lib().mxattn_quantize_qmax(x.data_ptr(), codes.data_ptr(), scales.data_ptr(), block_axis,
                                     float(qmax), B, H, N, d, _stream(stream))
     _check(st, "mxattn_quantize_qmax")
@@ -189,7 +203,7 @@ def qmax_sse(x: torch.Tensor, block_axis: int, qs, stream=None, out=None):
     B, H, N, d = _bhnd(x)
     q = (ctypes.c_double * len(qs))(*[float(v) for v in qs])
     if out is None:
-        out = torch.empty((B * H, len(qs)), dtype=torch.float64, device=x.device)
+        out = _empty((B * H, len(qs)), torch.float64, x.device, stream)
     st = lib().mxattn_qmax_sse(x.data_ptr(), block_axis, ctypes.cast(q, ctypes.c_void_p), len(qs),
                                out.data_ptr(), B, H, N, d, _stream(stream))
     _check(st, "mxattn_qmax_sse")
@@ -211,7 +225,7 @@ def softmax_rows(q: torch.Tensor, k: torch.Tensor, row0: int = 0, rows: int | No
     rows = Nq - row0 if rows is None else rows
     ld = (Nkv + 3) // 4 * 4 if ld is None else ld
     if out is None:
-        out = torch.empty((B, H, rows, ld), dtype=torch.float32, device=q.device)
+        out = _empty((B, H, rows, ld), torch.float32, q.device, stream)
     st = lib().mxattn_softmax_rows(q.data_ptr(), k.data_ptr(), out.data_ptr(), B, H, Nq, Nkv, d, row0,
                                    rows, ld, _stream(stream))
     _check(st, "mxattn_softmax_rows")
@@ -226,7 +240,7 @@ def rowsum_diag(p: torch.Tensor, N: int, mode, gamma: float = 1.0, stream=None, 
     ld = p.shape[-1]
     rows = p.numel() // ld
     if out is None:
-        out = torch.empty((rows, 8), dtype=torch.float64, device=p.device)
+        out = _empty((rows, 8), torch.float64, p.device, stream)
     st = lib().mxattn_rowsum_diag(p.data_ptr(), rows, N, ld, _mode(mode), float(gamma), out.data_ptr(),
                                   _stream(stream))
     _check(st, "mxattn_rowsum_diag")
@@ -241,7 +255,7 @@ def attention_rowsum_diag(q: torch.Tensor, k: torch.Tensor, mode, gamma: float =
     if (Bk, Hk, dk) != (B, H, d):
         raise ValueError("k must be [B, H, Nkv, d] with q's B, H, d")
     if out is None:
-        out = torch.empty((B, H, Nq, 8), dtype=torch.float64, device=q.device)
+        out = _empty((B, H, Nq, 8), torch.float64, q.device, stream)
     st = lib().mxattn_attention_rowsum_diag(q.data_ptr(), k.data_ptr(), B, H, Nq, Nkv, d, _mode(mode),
                                             float(gamma), out.data_ptr(), _stream(stream))
     _check(st, "mxattn_attention_rowsum_diag")
@@ -254,7 +268,7 @@ def forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mode, out=None, s
     if _bhnd(k) != q.shape or _bhnd(v) != q.shape:
         raise ValueError("q, k, v must have the same shape")
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     st = lib().mxattn_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, H, N, d,
                               _mode(mode), _stream(stream))
     _check(st, "mxattn_forward")
@@ -266,7 +280,7 @@ def attend(qc, qs, kc, ks, vc, vs, N: int, mode, out=None, stream=None):
     B, H = qc.shape[0], qc.shape[1]
     d = qc.shape[3] * 2
     if out is None:
-        out = torch.empty((B, H, N, d), dtype=torch.bfloat16, device=qc.device)
+        out = _empty((B, H, N, d), torch.bfloat16, qc.device, stream)
     st = lib().mxattn_attend(qc.data_ptr(), qs.data_ptr(), kc.data_ptr(), ks.data_ptr(),
                              vc.data_ptr(), vs.data_ptr(), out.data_ptr(), B, H, N, d, _mode(mode),
                              _stream(stream))
@@ -281,7 +295,7 @@ def cross_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mode, out=N
     if (Bk, Hk, dk) != (B, H, d) or _bhnd(v) != k.shape:
         raise ValueError("k and v must be [B, H, Nkv, d] with q's B, H, d")
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     st = lib().mxattn_cross_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, H,
                                     Nq, Nkv, d, _mode(mode), _stream(stream))
     _check(st, "mxattn_cross_forward")
@@ -293,7 +307,7 @@ def cross_attend(qc, qs, kc, ks, vc, vs, Nq: int, Nkv: int, mode, out=None, stre
     B, H = qc.shape[0], qc.shape[1]
     d = qc.shape[3] * 2
     if out is None:
-        out = torch.empty((B, H, Nq, d), dtype=torch.bfloat16, device=qc.device)
+        out = _empty((B, H, Nq, d), torch.bfloat16, qc.device, stream)
     st = lib().mxattn_cross_attend(qc.data_ptr(), qs.data_ptr(), kc.data_ptr(), ks.data_ptr(),
                                    vc.data_ptr(), vs.data_ptr(), out.data_ptr(), B, H, Nq, Nkv, d,
                                    _mode(mode), _stream(stream))
@@ -380,7 +394,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
     qp, qs = _heads(q, "q", dev)
     B, Hq, N, d = q.shape
     if q_out is None:
-        q_out = q.new_empty((B, Hq, N, d))
+        q_out = _empty((B, Hq, N, d), q.dtype, q.device, stream)
         qop, qos = q_out.data_ptr(), None
     elif q_out.shape != q.shape:
         raise ValueError("q_out must have q's shape")
@@ -394,7 +408,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight=None, k_weigh
         if k.shape != (B, Hkv, N, d):
             raise ValueError("k must be [B, Hkv, N, d] with q's B, N, d")
         if k_out is None:
-            k_out = q.new_empty((B, Hkv, N, d))
+            k_out = _empty((B, Hkv, N, d), q.dtype, q.device, stream)
             kop = k_out.data_ptr()
         elif k_out.shape != k.shape:
             raise ValueError("k_out must have k's shape")
@@ -494,7 +508,7 @@ def _attend(name, q, batch, middle, max_q, max_kv, out, stream, workspace="mxatt
     if callable(middle):
         middle = middle(dev, cache, heads, tokens)
     if out is None:
-        out = q.new_empty((tokens, Hq, d))
+        out = _empty((tokens, Hq, d), q.dtype, q.device, stream)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     op, ost = _token_rows(out, "out", dev)
@@ -572,11 +586,11 @@ def cache_select(weights: torch.Tensor, page_table, kv_len, budget: int, sinks: 
     seqs, max_pages = page_table.shape
     i32 = torch.int32
     if kept is None:
-        kept = torch.empty((seqs, heads, max(budget, 0)), dtype=i32, device=weights.device)
+        kept = _empty((seqs, heads, max(budget, 0)), i32, weights.device, stream)
     elif kept.shape != (seqs, heads, budget):
         raise ValueError("kept must be [seqs, heads, budget]")
     if counts is None:
-        counts = torch.empty((seqs,), dtype=i32, device=weights.device)
+        counts = _empty((seqs,), i32, weights.device, stream)
     L, work, size = _lib or lib(), None, 0
     if stream is None:  # (as for attention)
         size = L.mxattn_cache_select_workspace(page, seqs, max_pages, heads)

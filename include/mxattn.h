@@ -444,9 +444,10 @@ int mxattn_cache_attend_tree(const void* q, int64_t q_stride, const uint8_t* k_c
  *                    Hq / Hkv heads
  * in fp32, p the probabilities that O is made of (before they are rounded to f16).  Scores
  * are fp32 sums of exact products in this call, whatever its bounds: off by 2^-20 of
- * sum |q k| and less, and the p of a row add up to 1 within 2^-16.  Weights lie beside the cache, fp32
- * [pages, Hkv, page_tokens]; those of other positions and sequences are not written.
- *   weights      NULL: zeros
+ * sum |q k| and less, and the p of a row add up to 1 but for the rounding of their fp32 sums
+ * (2^-16 over 3000 keys).  Weights lie beside the cache, fp32 [pages, Hkv, page_tokens]; those
+ * of other positions and sequences are not written.
+ *   weights      NULL: zeros.  A key that was new to a call without weights has what lies there.
  *   weights_out  may be `weights`; must not overlap it otherwise
  *   max_kv       here a limit: a sequence that is longer counts as one of impossible
  *                length (its queries get NaN, its weights are not written).
@@ -476,6 +477,8 @@ size_t mxattn_cache_attend_weights_workspace(int64_t page_tokens, int64_t seqs, 
  *   counts   device int32 [seqs]: min(kv_len, budget); 0 for an impossible length
  *   budget   1 .. 2^24, sinks >= 0, recent >= 0, sinks + recent <= budget
  *            (MXATTN_ERR_VALUE otherwise); seqs * Hkv < 2^22
+ * Kernels and workspace go by the table's width, max_pages * page_tokens: short sequences
+ * are cut faster under a narrow table.
  *   workspace  as mxattn_cache_attend's, of mxattn_cache_select_workspace() bytes: none
  *            where max_pages * page_tokens <= 16384 (65536 from seqs * Hkv = 128 on), else at
  *            most 2.3 MB for each sequence and KV head.  It shares no byte with the other
@@ -505,7 +508,12 @@ size_t mxattn_cache_select_workspace(int64_t page_tokens, int64_t seqs, int64_t 
  *              place, where kept ascends and kept[i] >= base + i (anything else gives
  *              undefined contents there; nothing out of range).
  *   weights    device fp32 [pages, Hkv, page_tokens], or NULL
- * In place a head's blocks are moved one turn after another; to other pages all at once.
+ * Keys keep the rotation that they were stored with.  Where that is by position, tokens that
+ * come later need theirs given (mxattn_cache_append's `positions`, and their queries'): a
+ * token's place in its sequence, which the calls take without them, is no longer its position.
+ * In place a head's K and V are two workgroups' work, 128 tokens a turn, one turn after
+ * another: meant for a few blocks (accepted drafts), and right but slow for many.  To other
+ * pages all turns run at once.
  * Sequences of a call must not share pages that are written.  seqs * Hkv < 2^22. */
 int mxattn_cache_compact(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int64_t pages,
                          int64_t page_tokens, const int32_t* page_table, int64_t seqs, int64_t max_pages,

@@ -609,7 +609,8 @@ def cache_compact(k_codes: torch.Tensor, k_scales, v_codes, v_scales, page_table
     """Move kept tokens together: position base + i (i < counts) of a sequence becomes what was at kept[.., i], in K, V
     and, if given, fp32 weights [pages, Hkv, page_tokens].  kept: int32 [seqs, Hkv or 1, width]; counts, base (None: 0):
     int32 [seqs].  out_table: the page table of where they go, pages that hold none of the sources; None: in place
-    (kept ascending, kept[i] >= base + i)."""
+    (kept ascending, kept[i] >= base + i; a head's blocks one after another, so for a few blocks).  Keys keep their
+    rotation: tokens appended afterwards need `positions`, as their place in the sequence is no longer their position."""
     if not k_codes.is_cuda or k_codes.dim() != 6 or kept.dim() != 3:
         raise ValueError("k_codes must be a CUDA tensor as of cache_shapes, kept [seqs, heads or 1, width]")
     dev, d = k_codes.get_device(), 128

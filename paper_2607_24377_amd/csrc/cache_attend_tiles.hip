@@ -25,7 +25,7 @@
 // tiles of a workgroup, of which three steps are 6.  Trees of 25 drafts of 16 sequences
 // over 6000 keys, 40 heads on 8: 48 and 8, of which 20 stay however few the keys are (the
 // share's place, first loads, parts of 64 KiB written); trees of 64 over 65536 keys, 2
-// sequences: 157 and 10, 870 TFLOP/s.  Masked steps are said to be rare, so that the others'
+// sequences: 161 to 166 and 10, 830 to 850 TFLOP/s.  Masked steps are said to be rare, so that the others'
 // code runs straight on: those prompts 148 us without, the frame 3 % more.
 #include "cache_attend.h"
 

@@ -17,8 +17,8 @@
 // 160 rows of scores of some hundreds added up to 159.97).
 //
 // Bound by what attention leaves and by the exponentials: 64 tokens over 8200 keys, 32 heads
-// on 8, 57 MB, 15 us; 4 prompts of up to 2048 tokens 135 to 139 us, beside 250 to 270 for their
-// attention (86 vector instructions for 32 x 32 scores, 16 of them exponentials; vector issue
+// on 8, 57 MB, 15 us; 4 prompts of up to 2048 tokens 135 to 139 us, beside 261 and 19 for their
+// attention, which FP8 products would do in 241 (86 vector instructions for 32 x 32 scores, 16 of them exponentials; vector issue
 // busy 44 %, matrix cores 28 %; the longest prompt's 128 steps follow one another); 1560 rows
 // x 32760 keys x 40 heads 730.
 #include "cache_attend.h"

@@ -66,3 +66,17 @@ def test_outputs_of_many_short_sequences(mx):  # noqa: F811
         o = mx.cache_attend_weights(q, *cache, table.cuda(), ints(list(range(S + 1))), ints(lens), None, True, 1, m)[0].cpu()
         assert bool(o.isfinite().all())
         assert bool(((o[some].double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("new,past,bounds", [([1, 3], [900, 500], (3, 903)), ([40, 60], [300, 1900], (60, 2000))])
+@pytest.mark.parametrize("byte,power", [(0, 116), (0, 124), (1, 123), (20, 104)])
+def test_keys_of_the_smallest_scales(mx, new, past, bounds, byte, power):  # noqa: F811
+    """Scale bytes down to 0 (2^-127, which fp32 holds as a subnormal) under queries so large that scores count."""
+    table, start, lens, pages = batch(new, past, 64)
+    cache = filled(mx, pages, 2, 64, 7)
+    cache[1].fill_(byte)
+    q = (rows(start[-1], 8, 5).double().clamp(-3, 3) * 2.0 ** power).to(torch.bfloat16)
+    want, tol, sums = steps.attend(ref.Cache(*cache), q.cpu(), table, start, lens, steps.causal)
+    o, w = mx.cache_attend_weights(q, *cache, table.cuda(), ints(start), ints(lens), None, True, *bounds)
+    assert bool(((o.cpu().double() - want).abs() <= tol).all())
+    check.weights(w.cpu(), sums, None, table, start, lens)
